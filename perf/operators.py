@@ -25,7 +25,7 @@ import torch
 own = False
 
 K = 256
-LOW_E, HIGH_E = -64, 64     # exponents of an all-zero page, and of the largest that is kept
+LOW_E, HIGH_E = -40, 40     # exponents of an all-zero page, and of the largest that is kept
 
 
 def listed():
