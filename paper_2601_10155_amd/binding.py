@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import os
 import warnings
+from typing import NamedTuple
 
 import torch
 
@@ -44,6 +45,12 @@ class _PythonOnly:
 class _Shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("d_k", ctypes.c_int32),
                 ("m", ctypes.c_int32), ("K", ctypes.c_int32)]
+
+
+class _Pool(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("H", ctypes.c_int32), ("d_k", ctypes.c_int32), ("m", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("value_type", ctypes.c_int), ("codes", ctypes.c_void_p),
+                ("values", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
 
 
 def lib_path() -> str:
@@ -101,6 +108,29 @@ def load_library():
         lib.lookat_probe_score_prefill_form.restype = i32
         lib.lookat_kmeans_step.argtypes = [sp, i64, vp, vp, vp, vp, vp]
         lib.lookat_kmeans_step.restype = ctypes.c_int
+        pp = ctypes.POINTER(_Pool)
+        lib.lookat_pages_write.argtypes = [pp, i32, i64, vp, i64, vp, ctypes.c_int, i64, vp, i32, i64, vp, vp, vp]
+        lib.lookat_pages_write.restype = ctypes.c_int
+        lib.lookat_attend_pages_workspace_bytes.argtypes = [pp, i32, i32, i32, i64, i32]
+        lib.lookat_attend_pages_workspace_bytes.restype = sz
+        lib.lookat_attend_pages_auto_splits.argtypes = [pp, i32, i32, i32, i64]
+        lib.lookat_attend_pages_auto_splits.restype = i32
+        lib.lookat_attend_pages.argtypes = [pp, i32, i32, vp, vp, i32, i64, vp, i64, f32, i32, vp, sz, vp, vp]
+        lib.lookat_attend_pages.restype = ctypes.c_int
+        lib.lookat_pages_copy.argtypes = [pp, i32, vp, vp, vp]
+        lib.lookat_pages_copy.restype = ctypes.c_int
+        lib.lookat_pages_fork.argtypes = [pp, i32, vp, i32, i64, vp, vp, i32, vp, vp, vp]
+        lib.lookat_pages_fork.restype = ctypes.c_int
+        lib.lookat_pages_free.argtypes = [pp, i32, vp, i32, i64, vp, vp, i32, vp, vp]
+        lib.lookat_pages_free.restype = ctypes.c_int
+        lib.lookat_pages_reserve_workspace_bytes.argtypes = [pp, i32]
+        lib.lookat_pages_reserve_workspace_bytes.restype = sz
+        lib.lookat_pages_reserve.argtypes = [pp, i32, vp, i32, i64, vp, vp, vp, vp, vp, sz, vp]
+        lib.lookat_pages_reserve.restype = ctypes.c_int
+        lib.lookat_pages_compact_workspace_bytes.argtypes = [pp]
+        lib.lookat_pages_compact_workspace_bytes.restype = sz
+        lib.lookat_pages_compact.argtypes = [pp, i32, vp, i32, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        lib.lookat_pages_compact.restype = ctypes.c_int
         lib.lookat_probe_stream_read.argtypes = [vp, sz, vp, vp]
         lib.lookat_probe_stream_read.restype = ctypes.c_int
         lib.lookat_probe_stream_write.argtypes = [vp, sz, ctypes.c_uint32, vp]
@@ -593,6 +623,243 @@ def lookat_kmeans(calib: torch.Tensor, codebooks: torch.Tensor, iters: int) -> t
         lookat_kmeans_step(calib, cur, nxt, assign)
         cur, nxt = nxt, cur
     return cur
+
+
+# ---- the paged cache with 8-bit values (include/lookat_pages.h) ------------------------------------------------
+LOOKAT_VALUES_I8 = 1
+LOOKAT_VALUES_E4M3 = 2
+
+
+class PagePool(NamedTuple):
+    """The pages of one layer's cache: codes [P,H,page,m] uint8, values [P,H,page/8,d_k,8] int8 or float8_e4m3fn (token t of a
+    page at [t // 8, :, t % 8]), exponents [P,H] int8; a stored q stands for q * 2^exponent."""
+    codes: torch.Tensor
+    values: torch.Tensor
+    exponents: torch.Tensor
+
+
+def page_pool(pages: int, H: int, d_k: int, m: int, page: int = 64, value_dtype: torch.dtype = torch.int8, device="cuda") -> PagePool:
+    """A pool of `pages` free pages for `page` tokens of H heads each (value_dtype int8 or float8_e4m3fn)."""
+    if value_dtype not in (torch.int8, torch.float8_e4m3fn):
+        raise TypeError(f"expected int8 or float8_e4m3fn values, got {value_dtype}")
+    zeros = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)  # noqa: E731
+    return PagePool(zeros(pages, H, page, m), zeros(pages, H, page // 8, d_k, 8).view(value_dtype), zeros(pages, H).view(torch.int8))
+
+
+def _pool(pool: PagePool) -> _Pool:
+    codes, values, exponents = pool
+    if codes.dim() != 4 or values.dim() != 5 or codes.dtype != torch.uint8 or exponents.dtype != torch.int8:
+        raise ValueError("a pool is codes uint8 [P,H,page,m], values [P,H,page/8,d_k,8] and exponents int8 [P,H]")
+    P, H, page, m = codes.shape
+    if tuple(values.shape[:2]) != (P, H) or values.shape[2] * 8 != page or values.shape[4] != 8 or tuple(exponents.shape) != (P, H):
+        raise ValueError("the pool's values must be [P,H,page/8,d_k,8] and its exponents [P,H] for codes [P,H,page,m]")
+    if values.dtype == torch.int8:
+        tag = LOOKAT_VALUES_I8
+    elif values.dtype == torch.float8_e4m3fn:
+        tag = LOOKAT_VALUES_E4M3
+    else:
+        raise TypeError(f"expected int8 or float8_e4m3fn values, got {values.dtype}")
+    if not (codes.is_contiguous() and values.is_contiguous() and exponents.is_contiguous()):
+        raise ValueError("the pool's tensors must be contiguous")
+    _dev(codes, "codes")
+    if values.device != codes.device or exponents.device != codes.device:
+        raise ValueError("the pool's tensors must live on one device")
+    return _Pool(P, H, values.shape[3], m, page, tag, codes.data_ptr(), values.data_ptr(), exponents.data_ptr())
+
+
+def _int_array(t: torch.Tensor, name: str, pool: PagePool, n: int | None = None) -> int:
+    """A dense int32 array on the pool's device; its address."""
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be a contiguous int32 [{'n' if n is None else n}] tensor")
+    if t.device != pool.codes.device:
+        raise ValueError(f"{name} must live on the pool's device")
+    return t.data_ptr()
+
+
+def _table(t: torch.Tensor, name: str, pool: PagePool) -> tuple[int, int, int, int]:
+    """Rows, entries per row, row stride and address of a table whose rows are dense."""
+    if t.dtype != torch.int32 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be int32 [S,W] with dense rows")
+    if t.device != pool.codes.device:
+        raise ValueError(f"{name} must live on the pool's device")
+    S, W = t.shape
+    return S, W, t.stride(0) if S > 1 else max(W, 1), t.data_ptr()
+
+
+class _OnDevice:
+    """The pool's device as the current one during a call, and the stream that is current there."""
+
+    def __init__(self, pool: PagePool):
+        self.index = pool.codes.device.index
+        self.guard = None if torch.cuda.current_device() == self.index else torch.cuda.device(self.index)
+
+    def __enter__(self) -> int:
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *args):
+        if self.guard is not None:
+            self.guard.__exit__(*args)
+
+
+def _scratch(workspace, need: int, pool: PagePool) -> torch.Tensor | None:
+    if not need:
+        return workspace
+    if workspace is not None and workspace.device != pool.codes.device:
+        raise ValueError("workspace must live on the pool's device")
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=pool.codes.device)
+    return workspace
+
+
+def _bytes(t: torch.Tensor | None) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _ptr(t: torch.Tensor | None) -> int | None:
+    return None if t is None else t.data_ptr()
+
+
+def lookat_pages_write(pool: PagePool, codes: torch.Tensor, values: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                       counts: torch.Tensor | None = None) -> None:
+    """The last counts[b] tokens (default N) of every sequence enter its pages: codes [B,H,N,m] uint8 (of lookat_encode_keys), values
+    [B,H,N,d_k] fp16|fp32 in rows 0..counts[b]-1, table [B,W] int32, lengths [B] int32 INCLUDING them.  In place."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    if codes.dim() != 4 or values.dim() != 4 or codes.dtype != torch.uint8 or tuple(codes.shape[:3]) != tuple(values.shape[:3]) \
+            or codes.shape[1] != c_pool.H or codes.shape[3] != c_pool.m or values.shape[3] != c_pool.d_k:
+        raise ValueError("codes must be uint8 [B,H,N,m] and values [B,H,N,d_k] of the pool's heads")
+    B, H, N, _ = codes.shape
+    tag = _dtype_tag(values)
+    if codes.device != pool.codes.device or values.device != pool.codes.device:
+        raise ValueError("codes and values must live on the pool's device")
+    rows, W, stride, t_ptr = _table(table, "table", pool)
+    if rows != B:
+        raise ValueError("table must have a row for every sequence")
+    l_ptr = _int_array(lengths, "lengths", pool, B)
+    n_ptr = None if counts is None else _int_array(counts, "counts", pool, B)
+    if N == 0 or B == 0:
+        return
+    with _OnDevice(pool) as stream:
+        _check(lib.lookat_pages_write(ctypes.byref(c_pool), B, N, codes.data_ptr(), _bh_stride(codes, "codes"), values.data_ptr(), tag,
+                                      _bh_stride(values, "values"), t_ptr, W, stride, l_ptr, n_ptr, stream))
+
+
+def attend_pages_workspace_bytes(pool: PagePool, B: int, group: int, W: int, max_length: int = 0, num_splits: int = 0) -> int:
+    return int(load_library().lookat_attend_pages_workspace_bytes(ctypes.byref(_pool(pool)), B, group, W, max_length, num_splits))
+
+
+def attend_pages_auto_splits(pool: PagePool, B: int, group: int, W: int, max_length: int = 0) -> int:
+    return int(load_library().lookat_attend_pages_auto_splits(ctypes.byref(_pool(pool)), B, group, W, max_length))
+
+
+def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, scale: float, max_length: int = 0,
+                        num_splits: int = 0, workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """lut [B,H*g,m,256] fp32 (of lookat_build_lut; g query heads share a key/value head), table [B,W] int32, lengths [B] int32
+    -> out [B,H*g,d_k] fp32; zeros for a sequence without tokens.  max_length: the longest length the caller knows of (0: W * page);
+    it sizes the launch only."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    B, W, stride, t_ptr = _table(table, "table", pool)
+    H, d_k, m = c_pool.H, c_pool.d_k, c_pool.m
+    if lut.dim() != 4 or lut.shape[0] != B or lut.shape[1] % H or tuple(lut.shape[2:]) != (m, 256) or lut.dtype != torch.float32 \
+            or not lut.is_contiguous():
+        raise ValueError("lut must be contiguous fp32 [B,H*g,m,256]")
+    g = lut.shape[1] // H
+    l_ptr = _int_array(lengths, "lengths", pool, B)
+    if out is None:
+        out = torch.empty((B, H * g, d_k), dtype=torch.float32, device=pool.codes.device)
+    if out.dtype != torch.float32 or out.numel() != B * H * g * d_k or not out.is_contiguous():
+        raise ValueError("out must be contiguous fp32 [B,H*g,d_k]")
+    if lut.device != pool.codes.device or out.device != pool.codes.device:
+        raise ValueError("lut and out must live on the pool's device")
+    with _OnDevice(pool) as stream:
+        need = lib.lookat_attend_pages_workspace_bytes(ctypes.byref(c_pool), B, g, W, max_length, num_splits)
+        workspace = _scratch(workspace, need, pool)
+        _check(lib.lookat_attend_pages(ctypes.byref(c_pool), B, g, lut.data_ptr(), t_ptr, W, stride, l_ptr, int(max_length), float(scale),
+                                       int(num_splits), _ptr(workspace), _bytes(workspace), out.data_ptr(), stream))
+    return out
+
+
+def lookat_pages_copy(pool: PagePool, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Pages src[i] onto pages dst[i] (int32 [n]; the destinations distinct and none of them a source)."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    n = src.shape[0] if src.dim() else 0
+    s_ptr, d_ptr = _int_array(src, "src", pool), _int_array(dst, "dst", pool, n)
+    with _OnDevice(pool) as stream:
+        _check(lib.lookat_pages_copy(ctypes.byref(c_pool), n, s_ptr, d_ptr, stream))
+
+
+def _books(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor) -> tuple:
+    S, W, stride, t_ptr = _table(table, "table", pool)
+    return S, t_ptr, W, stride, _int_array(lengths, "lengths", pool, S), _int_array(refs, "refs", pool, pool.codes.shape[0])
+
+
+def lookat_pages_fork(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, src: torch.Tensor,
+                      dst: torch.Tensor) -> None:
+    """The empty sequences dst[i] begin as src[i]: rows and lengths copied, pages shared and counted once more.
+    table [S,W], lengths [S], refs [P], src, dst [n], all int32.  In place."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    books = _books(pool, table, lengths, refs)
+    n = src.shape[0] if src.dim() else 0
+    s_ptr, d_ptr = _int_array(src, "src", pool), _int_array(dst, "dst", pool, n)
+    with _OnDevice(pool) as stream:
+        _check(lib.lookat_pages_fork(ctypes.byref(c_pool), *books, n, s_ptr, d_ptr, stream))
+
+
+def lookat_pages_free(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, slots: torch.Tensor) -> None:
+    """Gives up the sequences `slots` (int32 [n]): their pages are counted once less, their rows become -1, their lengths 0.  In place."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    books = _books(pool, table, lengths, refs)
+    ptr = _int_array(slots, "slots", pool)
+    with _OnDevice(pool) as stream:
+        _check(lib.lookat_pages_free(ctypes.byref(c_pool), *books, slots.shape[0], ptr, stream))
+
+
+def lookat_pages_reserve(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, new_lengths: torch.Tensor,
+                         missing: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Room for the sequences to grow to new_lengths [S] int32 (not above lengths: as it is): free pages in ascending order, shared last
+    pages copied, lengths set.  Returns `missing` [1] int32: 0, or how many pages are lacking and nothing was changed."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    books = _books(pool, table, lengths, refs)
+    ptr = _int_array(new_lengths, "new_lengths", pool, books[0])
+    if missing is None:
+        missing = torch.empty(1, dtype=torch.int32, device=pool.codes.device)
+    m_ptr = _int_array(missing, "missing", pool, 1)
+    with _OnDevice(pool) as stream:
+        workspace = _scratch(workspace, lib.lookat_pages_reserve_workspace_bytes(ctypes.byref(c_pool), books[0]), pool)
+        _check(lib.lookat_pages_reserve(ctypes.byref(c_pool), *books, ptr, m_ptr, _ptr(workspace), _bytes(workspace), stream))
+    return missing
+
+
+def lookat_pages_compact(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, table_out: torch.Tensor | None = None,
+                         refs_out: torch.Tensor | None = None, live: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The pages in use move to the lowest ids.  Returns the new table [S,W], the new refs [P] and live [1], the number of pages in use
+    (int32); the old table and refs are not changed."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    books = _books(pool, table, lengths, refs)
+    if table_out is None:
+        table_out = torch.empty(table.shape, dtype=torch.int32, device=pool.codes.device)
+    if refs_out is None:
+        refs_out = torch.empty_like(refs)
+    if live is None:
+        live = torch.empty(1, dtype=torch.int32, device=pool.codes.device)
+    S, W, stride, t_ptr = _table(table_out, "table_out", pool)
+    if (S, W) != (books[0], books[2]):
+        raise ValueError("table_out must have the table's shape")
+    r_ptr, l_ptr = _int_array(refs_out, "refs_out", pool, pool.codes.shape[0]), _int_array(live, "live", pool, 1)
+    with _OnDevice(pool) as device_stream:
+        workspace = _scratch(workspace, lib.lookat_pages_compact_workspace_bytes(ctypes.byref(c_pool)), pool)
+        _check(lib.lookat_pages_compact(ctypes.byref(c_pool), *books, t_ptr, stride, r_ptr, l_ptr, _ptr(workspace), _bytes(workspace),
+                                        device_stream))
+    return table_out, refs_out, live
 
 
 def lookat_probe_stream_read(src: torch.Tensor, sink: torch.Tensor) -> None:

@@ -61,7 +61,7 @@ def build(verbose: bool = True, force: bool = True) -> str:
         objs.append(obj)
         path = os.path.join(CSRC, src)
         deps = [path] + [os.path.join(CSRC, h) for h in os.listdir(CSRC) if h.endswith(".h")] + \
-               [os.path.join(ROOT, "include", "lookat.h")]
+               [os.path.join(ROOT, "include", h) for h in ("lookat.h", "lookat_pages.h")]
         if not force and os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
             continue
         cmd = [cc, *COMMON, *EXTRA.get(src, []), "-c", path, "-o", obj]
