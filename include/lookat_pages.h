@@ -135,7 +135,7 @@ int lookat_pages_free(const lookat_page_pool *pool, int32_t S, int32_t *table, i
  * lengths become the new ones.  If there are too few free pages, or a row is too short, NOTHING is changed and
  * missing[0] says by how many pages, else missing[0] = 0.
  * (Of several sequences that share a last page and all grow, all get a copy; the page itself becomes free.)
- *   new_lengths  [S] int32, must not be lengths itself;  missing  [1] int32
+ *   new_lengths  [S] int32, must not overlap lengths;  missing  [1] int32
  *   workspace    lookat_pages_reserve_workspace_bytes(pool, S) bytes, 16-byte aligned
  */
 size_t lookat_pages_reserve_workspace_bytes(const lookat_page_pool *pool, int32_t S);

@@ -33,45 +33,49 @@ __device__ __forceinline__ int clamp_length(int length, int W, int page_log2)
     return length < 0 ? 0 : length < most ? length : most;
 }
 
-// 16-byte units of one page: its codes, then its values (the exponents go apart: H bytes).
-__host__ __device__ __forceinline__ uint32_t page_units(const PoolArgs &p)
-{
-    return ((uint32_t)p.H << p.page_log2) * (uint32_t)(p.m + p.d_k) / 16u;
-}
-constexpr int kCopyThreads = 256;
-constexpr int kCopyUnits = 4;             // 16-byte units per thread and part, all requested before the first is stored
-constexpr uint32_t kCopyPart = kCopyThreads * kCopyUnits;
-__host__ __device__ __forceinline__ uint32_t page_parts(const PoolArgs &p) { return (page_units(p) + kCopyPart - 1) / kCopyPart; }
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// One workgroup of kCopyThreads copies part `part` of page src onto page dst (both in range, src != dst).
+// A page is copied in parts of one region, codes or values, kCopyPart 16-byte units each (the exponents, H bytes, go with part 0).
+constexpr int kCopyThreads = 256;
+constexpr int kCopyUnits = 4;             // per thread, all requested before the first is stored
+constexpr uint32_t kCopyPart = kCopyThreads * kCopyUnits;
+__host__ __device__ __forceinline__ uint32_t code_units(const PoolArgs &p) { return ((uint32_t)p.H << p.page_log2) * (uint32_t)p.m / 16u; }
+__host__ __device__ __forceinline__ uint32_t value_units(const PoolArgs &p) { return ((uint32_t)p.H << p.page_log2) * (uint32_t)p.d_k / 16u; }
+__host__ __device__ __forceinline__ uint32_t parts_of(uint32_t units) { return (units + kCopyPart - 1) / kCopyPart; }
+__host__ __device__ __forceinline__ uint32_t page_parts(const PoolArgs &p) { return parts_of(code_units(p)) + parts_of(value_units(p)); }
+
+// One workgroup of kCopyThreads copies part `part` of page src onto page dst (both in range, src != dst).  A thread's last units repeat the
+// region's last one instead of being skipped, so that all loads go out together, without a branch between them.
 __device__ __forceinline__ void copy_page_part(const PoolArgs &p, int src, int dst, uint32_t part)
 {
-    const uint32_t units = page_units(p);
-    const uint32_t code_units = ((uint32_t)p.H << p.page_log2) * (uint32_t)p.m / 16u;
-    const uint32_t value_units = units - code_units;
-    const uint4 *codes = reinterpret_cast<const uint4 *>(p.codes), *values = reinterpret_cast<const uint4 *>(p.values);
-    const int64_t code_from = (int64_t)src * code_units, code_to = (int64_t)dst * code_units;
-    const int64_t value_from = (int64_t)src * value_units, value_to = (int64_t)dst * value_units;
-    uint4 x[kCopyUnits];
+    const uint32_t code_parts = parts_of(code_units(p));
+    const bool values = part >= code_parts;
+    const uint32_t units = values ? value_units(p) : code_units(p);
+    const uint32_t u0 = (values ? part - code_parts : part) * kCopyPart + threadIdx.x;
+    u32x4 *base = reinterpret_cast<u32x4 *>(values ? p.values : p.codes);
+    const u32x4 *from = base + (int64_t)src * units;
+    u32x4 *to = base + (int64_t)dst * units;
+    int8_t e = 0;
+    const bool exponents = part == 0 && (int)threadIdx.x < p.H;
+    if (exponents)
+        e = p.exponents[(int64_t)src * p.H + threadIdx.x];
+    u32x4 x[kCopyUnits];
 #pragma unroll
     for (int k = 0; k < kCopyUnits; ++k) {
-        const uint32_t u = part * kCopyPart + k * kCopyThreads + threadIdx.x;
+        const uint32_t u = u0 + k * kCopyThreads;
+        x[k] = from[u < units ? u : units - 1];
+    }
+#pragma unroll
+    for (int k = 0; k < kCopyUnits; ++k) {
+        const uint32_t u = u0 + k * kCopyThreads;
         if (u < units)
-            x[k] = u < code_units ? codes[code_from + u] : values[value_from + (u - code_units)];
+            to[u] = x[k];
     }
-#pragma unroll
-    for (int k = 0; k < kCopyUnits; ++k) {
-        const uint32_t u = part * kCopyPart + k * kCopyThreads + threadIdx.x;
-        if (u < units) {
-            if (u < code_units)
-                reinterpret_cast<uint4 *>(p.codes)[code_to + u] = x[k];
-            else
-                reinterpret_cast<uint4 *>(p.values)[value_to + (u - code_units)] = x[k];
-        }
-    }
-    if (part == 0)
-        for (int h = threadIdx.x; h < p.H; h += kCopyThreads)
+    if (exponents) {
+        p.exponents[(int64_t)dst * p.H + threadIdx.x] = e;
+        for (int h = threadIdx.x + kCopyThreads; h < p.H; h += kCopyThreads)
             p.exponents[(int64_t)dst * p.H + h] = p.exponents[(int64_t)src * p.H + h];
+    }
 }
 
 #endif  // __HIPCC__

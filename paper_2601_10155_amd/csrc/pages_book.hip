@@ -485,7 +485,7 @@ extern "C" int lookat_pages_copy(const lookat_page_pool *pool, int32_t n, const 
     const PoolArgs p = pool_args(pool);
     const int64_t groups = (int64_t)n * page_parts(p);
     if (groups > 0x7fffffffLL)
-        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d pages of %u bytes exceed one launch", n, page_units(p) * 16);
+        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d pages of %u parts exceed one launch", n, page_parts(p));
     hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)groups), dim3(kCopyThreads), 0, static_cast<hipStream_t>(stream), p, src, dst, n,
                        page_parts(p));
     return check_launch("lookat_pages_copy");
@@ -544,8 +544,8 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
         return fail(LOOKAT_ERR_NULL, "new_lengths and missing must be non-NULL");
     if ((reinterpret_cast<uintptr_t>(new_lengths) | reinterpret_cast<uintptr_t>(missing)) & 3u)
         return fail(LOOKAT_ERR_ALIGN, "new_lengths and missing must be 4-byte aligned");
-    if (new_lengths == lengths)
-        return fail(LOOKAT_ERR_SHAPE, "new_lengths must not be lengths itself");
+    if (new_lengths < lengths + S && lengths < new_lengths + S)
+        return fail(LOOKAT_ERR_SHAPE, "new_lengths and lengths must not overlap");
     if (int rc = check_workspace(lookat_pages_reserve_workspace_bytes(pool, S), workspace, workspace_bytes))
         return rc;
     const PoolArgs p = pool_args(pool);

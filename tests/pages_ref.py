@@ -184,7 +184,7 @@ class Books:
 
     def reserve(self, new_lengths, cache=None):
         need = []                                       # (slot, entry, page to copy or None)
-        over = 0
+        count = over = 0
         for s in range(self.S):
             has, want = max(0, int(self.lengths[s])), int(new_lengths[s])
             if want <= has:
@@ -194,13 +194,13 @@ class Books:
                 i = self.table[s, has // self.page]
                 if 0 <= i < len(self.refs) and self.refs[i] > 1:
                     mine.append((s, has // self.page, int(i)))
-            last = -(-want // self.page)
-            mine += [(s, w, None) for w in range(-(-has // self.page), last)]
-            if mine:
+            first, last = -(-has // self.page), -(-want // self.page)
+            count += len(mine) + last - first
+            if mine or last > first:
                 over += max(0, last - self.W)
-            need += mine
+            need += mine + [(s, w, None) for w in range(first, min(last, self.W))]
         free = [i for i in range(len(self.refs)) if self.refs[i] <= 0]
-        missing = max(0, len(need) - len(free)) + over
+        missing = max(0, count - len(free)) + over
         if missing:
             return missing
         for (s, w, old), i in zip(need, free):

@@ -122,7 +122,7 @@ def test_upkeep_refusals(lib):  # noqa: F811
     assert c["copy"](pool(H=4096, page=128, d_k=128, m=16), n=1 << 30) == E_UNSUP
     r = c["reserve"]
     assert r(pool(), new=None) == E_NULL and r(pool(), missing=None) == E_NULL
-    assert r(pool(), new=FAKE) == E_SHAPE                                    # lengths itself
+    assert r(pool(), new=FAKE) == E_SHAPE and r(pool(), new=FAKE + 16) == E_SHAPE and r(pool(), new=FAKE - 4) == E_SHAPE      # over lengths
     need = lib.lookat_pages_reserve_workspace_bytes(ctypes.byref(pool()), 5)
     assert need > 0 and r(pool(), wsb=need - 1) == E_WS and r(pool(), ws=None) == E_WS and r(pool(), ws=FAKE + 4) == E_ALIGN
     k = c["compact"]
