@@ -40,6 +40,7 @@ class _PythonOnly:
     def _leave(*args):
         return None
     encode_keys = build_lut = attend_decode = decode_step = decode_step_split = decode_step_gqa = score_prefill = _leave
+    pages_write = attend_pages = pages_copy = pages_fork = pages_free = pages_reserve = pages_compact = _leave
 
 
 class _Shape(ctypes.Structure):
@@ -152,6 +153,9 @@ def load_library():
                 ctypes.cast(getattr(lib, "lookat_" + name), vp).value for name in (
                     "encode_keys", "build_lut", "attend_decode", "attend_decode_workspace_bytes", "decode_step", "decode_step_split",
                     "decode_step_split_workspace_bytes", "decode_step_gqa", "decode_step_gqa_workspace_bytes", "score_prefill")))
+            native.bind_pages(*(ctypes.cast(getattr(lib, "lookat_" + name), vp).value for name in (
+                "pages_write", "attend_pages", "attend_pages_workspace_bytes", "pages_copy", "pages_fork", "pages_free", "pages_reserve",
+                "pages_reserve_workspace_bytes", "pages_compact", "pages_compact_workspace_bytes")))
         except (ImportError, AttributeError, TypeError) as e:
             # (not built, or for another torch: the same library calls are made, 2 to 6 us later each)
             warnings.warn(f"the native marshalling is not available ({e}); run `python -m paper_2601_10155_amd.build`", RuntimeWarning)
@@ -725,6 +729,11 @@ def lookat_pages_write(pool: PagePool, codes: torch.Tensor, values: torch.Tensor
                        counts: torch.Tensor | None = None) -> None:
     """The last counts[b] tokens (default N) of every sequence enter its pages: codes [B,H,N,m] uint8 (of lookat_encode_keys), values
     [B,H,N,d_k] fp16|fp32 in rows 0..counts[b]-1, table [B,W] int32, lengths [B] int32 INCLUDING them.  In place."""
+    rc = _native().pages_write(pool, codes, values, table, lengths, counts)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return
     lib = load_library()
     c_pool = _pool(pool)
     if codes.dim() != 4 or values.dim() != 4 or codes.dtype != torch.uint8 or tuple(codes.shape[:3]) != tuple(values.shape[:3]) \
@@ -759,6 +768,13 @@ def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, 
     """lut [B,H*g,m,256] fp32 (of lookat_build_lut; g query heads share a key/value head), table [B,W] int32, lengths [B] int32
     -> out [B,H*g,d_k] fp32; zeros for a sequence without tokens.  max_length: the longest length the caller knows of (0: W * page);
     it sizes the launch only."""
+    rc = _native().attend_pages(lut, pool, table, lengths, scale, max_length, num_splits, workspace, out)
+    if rc is not None:
+        if out is None and rc.__class__ is not int:
+            return rc                # the output, allocated there
+        if rc:
+            _check(rc)
+        return out
     lib = load_library()
     c_pool = _pool(pool)
     B, W, stride, t_ptr = _table(table, "table", pool)
@@ -784,6 +800,11 @@ def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, 
 
 def lookat_pages_copy(pool: PagePool, src: torch.Tensor, dst: torch.Tensor) -> None:
     """Pages src[i] onto pages dst[i] (int32 [n]; the destinations distinct and none of them a source)."""
+    rc = _native().pages_copy(pool, src, dst)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return
     lib = load_library()
     c_pool = _pool(pool)
     n = src.shape[0] if src.dim() else 0
@@ -801,6 +822,11 @@ def lookat_pages_fork(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor
                       dst: torch.Tensor) -> None:
     """The empty sequences dst[i] begin as src[i]: rows and lengths copied, pages shared and counted once more.
     table [S,W], lengths [S], refs [P], src, dst [n], all int32.  In place."""
+    rc = _native().pages_fork(pool, table, lengths, refs, src, dst)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return
     lib = load_library()
     c_pool = _pool(pool)
     books = _books(pool, table, lengths, refs)
@@ -812,6 +838,11 @@ def lookat_pages_fork(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor
 
 def lookat_pages_free(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, slots: torch.Tensor) -> None:
     """Gives up the sequences `slots` (int32 [n]): their pages are counted once less, their rows become -1, their lengths 0.  In place."""
+    rc = _native().pages_free(pool, table, lengths, refs, slots)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return
     lib = load_library()
     c_pool = _pool(pool)
     books = _books(pool, table, lengths, refs)
@@ -824,6 +855,13 @@ def lookat_pages_reserve(pool: PagePool, table: torch.Tensor, lengths: torch.Ten
                          missing: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Room for the sequences to grow to new_lengths [S] int32 (not above lengths: as it is): free pages in ascending order, shared last
     pages copied, lengths set.  Returns `missing` [1] int32: 0, or how many pages are lacking and nothing was changed."""
+    rc = _native().pages_reserve(pool, table, lengths, refs, new_lengths, missing, workspace)
+    if rc is not None:
+        if missing is None and rc.__class__ is not int:
+            return rc                # allocated there
+        if rc:
+            _check(rc)
+        return missing
     lib = load_library()
     c_pool = _pool(pool)
     books = _books(pool, table, lengths, refs)
@@ -842,6 +880,12 @@ def lookat_pages_compact(pool: PagePool, table: torch.Tensor, lengths: torch.Ten
                          workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """The pages in use move to the lowest ids.  Returns the new table [S,W], the new refs [P] and live [1], the number of pages in use
     (int32); the old table and refs are not changed."""
+    if table_out is None and refs_out is None and live is None:
+        rc = _native().pages_compact(pool, table, lengths, refs, workspace)
+        if rc.__class__ is tuple:
+            return rc
+        if rc:
+            _check(rc)
     lib = load_library()
     c_pool = _pool(pool)
     books = _books(pool, table, lengths, refs)

@@ -68,7 +68,7 @@ def build(verbose: bool = True, force: bool = True) -> str:
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    deps = [os.path.join(CSRC, "marshal.cpp"), os.path.join(ROOT, "include", "lookat.h")]
+    deps = [os.path.join(CSRC, "marshal.cpp")] + [os.path.join(ROOT, "include", h) for h in ("lookat.h", "lookat_pages.h")]
     if force or not (os.path.exists(MARSHAL) and all(os.path.getmtime(MARSHAL) >= os.path.getmtime(d) for d in deps)):
         cmd = marshal_command()
         if verbose:

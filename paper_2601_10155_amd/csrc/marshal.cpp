@@ -9,11 +9,12 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
 
-#include "lookat.h"
+#include "lookat_pages.h"
 
 namespace {
 
@@ -30,6 +31,20 @@ struct Entries {
     decltype(&lookat_score_prefill) score_prefill;
 };
 Entries entry = {};
+// the paged cache's, in the order in which bind_pages() takes their addresses
+struct PageEntries {
+    decltype(&lookat_pages_write) write;
+    decltype(&lookat_attend_pages) attend;
+    decltype(&lookat_attend_pages_workspace_bytes) attend_workspace_bytes;
+    decltype(&lookat_pages_copy) copy;
+    decltype(&lookat_pages_fork) fork;
+    decltype(&lookat_pages_free) free;
+    decltype(&lookat_pages_reserve) reserve;
+    decltype(&lookat_pages_reserve_workspace_bytes) reserve_workspace_bytes;
+    decltype(&lookat_pages_compact) compact;
+    decltype(&lookat_pages_compact_workspace_bytes) compact_workspace_bytes;
+};
+PageEntries pages = {};
 PyObject *stream_of_device = nullptr;   // torch's "current raw stream of device i"
 
 // A tensor whose memory can be handed to the library as it is (no subclass, no wrapper of a transform), or nullptr.
@@ -353,12 +368,247 @@ PyObject *prefill(PyObject *const *args, Py_ssize_t n)
     return status(rc);
 }
 
+// ---- the paged cache -----------------------------------------------------------------------------------------------
+// (codes, values, exponents), dense, on the current device (another one is left to the Python function, which makes it current)
+struct Pool {
+    lookat_page_pool c;
+    const at::Tensor *codes;
+};
+bool pool_of(PyObject *o, Pool &p)
+{
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3)
+        return false;
+    const at::Tensor *codes = dense(PyTuple_GET_ITEM(o, 0), at::kByte), *values = plain(PyTuple_GET_ITEM(o, 1));
+    const at::Tensor *exponents = dense(PyTuple_GET_ITEM(o, 2), at::kChar);
+    if (!codes || !values || !exponents || !values->is_contiguous() || codes->dim() != 4 || values->dim() != 5 || exponents->dim() != 2)
+        return false;
+    const bool i8 = values->scalar_type() == at::kChar;
+    if (!i8 && values->scalar_type() != at::kFloat8_e4m3fn)
+        return false;
+    const int64_t P = codes->size(0), H = codes->size(1), page = codes->size(2), m = codes->size(3), d_k = values->size(3);
+    if (values->size(0) != P || values->size(1) != H || values->size(2) * 8 != page || values->size(4) != 8 || exponents->size(0) != P ||
+        exponents->size(1) != H || std::max({P, H, page, m, d_k}) > 0x7fffffff || values->device() != codes->device() ||
+        exponents->device() != codes->device() || c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != codes->device())
+        return false;
+    p.c = lookat_page_pool{(int32_t)P, (int32_t)H, (int32_t)d_k, (int32_t)m, (int32_t)page, i8 ? LOOKAT_VALUES_I8 : LOOKAT_VALUES_E4M3,
+                           static_cast<uint8_t *>(codes->data_ptr()), values->data_ptr(), static_cast<int8_t *>(exponents->data_ptr())};
+    p.codes = codes;
+    return true;
+}
+bool beside(const Pool &p, const at::Tensor &t) { return t.device() == p.codes->device(); }
+
+// A dense int32 array of n numbers (n < 0: of any positive number of them), or nullptr.
+int32_t *ints(PyObject *o, const Pool &p, int64_t n)
+{
+    const at::Tensor *t = dense(o, at::kInt);
+    return t && t->dim() == 1 && (n < 0 || t->size(0) == n) && t->size(0) <= 0x7fffffff && beside(p, *t) ? static_cast<int32_t *>(t->data_ptr())
+                                                                                                        : nullptr;
+}
+struct Table {
+    int32_t rows, W;
+    int64_t stride;
+    int32_t *ptr;
+};
+bool table_of(PyObject *o, const Pool &p, Table &x)
+{
+    const at::Tensor *t = plain(o, at::kInt);
+    if (!t || t->dim() != 2 || (t->size(1) > 1 && t->stride(1) != 1) || std::max(t->size(0), t->size(1)) > 0x7fffffff || !beside(p, *t))
+        return false;
+    x = Table{(int32_t)t->size(0), (int32_t)t->size(1), t->size(0) > 1 ? t->stride(0) : t->size(1), static_cast<int32_t *>(t->data_ptr())};
+    return true;
+}
+// A workspace of `need` bytes: the given one, or one allocated here.
+bool scratch_of(PyObject *o, size_t need, const Pool &p, at::Tensor &own, void *&ptr, size_t &bytes)
+{
+    if (o != Py_None) {
+        const at::Tensor *w = plain(o);
+        if (!w || !beside(p, *w))
+            return false;
+        ptr = w->data_ptr();
+        bytes = (size_t)w->numel() * w->element_size();
+        return bytes >= need;
+    }
+    ptr = nullptr;
+    bytes = need;
+    if (need) {
+        own = at::empty({(int64_t)need}, p.codes->options());
+        ptr = own.data_ptr();
+    }
+    return true;
+}
+
+// pool, codes, values, table, lengths, counts | None
+PyObject *pages_write(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    Table t;
+    if (n != 6 || !pool_of(args[0], p) || !table_of(args[3], p, t))
+        GIVE_UP;
+    const at::Tensor *codes = plain(args[1], at::kByte), *values = plain(args[2]);
+    if (!codes || !values || codes->dim() != 4 || values->dim() != 4 || !beside(p, *codes) || !beside(p, *values))
+        GIVE_UP;
+    const bool f16 = values->scalar_type() == at::kHalf;
+    const int64_t B = codes->size(0), H = codes->size(1), N = codes->size(2);
+    int64_t cs, vs;
+    int32_t *lengths = ints(args[4], p, t.rows), *counts = args[5] == Py_None ? nullptr : ints(args[5], p, t.rows);
+    void *stream;
+    if ((!f16 && values->scalar_type() != at::kFloat) || B != t.rows || H != p.c.H || codes->size(3) != p.c.m || values->size(0) != B ||
+        values->size(1) != H || values->size(2) != N || values->size(3) != p.c.d_k || !lengths || (args[5] != Py_None && !counts) ||
+        !bh_stride(*codes, cs) || !bh_stride(*values, vs) || !current_stream(*codes, stream))
+        GIVE_UP;
+    CALL(rc, pages.write(&p.c, (int32_t)B, N, static_cast<const uint8_t *>(codes->data_ptr()), cs, values->data_ptr(), f16 ? LOOKAT_F16 : LOOKAT_F32, vs,
+                         t.ptr, t.W, t.stride, lengths, counts, stream));
+    return status(rc);
+}
+
+// lut, pool, table, lengths, scale, max_length, num_splits, workspace | None, out | None
+PyObject *attend_pages(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    Table t;
+    float scale;
+    int64_t longest, splits;
+    if (n != 9 || !pool_of(args[1], p) || !table_of(args[2], p, t) || !number(args[4], scale) || !integer(args[5], 0, INT64_MAX, longest) ||
+        !integer(args[6], 0, 0x7fffffff, splits))
+        GIVE_UP;
+    const at::Tensor *lut = dense(args[0], at::kFloat), *out = args[8] == Py_None ? nullptr : dense(args[8], at::kFloat);
+    const int32_t *lengths = ints(args[3], p, t.rows);
+    if (!lut || lut->dim() != 4 || lut->size(0) != t.rows || lut->size(1) % p.c.H || lut->size(1) > 0x7fffffff || lut->size(2) != p.c.m ||
+        lut->size(3) != 256 || !beside(p, *lut) || !lengths || (args[8] != Py_None && (!out || out->numel() != t.rows * lut->size(1) * p.c.d_k || !beside(p, *out))))
+        GIVE_UP;
+    const int32_t group = (int32_t)(lut->size(1) / p.c.H);
+    at::Tensor own, made;
+    void *ws, *stream;
+    size_t bytes;
+    if (!scratch_of(args[7], pages.attend_workspace_bytes(&p.c, t.rows, group, t.W, longest, (int32_t)splits), p, own, ws, bytes) ||
+        !current_stream(*lut, stream))
+        GIVE_UP;
+    if (!out)
+        made = at::empty({t.rows, lut->size(1), p.c.d_k}, lut->options());
+    float *op = static_cast<float *>((out ? *out : made).data_ptr());
+    CALL(rc, pages.attend(&p.c, t.rows, group, static_cast<const float *>(lut->data_ptr()), t.ptr, t.W, t.stride, lengths, longest, scale,
+                          (int32_t)splits, ws, bytes, op, stream));
+    return rc == LOOKAT_OK && made.defined() ? THPVariable_Wrap(std::move(made)) : status(rc);
+}
+
+// pool, src, dst
+PyObject *pages_copy(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    if (n != 3 || !pool_of(args[0], p))
+        GIVE_UP;
+    const int32_t *src = ints(args[1], p, -1);
+    const int64_t count = src ? THPVariable_Unpack(args[1]).size(0) : 0;
+    const int32_t *dst = ints(args[2], p, count);
+    void *stream;
+    if (!src || !dst || !current_stream(*p.codes, stream))
+        GIVE_UP;
+    CALL(rc, pages.copy(&p.c, (int32_t)count, src, dst, stream));
+    return status(rc);
+}
+
+struct Books {
+    Pool p;
+    Table t;
+    int32_t *lengths, *refs;
+};
+// pool, table, lengths, refs
+bool books_of(PyObject *const *args, Books &b)
+{
+    return pool_of(args[0], b.p) && table_of(args[1], b.p, b.t) && (b.lengths = ints(args[2], b.p, b.t.rows)) &&
+           (b.refs = ints(args[3], b.p, b.p.c.pages));
+}
+
+// pool, table, lengths, refs, src, dst
+PyObject *pages_fork(PyObject *const *args, Py_ssize_t n)
+{
+    Books b;
+    if (n != 6 || !books_of(args, b))
+        GIVE_UP;
+    const int32_t *src = ints(args[4], b.p, -1);
+    const int64_t count = src ? THPVariable_Unpack(args[4]).size(0) : 0;
+    const int32_t *dst = ints(args[5], b.p, count);
+    void *stream;
+    if (!src || !dst || !current_stream(*b.p.codes, stream))
+        GIVE_UP;
+    CALL(rc, pages.fork(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, (int32_t)count, src, dst, stream));
+    return status(rc);
+}
+
+// pool, table, lengths, refs, slots
+PyObject *pages_free(PyObject *const *args, Py_ssize_t n)
+{
+    Books b;
+    if (n != 5 || !books_of(args, b))
+        GIVE_UP;
+    const int32_t *slots = ints(args[4], b.p, -1);
+    void *stream;
+    if (!slots || !current_stream(*b.p.codes, stream))
+        GIVE_UP;
+    const int32_t count = (int32_t)THPVariable_Unpack(args[4]).size(0);
+    CALL(rc, pages.free(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, count, slots, stream));
+    return status(rc);
+}
+
+// pool, table, lengths, refs, new_lengths, missing | None, workspace | None
+PyObject *pages_reserve(PyObject *const *args, Py_ssize_t n)
+{
+    Books b;
+    if (n != 7 || !books_of(args, b))
+        GIVE_UP;
+    const int32_t *wanted = ints(args[4], b.p, b.t.rows);
+    int32_t *missing = args[5] == Py_None ? nullptr : ints(args[5], b.p, 1);
+    at::Tensor own, made;
+    void *ws, *stream;
+    size_t bytes;
+    if (!wanted || (args[5] != Py_None && !missing) ||
+        !scratch_of(args[6], pages.reserve_workspace_bytes(&b.p.c, b.t.rows), b.p, own, ws, bytes) || !current_stream(*b.p.codes, stream))
+        GIVE_UP;
+    if (!missing) {
+        made = at::empty({1}, b.p.codes->options().dtype(at::kInt));
+        missing = static_cast<int32_t *>(made.data_ptr());
+    }
+    CALL(rc, pages.reserve(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, wanted, missing, ws, bytes, stream));
+    return rc == LOOKAT_OK && made.defined() ? THPVariable_Wrap(std::move(made)) : status(rc);
+}
+
+// pool, table, lengths, refs, workspace | None  ->  (table, refs, live), all made here; given outputs are left to the Python function
+PyObject *pages_compact(PyObject *const *args, Py_ssize_t n)
+{
+    Books b;
+    at::Tensor own;
+    void *ws, *stream;
+    size_t bytes;
+    if (n != 5 || !books_of(args, b) || !scratch_of(args[4], pages.compact_workspace_bytes(&b.p.c), b.p, own, ws, bytes) ||
+        !current_stream(*b.p.codes, stream))
+        GIVE_UP;
+    const auto options = b.p.codes->options().dtype(at::kInt);
+    at::Tensor table = at::empty({b.t.rows, b.t.W}, options), refs = at::empty({b.p.c.pages}, options), live = at::empty({1}, options);
+    CALL(rc, pages.compact(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, static_cast<int32_t *>(table.data_ptr()), b.t.W,
+                           static_cast<int32_t *>(refs.data_ptr()), static_cast<int32_t *>(live.data_ptr()), ws, bytes, stream));
+    if (rc != LOOKAT_OK)
+        return status(rc);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(table)), THPVariable_Wrap(std::move(refs)), THPVariable_Wrap(std::move(live)));
+}
+
 // No C++ exception crosses into the interpreter: whatever torch throws while a tensor is looked at, the Python function
 // will meet as well, and raise.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (!entry.score_prefill)
+        GIVE_UP;
+    try {
+        return F(args, n);
+    } catch (...) {
+        GIVE_UP;
+    }
+}
+// The same for the paged cache's calls.
+template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
+PyObject *guarded_pages(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!entry.score_prefill || !pages.compact_workspace_bytes)
         GIVE_UP;
     try {
         return F(args, n);
@@ -393,6 +643,30 @@ PyObject *bind(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// bind_pages(addresses of the entry points in the order of PageEntries)
+PyObject *bind_pages(PyObject *, PyObject *args)
+{
+    unsigned long long a[10];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKK", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7, a + 8, a + 9))
+        return nullptr;
+    pages.write = reinterpret_cast<decltype(pages.write)>(a[0]);
+    pages.attend = reinterpret_cast<decltype(pages.attend)>(a[1]);
+    pages.attend_workspace_bytes = reinterpret_cast<decltype(pages.attend_workspace_bytes)>(a[2]);
+    pages.copy = reinterpret_cast<decltype(pages.copy)>(a[3]);
+    pages.fork = reinterpret_cast<decltype(pages.fork)>(a[4]);
+    pages.free = reinterpret_cast<decltype(pages.free)>(a[5]);
+    pages.reserve = reinterpret_cast<decltype(pages.reserve)>(a[6]);
+    pages.reserve_workspace_bytes = reinterpret_cast<decltype(pages.reserve_workspace_bytes)>(a[7]);
+    pages.compact = reinterpret_cast<decltype(pages.compact)>(a[8]);
+    pages.compact_workspace_bytes = reinterpret_cast<decltype(pages.compact_workspace_bytes)>(a[9]);
+    Py_RETURN_NONE;
+}
+
+template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
+PyMethodDef page_method(const char *name)
+{
+    return PyMethodDef{name, (PyCFunction)(void (*)(void))guarded_pages<F>, METH_FASTCALL, nullptr};
+}
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyMethodDef method(const char *name)
 {
@@ -400,7 +674,10 @@ PyMethodDef method(const char *name)
 }
 PyMethodDef methods[] = {method<step0>("decode_step"),   method<step1>("decode_step_split"), method<step2>("decode_step_gqa"),
                          method<attend>("attend_decode"), method<encode>("encode_keys"),      method<lut>("build_lut"),
-                         method<prefill>("score_prefill"), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         method<prefill>("score_prefill"), page_method<pages_write>("pages_write"), page_method<attend_pages>("attend_pages"),
+                         page_method<pages_copy>("pages_copy"), page_method<pages_fork>("pages_fork"), page_method<pages_free>("pages_free"),
+                         page_method<pages_reserve>("pages_reserve"), page_method<pages_compact>("pages_compact"),
+                         {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -540,3 +540,96 @@ def test_a_captured_decode_step(lk):
             torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(captured.state(), eager.state())), f"replay {n}"
     assert int(captured.lengths[0]) == 40 and int(captured.missing) == 0
+
+
+# ---- the binding -------------------------------------------------------------------------------------------------
+class Watch:
+    """Stands in for the native marshalling: passes calls on and notes which were taken, or takes none."""
+
+    def __init__(self, native):
+        self.native, self.taken = native, {}
+
+    def __getattr__(self, name):
+        def f(*a):
+            rc = getattr(self.native, name)(*a) if self.native else None
+            self.taken[name] = rc is not None
+            return rc
+        return f
+
+
+def test_native_and_python_marshalling_agree(lk, monkeypatch):
+    """A turn of every call through either: the same state, and the native one takes the calls that need no work."""
+    from paper_2601_10155_amd import binding
+    native = binding._marshal
+    states = []
+    for watch in (Watch(native), Watch(None)):
+        monkeypatch.setattr(binding, "_marshal", watch)
+        rng = np.random.default_rng(40)
+        c = random_cache(rng, 40, 3, 64, 4, 16, "float8")
+        pool = on_gpu(lk, c)
+        lengths = [100, 17, 64, 0, 0]
+        wide = torch.full((5, 11), -1, dtype=torch.int32, device="cuda")
+        wide[:, 2:10] = dev(random_table(rng, lengths, 16, 8, 40))
+        table, n = wide[:, 2:10], i32(*lengths)
+        refs = torch.zeros(40, dtype=torch.int32, device="cuda")
+        refs[table[table >= 0].long()] = 1
+        lut = dev(rng.standard_normal((5, 6, 4, 256)).astype(np.float32))
+        out = torch.zeros((5, 6, 64), device="cuda")
+        lk.lookat_pages_fork(pool, table, n, refs, i32(0, 1), i32(3, 4))
+        missing = lk.lookat_pages_reserve(pool, table, n, refs, n + 9)
+        given = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+        ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+        assert lk.lookat_pages_reserve(pool, table, n, refs, n.clone(), given, ws) is given
+        codes = dev(rng.integers(0, 256, (5, 3, 12, 4), dtype=np.uint8))[:, :, 2:11]
+        for dtype in (np.float16, np.float32):
+            values = dev(rng.standard_normal((5, 3, 9, 64)).astype(dtype))
+            lk.lookat_pages_write(pool, codes, values, table, n, i32(9, 3, 0, 1, 9))
+        lk.lookat_pages_write(pool, codes, values, table, n)
+        made = lk.lookat_attend_pages(lut, pool, table, n, 0.125, 200)
+        assert lk.lookat_attend_pages(lut, pool, table, n, 0.125, num_splits=2, out=out) is out
+        free = torch.nonzero(refs == 0)[:, 0].to(torch.int32)
+        lk.lookat_pages_copy(pool, table[0, :2].contiguous(), free[:2].contiguous())
+        lk.lookat_pages_free(pool, table, n, refs, i32(1, 2))
+        compacted = lk.lookat_pages_compact(pool, table, n, refs)
+        outs = torch.empty((5, 8), dtype=torch.int32, device="cuda"), torch.empty_like(refs), torch.empty_like(given)
+        again = lk.lookat_pages_compact(pool, table, n, refs, *outs)
+        assert all(x is y for x, y in zip(again, outs)) and all(torch.equal(x, y) for x, y in zip(again, compacted))
+        torch.cuda.synchronize()
+        states.append([wide, n, refs, missing, given, made, out, *compacted, pool.codes, pool.values.view(torch.uint8), pool.exponents])
+        if watch.native:
+            assert watch.taken == {name: True for name in ("pages_fork", "pages_reserve", "pages_write", "attend_pages", "pages_copy", "pages_free", "pages_compact")}
+    assert all(torch.equal(x, y) for x, y in zip(*states))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_what_the_binding_refuses(lk, monkeypatch, native):
+    from paper_2601_10155_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", Watch(None))
+    pool = lk.page_pool(10, 2, 64, 4, 16)
+    table, n, refs = torch.full((3, 4), -1, dtype=torch.int32, device="cuda"), i32(0, 0, 0), i32(*[0] * 10)
+    lut = torch.zeros((3, 2, 4, 256), device="cuda")
+    codes, values = torch.zeros((3, 2, 1, 4), dtype=torch.uint8, device="cuda"), torch.zeros((3, 2, 1, 64), device="cuda")
+    for bad in (lambda: lk.lookat_attend_pages(lut, pool, table.long(), n, 1.0), lambda: lk.lookat_attend_pages(lut, pool, table.t(), n, 1.0),
+                lambda: lk.lookat_attend_pages(lut, pool, table, n[:2], 1.0), lambda: lk.lookat_attend_pages(lut.half(), pool, table, n, 1.0),
+                lambda: lk.lookat_attend_pages(lut[:, :, :3], pool, table, n, 1.0), lambda: lk.lookat_attend_pages(lut[:2], pool, table, n, 1.0),
+                lambda: lk.lookat_attend_pages(lut[:, :1].contiguous(), pool, table, n, 1.0), lambda: lk.lookat_attend_pages(lut, pool, table.cpu(), n, 1.0),
+                lambda: lk.lookat_attend_pages(lut, pool, table, n, 1.0, out=lut), lambda: lk.lookat_attend_pages(lut.cpu(), pool, table, n, 1.0),
+                lambda: lk.lookat_pages_write(pool, codes, values[:2], table, n), lambda: lk.lookat_pages_write(pool, codes, values[..., :32], table, n),
+                lambda: lk.lookat_pages_write(pool, codes, values, table[:2], n), lambda: lk.lookat_pages_write(pool, codes.int(), values, table, n),
+                lambda: lk.lookat_pages_write(pool, codes, values.permute(0, 1, 3, 2).contiguous().permute(0, 1, 3, 2).expand(3, 2, 2, 64), table, n),
+                lambda: lk.lookat_pages_write(pool, codes, values, table, n, n.long()), lambda: lk.lookat_pages_copy(pool, n, n[:1]),
+                lambda: lk.lookat_pages_copy(pool, n.float(), n), lambda: lk.lookat_pages_fork(pool, table, n, refs[:9], n, n),
+                lambda: lk.lookat_pages_free(pool, table, n, refs, n.view(1, 3)), lambda: lk.lookat_pages_reserve(pool, table, n, refs, n[:1]),
+                lambda: lk.lookat_pages_compact(pool, table, n, refs, table_out=table[:2].clone())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        lk.lookat_pages_write(pool, codes, values.double(), table, n)
+    for bad in (lambda: lk.lookat_pages_reserve(pool, table, n, refs, n), lambda: lk.lookat_pages_compact(pool, table, n, refs, table_out=table),
+                lambda: lk.lookat_attend_pages(lut, pool, table, n, 1.0, max_length=-1), lambda: lk.lookat_attend_pages(lut, pool, table, n, 1.0, num_splits=70000),
+                lambda: lk.lookat_pages_copy(lk.page_pool(4, 1, 64, 32, 16), n, n)):
+        with pytest.raises(lk.LookatError):
+            bad()
+    torch.cuda.synchronize()
+    assert torch.all(table == -1) and torch.all(n == 0)
