@@ -82,7 +82,8 @@ int lookat_pages_write(const lookat_page_pool *pool, int32_t B, int64_t N,
  *   max_length    the longest length the host knows of, or 0 for W * page: it sizes the launch alone; longer sequences are
  *                 right too
  *   group         1, 2, 4 or 8, otherwise LOOKAT_ERR_UNSUPPORTED
- *   num_splits    ranges per (b, key/value head), 0 = the library's choice (from the sizes given here; lengths stay on the device)
+ *   num_splits    0: the sequences are cut into ranges by their lengths, on the device, where they are long enough to gain from it; >= 1: that
+ *                 many equal ranges of max_length per (b, key/value head).  The result does not depend on it beyond fp32 rounding
  *   workspace     lookat_attend_pages_workspace_bytes(pool, B, group, W, max_length, num_splits) bytes, 16-byte aligned (NULL when 0);
  *                 calls in flight at once must not share one
  *   out           [B, H*group, d_k] fp32, 16-byte aligned
@@ -98,9 +99,6 @@ int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int32_t group,
                         void *workspace, size_t workspace_bytes,
                         float *out,
                         void *stream);
-
-/* The ranges per (b, key/value head) lookat_attend_pages takes when num_splits is 0 (host only); 0 if the arguments are invalid. */
-int32_t lookat_attend_pages_auto_splits(const lookat_page_pool *pool, int32_t B, int32_t group, int32_t W, int64_t max_length);
 
 /*
  * Copies pages src[i] onto pages dst[i] (codes, values, exponents), i < n.  Pairs with an id outside [0, pages) or with

@@ -114,8 +114,6 @@ def load_library():
         lib.lookat_pages_write.restype = ctypes.c_int
         lib.lookat_attend_pages_workspace_bytes.argtypes = [pp, i32, i32, i32, i64, i32]
         lib.lookat_attend_pages_workspace_bytes.restype = sz
-        lib.lookat_attend_pages_auto_splits.argtypes = [pp, i32, i32, i32, i64]
-        lib.lookat_attend_pages_auto_splits.restype = i32
         lib.lookat_attend_pages.argtypes = [pp, i32, i32, vp, vp, i32, i64, vp, i64, f32, i32, vp, sz, vp, vp]
         lib.lookat_attend_pages.restype = ctypes.c_int
         lib.lookat_pages_copy.argtypes = [pp, i32, vp, vp, vp]
@@ -757,10 +755,6 @@ def lookat_pages_write(pool: PagePool, codes: torch.Tensor, values: torch.Tensor
 
 def attend_pages_workspace_bytes(pool: PagePool, B: int, group: int, W: int, max_length: int = 0, num_splits: int = 0) -> int:
     return int(load_library().lookat_attend_pages_workspace_bytes(ctypes.byref(_pool(pool)), B, group, W, max_length, num_splits))
-
-
-def attend_pages_auto_splits(pool: PagePool, B: int, group: int, W: int, max_length: int = 0) -> int:
-    return int(load_library().lookat_attend_pages_auto_splits(ctypes.byref(_pool(pool)), B, group, W, max_length))
 
 
 def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, scale: float, max_length: int = 0,

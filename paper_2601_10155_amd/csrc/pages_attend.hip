@@ -23,19 +23,147 @@ namespace lookat {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 
 struct AttendArgs {
     const float *lut;
     const int32_t *table, *lengths;
     float *part, *out;
+    int2 *plan;                           // ranges by length: (first range, ranges) of every sequence, for the merge
     int64_t table_stride;
-    int32_t W, units, splits, chunk;      // units = sequences * key/value heads; chunk tokens per range (a multiple of 64)
+    int32_t W, B, units;                  // units = sequences * key/value heads
+    int32_t splits, chunk;                // equal ranges: their number and their tokens (a multiple of 64)
+    int32_t per_head;                     // ranges by length: how many there should be for each key/value head; 0: equal ranges
+    int32_t least;                        // ... of at least this many tokens
     float scale_log2e;
 };
 
 constexpr float kRefLag = 8.f;            // the reference moves when a logit exceeds it by more (log2 units)
 constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, below 2^15: fp16's range, its subnormals far below
-constexpr int kWeightRow = 72;            // halves between the staged weights of two columns: 64 tokens, 16 bytes of padding
+constexpr int kAttendThreads = 512;        // eight wavefronts; 128 registers each: two workgroups to a compute unit
+constexpr int kMostPlanned = 1024;        // sequences whose ranges are cut by their lengths
+
+// Ranges by length.  Sequences of unequal length cut into equally many ranges leave most of the chip waiting for the longest one, and the host
+// does not know the lengths.  So every workgroup looks at all of them: with c tokens per range, c such that all sequences
+// together make about `per_head` ranges for each head, sequence b gets ceil(length_b / c) ranges of nearly equal size, and the ranges of all
+// (sequence, head) pairs are dealt to the workgroups in order.  At most per_head + 1 + B per head: a workgroup that has none leaves.
+struct Range {
+    int b, h, split, splits, k0, k1, index;
+};
+__device__ __forceinline__ int range_tokens(float total, int per_head, int least)
+{
+    // (rounded the same in every workgroup; 2^-20 of a range more or less is what the extra range per head is for)
+    const float want = total / (float)per_head;
+    return want < (float)least ? least : want > 1073741824.f ? 1 << 30 : ((int)want + kTile) / kTile * kTile;
+}
+// a / b rounded down, for a quotient below 2^20
+__device__ __forceinline__ int quotient(int a, int b)
+{
+    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));      // off by one at most
+    q -= q * b > a;
+    q += a - q * b >= b;
+    return q;
+}
+__device__ __forceinline__ int ranges_of(int length, int c) { return length > c ? quotient(length - 1, c) + 1 : 1; }
+__device__ __forceinline__ void set_range(Range &r, int b, int place, int splits, int length, int c, int index)
+{
+    r.b = b;
+    r.splits = splits;
+    r.h = quotient(place, splits);
+    r.split = place - r.h * splits;
+    r.index = index;
+    // no less than length / splits (2^-20 more than its product with the reciprocal), and at most c: no range is empty
+    int size = ((int)((float)length * __builtin_amdgcn_rcpf((float)splits) * 1.000001f) + kTile) / kTile * kTile;
+    size = size < c ? size : c;
+    r.k0 = r.split * size;
+    r.k1 = r.split == splits - 1 ? length : r.k0 + size;
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int upto_lane(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8: within 16 lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // row_bcast:31 into rows 2 and 3
+}
+// (all threads of the workgroup; s: 36 ints of LDS; B <= kMostPlanned; false: no range)
+__device__ __forceinline__ bool range_by_length(const AttendArgs &a, int H, int page_log2, int *s, Range &r)
+{
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, waves = blockDim.x / kWave;
+    const int die = blockIdx.x % kXcds, nth = blockIdx.x / kXcds;
+    if (a.B <= kWave) {
+        // a lane per sequence, every wavefront for itself
+        const int length = lane < a.B ? clamp_length(a.lengths[lane], a.W, page_log2) : 0;
+        const int c = range_tokens(wave_sum((float)length), a.per_head, a.least);
+        const int n = lane < a.B ? ranges_of(length, c) : 0;
+        const int upto = upto_lane(n);
+        const int ranges = __builtin_amdgcn_readlane(upto, kWave - 1) * H, per_die = (ranges + kXcds - 1) / kXcds, index = die * per_die + nth;
+        if (nth >= per_die || index >= ranges)
+            return false;
+        if (index == 0 && wave == 0 && lane < a.B)
+            a.plan[lane] = make_int2((upto - n) * H, n);
+        const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(index < upto * H));
+        set_range(r, at, index - __builtin_amdgcn_readlane(upto - n, at) * H, __builtin_amdgcn_readlane(n, at), __builtin_amdgcn_readlane(length, at), c, index);
+        return true;
+    }
+    const int each = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;       // consecutive sequences of a thread: 1 to 16
+    const int b0 = tid * each;
+    float total = 0.f;
+    for (int j = 0; j < each; ++j)
+        if (b0 + j < a.B)
+            total += (float)clamp_length(a.lengths[b0 + j], a.W, page_log2);
+    total = wave_sum(total);
+    float *f = reinterpret_cast<float *>(s);
+    if (lane == 0)
+        f[wave] = total;
+    __syncthreads();
+    total = 0.f;
+    for (int w = 0; w < waves; ++w)
+        total += f[w];
+    const int c = range_tokens(total, a.per_head, a.least);
+    int n = 0;
+    for (int j = 0; j < each; ++j)
+        if (b0 + j < a.B) {
+            const int length = clamp_length(a.lengths[b0 + j], a.W, page_log2);
+            n += ranges_of(length, c);
+        }
+    int before = upto_lane(n);
+    if (lane == kWave - 1)
+        s[16 + wave] = before;
+    before -= n;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < waves; ++w) {
+        before += w < wave ? s[16 + w] : 0;
+        all += s[16 + w];
+    }
+    // consecutive ranges on one die: those of a (sequence, head) share its tables
+    const int ranges = all * H, per_die = (ranges + kXcds - 1) / kXcds;
+    const int index = die * per_die + nth;
+    if (nth >= per_die || index >= ranges)
+        return false;
+    for (int j = 0; j < each; ++j)
+        if (b0 + j < a.B) {
+            const int length = clamp_length(a.lengths[b0 + j], a.W, page_log2);
+            const int mine = ranges_of(length, c);
+            if (index == 0)
+                a.plan[b0 + j] = make_int2(before * H, mine);
+            if (index >= before * H && index < (before + mine) * H) {
+                s[32] = b0 + j;
+                s[33] = index - before * H;
+                s[34] = mine;
+                s[35] = length;
+            }
+            before += mine;
+        }
+    __syncthreads();
+    const int at = s[32], place = s[33], mine = s[34], length = s[35];
+    __syncthreads();                                      // (s is free again)
+    set_range(r, at, place, mine, length, c, index);
+    return true;
+}
 
 // Eight stored bytes (two registers) to eight fp16 numbers, exactly.
 template <bool FP8>
@@ -64,32 +192,108 @@ __device__ __forceinline__ v8h widen(uint32_t lo, uint32_t hi)
     return __builtin_bit_cast(v8h, r);
 }
 
-// LDS of a workgroup: tables and staged weights while it streams, the wavefronts' results afterwards.
-__host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k, int waves)
+template <int CTRL>
+__device__ __forceinline__ float lane_of(float x)
 {
-    const size_t stream = (size_t)G * M * kCentroids * 4 + (size_t)waves * 2 * G * kWeightRow * 2;
-    const size_t merge = (size_t)waves * G * (d_k + 2) * 4;
-    return stream > merge ? stream : merge;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_value(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+// Maxima or sums over the wavefront of G values at once, as scalars: every exchange serves two values, so that eight take 28 instructions.
+struct Max {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Sum {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+template <typename Op>
+__device__ __forceinline__ float over_row(float x, Op op)          // 16 lanes
+{
+    x = op(x, lane_of<0xB1>(x));
+    x = op(x, lane_of<0x4E>(x));
+    x = op(x, lane_of<0x141>(x));
+    return op(x, lane_of<0x140>(x));
+}
+// Lanes 0-31: over x's halves, 32-63: over y's.
+template <typename Op>
+__device__ __forceinline__ float over_halves(float x, float y, Op op)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// Rows 0 and 2: over x's rows 0, 1 and 2, 3; rows 1 and 3: over y's.
+template <typename Op>
+__device__ __forceinline__ float over_rows(float x, float y, Op op)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <int G, typename Op>
+__device__ __forceinline__ void over_wave(const float (&y)[G], float (&m)[G], Op op)
+{
+    if constexpr (G == 1) {
+        const float h = over_halves(y[0], y[0], op);
+        m[0] = lane_value(over_row(over_rows(h, h, op), op), 0);
+    } else if constexpr (G == 2) {
+        const float h = over_halves(y[0], y[1], op), a = over_row(over_rows(h, h, op), op);
+        m[0] = lane_value(a, 0);
+        m[1] = lane_value(a, 32);
+    } else if constexpr (G == 4) {
+        const float a = over_row(over_rows(over_halves(y[0], y[2], op), over_halves(y[1], y[3], op), op), op);
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            m[g] = lane_value(a, 16 * g);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float a = over_row(over_rows(over_halves(y[k], y[k + 4], op), over_halves(y[k + 2], y[k + 6], op), op), op);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                m[k + 2 * r] = lane_value(a, 16 * r);
+        }
+    }
+}
+
+// LDS of a workgroup: tables (afterwards the wavefronts' results), then the wavefronts' staged weights (afterwards their references and sums).
+constexpr int kAttendWaves = kAttendThreads / kWave;
+__host__ __device__ constexpr size_t attend_front_bytes(int G, int M, int d_k)
+{
+    const size_t tables = (size_t)G * M * kCentroids * 4, results = (size_t)kAttendWaves * G * (d_k + 2) * 4;
+    return tables > results ? tables : results;
+}
+__host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k)
+{
+    return attend_front_bytes(G, M, d_k) + (size_t)kAttendWaves * 2 * G * kTile * 2;
 }
 
 template <int DK, int M, int G, bool FP8>
-__global__ __launch_bounds__(1024) void attend_pages_kernel(PoolArgs p, AttendArgs a)
+__global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArgs p, AttendArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     constexpr int GP = G < 4 ? G : 4;                     // query heads whose tables are interleaved
     typedef float vg __attribute__((ext_vector_type(GP)));
     constexpr int CB = DK / 32;                           // 16-byte loads per lane and 32 tokens
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, waves = blockDim.x / kWave;
-    // ranges of one (sequence, head) on one die: its tables are fetched into one L2
-    const int unit = (int)(blockIdx.x / kXcds) / a.splits * kXcds + blockIdx.x % kXcds, split = (int)(blockIdx.x / kXcds) % a.splits;
-    if (unit >= a.units)
-        return;
-    const int b = unit / p.H, h = unit - b * p.H;
-    const int length = clamp_length(a.lengths[b], a.W, p.page_log2);
-    const int k0 = split * a.chunk;
-    const int k1 = split == a.splits - 1 || length - k0 < a.chunk ? length : k0 + a.chunk;
-    if (k0 >= k1 && split > 0)
-        return;                                           // (the merge knows the length)
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    Range r;
+    if (a.per_head) {
+        if (!range_by_length(a, p.H, p.page_log2, reinterpret_cast<int *>(lds), r))
+            return;
+    } else {
+        // ranges of one (sequence, head) on one die: its tables are fetched into one L2
+        const int unit = (int)(blockIdx.x / kXcds) / a.splits * kXcds + blockIdx.x % kXcds;
+        if (unit >= a.units)
+            return;
+        r.b = unit / p.H;
+        r.h = unit - r.b * p.H;
+        r.split = (int)(blockIdx.x / kXcds) % a.splits;
+        r.splits = a.splits;
+        r.index = unit * a.splits + r.split;
+        const int length = clamp_length(a.lengths[r.b], a.W, p.page_log2);
+        r.k0 = r.split * a.chunk;
+        r.k1 = r.split == a.splits - 1 || length - r.k0 < a.chunk ? length : r.k0 + a.chunk;
+        if (r.k0 >= r.k1 && r.split > 0)
+            return;                                       // (the merge knows the length)
+    }
+    const int b = r.b, h = r.h, k0 = r.k0, k1 = r.k1, unit = b * p.H + h;
     const int32_t *row = a.table + b * a.table_stride;
     const int page_mask = (1 << p.page_log2) - 1;
     const int col = lane & 15, quad = lane >> 4;
@@ -104,7 +308,6 @@ __global__ __launch_bounds__(1024) void attend_pages_kernel(PoolArgs p, AttendAr
     uint32_t codes[(M + 3) / 4];
     int exponent = 0;
     v4u v[2][CB];
-    uint32_t keep[2][2];                                  // FP8: the bytes of an octet that hold tokens
     auto request = [&](int t, int id) {
         const int key = t + lane;
         const int64_t place = (int64_t)(id < 0 ? 0 : id) * p.H + h;
@@ -130,81 +333,115 @@ __global__ __launch_bounds__(1024) void attend_pages_kernel(PoolArgs p, AttendAr
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 v[kk][cb] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(src + cb * 256));
-            if constexpr (FP8) {
-                // (bytes behind the last token may be NaN)
-                const int n = oid < 0 ? 0 : k1 - t - first;
-                keep[kk][0] = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
-                keep[kk][1] = n >= 8 ? ~0u : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1;
-            }
         }
     };
 
     int t = k0 + wave * kWave;
-    const int step = waves * kWave;
+    const int step = kAttendThreads;
     int id = page_of(t + lane);
     float *tables = reinterpret_cast<float *>(lds);
-    {
-        // tables [query head][i][c] -> [plane of GP heads][i][c][head], scaled
-        const float *src = a.lut + (int64_t)unit * G * M * kCentroids;
-        for (int j = tid; j < M * kCentroids; j += blockDim.x) {
+    // Tables [query head][i][c] -> [plane of GP heads][i][c][head], scaled; a thread takes four entries of GP heads at a time.  The first tile is
+    // requested between the tables' loads and their use.
+    constexpr int quads = G / GP * M * (kCentroids / 4), rounds = (quads + kAttendThreads - 1) / kAttendThreads;
+    constexpr int early = rounds * GP <= 8 ? rounds : 8 / GP;
+    const v4f *lut = reinterpret_cast<const v4f *>(a.lut + (int64_t)unit * G * M * kCentroids);
+    v4f x[early][GP];
+    auto table_load = [&](int round, int n) {
+        const int j = tid + round * kAttendThreads, at = quads % kAttendThreads && j >= quads ? quads - 1 : j;
+        const int plane = at / (M * (kCentroids / 4)), entry = at % (M * (kCentroids / 4));
 #pragma unroll
-            for (int g0 = 0; g0 < G; g0 += GP) {
-                vg x;
+        for (int g = 0; g < GP; ++g)
+            x[n][g] = lut[(plane * GP + g) * (M * (kCentroids / 4)) + entry];
+    };
+    auto table_store = [&](int round, int n) {
+        const int j = tid + round * kAttendThreads;
+        if (quads % kAttendThreads == 0 || j < quads) {
 #pragma unroll
-                for (int g = 0; g < GP; ++g)
-                    x[g] = src[(g0 + g) * (M * kCentroids) + j] * a.scale_log2e;
-                reinterpret_cast<vg *>(tables)[(g0 / GP) * (M * kCentroids) + j] = x;
+            for (int k = 0; k < GP; ++k) {                // GP * 4 floats as GP 16-byte stores, ordered entry, head
+                v4f y;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    y[w] = x[n][(4 * k + w) % GP][(4 * k + w) / GP] * a.scale_log2e;
+                reinterpret_cast<v4f *>(tables)[j * GP + k] = y;
             }
         }
-    }
+    };
+#pragma unroll
+    for (int n = 0; n < early; ++n)
+        table_load(n, n);
+    __builtin_amdgcn_sched_barrier(0);
     if (t < k1)
         request(t, id);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < early; ++n)
+        table_store(n, n);
+#pragma unroll
+    for (int r0 = early; r0 < rounds; r0 += early) {
+#pragma unroll
+        for (int n = 0; n < early; ++n)
+            if (r0 + n < rounds)
+                table_load(r0 + n, n);
+#pragma unroll
+        for (int n = 0; n < early; ++n)
+            if (r0 + n < rounds)
+                table_store(r0 + n, n);
+    }
     int id_next = page_of(t + step + lane);
     __syncthreads();
 
-    _Float16 *weights = reinterpret_cast<_Float16 *>(lds + (size_t)G * M * kCentroids * 4) + (size_t)wave * 2 * G * kWeightRow;
+    // staged weights: a row of 64 tokens per column, 128 bytes; its 16-byte pieces are permuted (xor with the row) so that neither side conflicts
+    constexpr int staged = 2 * G * kTile * 2;
+    char *weights = lds + attend_front_bytes(G, M, DK) + wave * staged;
+    int w_at = (lane >> 3) << 4 | (lane & 7) << 1;
+    auto weight = [&](int row) -> _Float16 & { return *reinterpret_cast<_Float16 *>(weights + row * (kTile * 2) + (w_at ^ ((row & 7) << 4))); };
     v4f acc[2 * CB];
 #pragma unroll
     for (int c = 0; c < 2 * CB; ++c)
         acc[c] = (v4f){0.f, 0.f, 0.f, 0.f};
-    float ref[G], z[G];
+    float lift[G], z[G];                                  // the reference less kRefLift (one value for the wavefront), the sum
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        ref[g] = -1e30f;
+        lift[g] = -1e30f;
         z[g] = 0.f;
     }
 
     while (t < k1) {
-        // logits
+        // logits, above the reference
         float y[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-            y[g] = 0.f;
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
-            const uint32_t c = (codes[i / 4] >> (8 * (i % 4))) & 0xffu;
-#pragma unroll
-            for (int g0 = 0; g0 < G; g0 += GP) {
-                const vg x = reinterpret_cast<const vg *>(tables)[((g0 / GP) * M + i) * kCentroids + c];
-#pragma unroll
-                for (int g = 0; g < GP; ++g)
-                    y[g0 + g] += x[g];
-            }
-        }
-        bool above = false;
         exponent = id < 0 ? 0 : exponent;                 // (a lane without a token has read some page's)
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            y[g] = id < 0 ? -INFINITY : y[g] + (float)exponent;
-            above |= y[g] > ref[g] + kRefLag;
+        for (int g = 0; g < G; ++g)
+            y[g] = (float)exponent;
+        constexpr int planes = G / GP, most_reads = 16 / GP, together = M * planes < most_reads ? M * planes : most_reads;
+#pragma unroll
+        for (int n0 = 0; n0 < M * planes; n0 += together) {
+            vg x[together];
+#pragma unroll
+            for (int n = 0; n < together; ++n) {
+                const int i = (n0 + n) / planes, plane = (n0 + n) % planes;
+                x[n] = reinterpret_cast<const vg *>(tables)[(plane * M + i) * kCentroids + ((codes[i / 4] >> (8 * (i % 4))) & 0xffu)];
+            }
+#pragma unroll
+            for (int n = 0; n < together; ++n)
+#pragma unroll
+                for (int g = 0; g < GP; ++g)
+                    y[(n0 + n) % planes * GP + g] += x[n][g];
         }
-        if (__builtin_amdgcn_ballot_w64(above)) {
-            float fix_n = 1.f;                            // for the column that this lane accumulates
+        float most = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            y[g] = id < 0 ? -INFINITY : y[g];
+            most = fmaxf(most, y[g] - lift[g]);
+        }
+        if (__builtin_amdgcn_ballot_w64(most > kRefLift + kRefLag)) {
+            float fix_n = 1.f, top[G];                    // fix_n: for the column that this lane accumulates
+            over_wave(y, top, Max());
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float to = fmaxf(ref[g], wave_max(y[g]));
-                const float fix = fast_exp2(ref[g] - to);
-                ref[g] = to;
+                const float to = fmaxf(lift[g], top[g] - kRefLift);
+                const float fix = fast_exp2(lift[g] - to);
+                lift[g] = lane_value(to, 0);
                 z[g] *= fix;
                 fix_n = (lane & (G - 1)) == g ? fix : fix_n;
             }
@@ -212,27 +449,42 @@ __global__ __launch_bounds__(1024) void attend_pages_kernel(PoolArgs p, AttendAr
             for (int c = 0; c < 2 * CB; ++c)
                 acc[c] *= fix_n;
         }
+        asm volatile("" : "+v"(w_at));                    // (the rows' places are computed here: kept from tile to tile they take eight registers)
         const float unscale = __uint_as_float((uint32_t)(127 - exponent) << 23);      // 2^-e
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const float w = fast_exp2(y[g] - (ref[g] - kRefLift));
+            const float w = fast_exp2(y[g] - lift[g]);
             z[g] = fmaf(w, unscale, z[g]);
             const _Float16 hi = (_Float16)w;
-            weights[g * kWeightRow + lane] = hi;
-            weights[(G + g) * kWeightRow + lane] = (_Float16)(w - (float)hi);
+            weight(g) = hi;
+            weight(G + g) = (_Float16)(w - (float)hi);
+        }
+        if constexpr (FP8) {
+            // bytes without a token behind them may be NaN: zeros in their place
+            if (__builtin_amdgcn_ballot_w64(id < 0)) {
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const int first = kk * 32 + quad * 8;
+                    const int n = __shfl(id, first) < 0 ? 0 : k1 - t - first;
+                    const uint32_t lo = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+                    const uint32_t hi = n >= 8 ? ~0u : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1;
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        v[kk][cb].x &= lo, v[kk][cb].y &= hi;
+                        v[kk][cb].z &= lo, v[kk][cb].w &= hi;
+                    }
+                }
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            const v8h wt = *reinterpret_cast<const v8h *>(weights + (col & (2 * G - 1)) * kWeightRow + kk * 32 + quad * 8);
+            const int row = col & (2 * G - 1);
+            const v8h wt = *reinterpret_cast<const v8h *>(weights + row * (kTile * 2) + (((kk * 4 + quad) ^ (row & 7)) << 4));
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                v4u x = v[kk][cb];
-                if constexpr (FP8) {
-                    x.x &= keep[kk][0], x.y &= keep[kk][1];
-                    x.z &= keep[kk][0], x.w &= keep[kk][1];
-                }
+                const v4u x = v[kk][cb];
                 acc[2 * cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FP8>(x.x, x.y), wt, acc[2 * cb], 0, 0, 0);
                 acc[2 * cb + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FP8>(x.z, x.w), wt, acc[2 * cb + 1], 0, 0, 0);
             }
@@ -247,107 +499,152 @@ __global__ __launch_bounds__(1024) void attend_pages_kernel(PoolArgs p, AttendAr
         }
     }
 
-    // the wavefronts' results
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-        z[g] = wave_sum(z[g]);
-    __syncthreads();                                      // every wavefront is done with its tables
-    float *red = reinterpret_cast<float *>(lds);
-#pragma unroll
-    for (int c = 0; c < 2 * CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float both = acc[c][r] + __shfl_xor(acc[c][r], G);      // columns n and n + G: the two terms of a weight
-            // row 4 quad + r of the instruction's result is coordinate 2 (4 quad + r) + (c & 1) of the 32 that a load covers
-            if (col < G)
-                red[(wave * G + col) * (DK + 2) + (c / 2) * 32 + 2 * (4 * quad + r) + (c & 1)] = both;
-        }
+    // The wavefronts' results: references and sums first, so that every wavefront brings its own to the common reference before they are added.
+    float sums[G];
+    over_wave(z, sums, Sum());
     if (lane == 0) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            red[(wave * G + g) * (DK + 2) + DK] = ref[g];
-            red[(wave * G + g) * (DK + 2) + DK + 1] = z[g];
-        }
+        for (int g = 0; g < G; ++g)
+            reinterpret_cast<v2f *>(weights)[g] = (v2f){lift[g], sums[g]};
     }
+    __syncthreads();                                      // and every wavefront is done with the tables
+    const int mine = col & (G - 1);
+    v2f stat[kAttendWaves];
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w)
+        stat[w] = *reinterpret_cast<const v2f *>(lds + attend_front_bytes(G, M, DK) + w * staged + mine * 8);
+    float top = stat[0].x, sum = 0.f, own = lift[0];
+#pragma unroll
+    for (int w = 1; w < kAttendWaves; ++w)
+        top = fmaxf(top, stat[w].x);
+#pragma unroll
+    for (int w = 0; w < kAttendWaves; ++w)
+        sum = fmaf(fast_exp2(stat[w].x - top), stat[w].y, sum);
+#pragma unroll
+    for (int g = 1; g < G; ++g)
+        own = mine == g ? lift[g] : own;
+    // one range: results are divided by the sum here; several: the merge does it
+    float f = fast_exp2(own - top);
+    if (r.splits == 1)
+        f = sum > 0.f ? f / sum : 0.f;
+    float *results = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int c = 0; c < 2 * CB; c += 2)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            // columns n and n + G: the two terms of a weight; row 4 quad + k of an instruction's result is coordinate 2 (4 quad + k) of the 32
+            // that a load covers, the next instruction's the coordinate behind it
+            v2f both;
+            both.x = (acc[c][k] + lane_of<0x120 + G>(acc[c][k])) * f;
+            both.y = (acc[c + 1][k] + lane_of<0x120 + G>(acc[c + 1][k])) * f;
+            if (col < G)
+                *reinterpret_cast<v2f *>(results + (wave * G + col) * (DK + 2) + c * 16 + 2 * (4 * quad + k)) = both;
+        }
     __syncthreads();
-    for (int j = tid; j < G * DK; j += blockDim.x) {
-        const int g = j / DK, d = j - g * DK;
-        float top = -1e30f, o = 0.f, sum = 0.f;
-        for (int w = 0; w < waves; ++w)
-            top = fmaxf(top, red[(w * G + g) * (DK + 2) + DK]);
-        for (int w = 0; w < waves; ++w) {
-            const float *x = red + (w * G + g) * (DK + 2);
-            const float f = fast_exp2(x[DK] - top);
-            o = fmaf(f, x[d], o);
-            sum = fmaf(f, x[DK + 1], sum);
-        }
-        if (a.splits == 1) {
-            a.out[((int64_t)unit * G + g) * DK + d] = sum > 0.f ? o / sum : 0.f;
-        } else {
-            float *part = a.part + (((int64_t)unit * G + g) * a.splits + split) * (DK + 2);
-            part[d] = o;
-            if (d == 0) {
-                part[DK] = top;
-                part[DK + 1] = sum;
-            }
-        }
+    float *to = r.splits == 1 ? a.out + (int64_t)unit * G * DK : a.part + (int64_t)r.index * G * (DK + 2);
+    const int row_to = r.splits == 1 ? DK : DK + 2;
+#pragma unroll
+    for (int j = tid; j < G * DK / 2; j += kAttendThreads) {
+        const int g = j / (DK / 2), d = j % (DK / 2) * 2;
+        v2f o = {0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w)
+            o += *reinterpret_cast<const v2f *>(results + (w * G + g) * (DK + 2) + d);
+        *reinterpret_cast<v2f *>(to + g * row_to + d) = o;
     }
+    if (r.splits > 1 && tid < G)                          // (lanes 0 to G - 1 of the first wavefront: mine == tid)
+        *reinterpret_cast<v2f *>(to + tid * row_to + DK) = (v2f){top, sum};
 }
 
-// Merges the ranges of one (sequence, query head) that its length reaches.  Thread per coordinate; the ranges' loads are issued eight at a time.
-__global__ __launch_bounds__(128) void attend_pages_merge_kernel(const float *__restrict__ part, float *__restrict__ out,
-                                                                 const int32_t *__restrict__ lengths, int splits, int chunk, int d_k, int per_sequence,
-                                                                 int W, int page_log2)
+// Merges the ranges of one (sequence, key/value head): a thread per query head and coordinate, the ranges' loads issued eight at a time.
+__global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, int H, int G, int d_k, int page_log2)
 {
     constexpr int GR = 8;
-    const int head = blockIdx.x, d = threadIdx.x;
-    const int length = clamp_length(lengths[head / per_sequence], W, page_log2);
-    int n = (length + chunk - 1) / chunk;
-    n = n < 1 ? 1 : n > splits ? splits : n;
-    const float *x = part + (int64_t)head * splits * (d_k + 2);
-    float top = -1e30f, o = 0.f, z = 0.f;
-    for (int s0 = 0; s0 < n; s0 += GR) {
-        float m_[GR], z_[GR], o_[GR];
-#pragma unroll
-        for (int j = 0; j < GR; ++j) {
-            const float *y = x + (int64_t)(s0 + j < n ? s0 + j : s0) * (d_k + 2);
-            m_[j] = y[d_k];
-            z_[j] = s0 + j < n ? y[d_k + 1] : 0.f;
-            o_[j] = s0 + j < n ? y[d] : 0.f;
-        }
-        float to = top;
-#pragma unroll
-        for (int j = 0; j < GR; ++j)
-            to = fmaxf(to, m_[j]);
-        const float fix = fast_exp2(top - to);
-        o *= fix;
-        z *= fix;
-#pragma unroll
-        for (int j = 0; j < GR; ++j) {
-            const float f = fast_exp2(m_[j] - to);
-            o = fmaf(f, o_[j], o);
-            z = fmaf(f, z_[j], z);
-        }
-        top = to;
+    const int unit = blockIdx.x, b = unit / H, h = unit - b * H;
+    int n;
+    int64_t first;
+    if (a.per_head) {
+        const int2 plan = a.plan[b];
+        n = plan.y;
+        first = plan.x + (int64_t)h * n;
+        if (n == 1)
+            return;                                       // written already
+    } else {
+        n = (clamp_length(a.lengths[b], a.W, page_log2) + a.chunk - 1) / a.chunk;
+        n = n < 1 ? 1 : n > a.splits ? a.splits : n;
+        first = (int64_t)unit * a.splits;
     }
-    out[(int64_t)head * d_k + d] = z > 0.f ? o / z : 0.f;
+    const int row = d_k + 2;
+    {
+        const int g = blockIdx.y, d = threadIdx.x;
+        const float *x = a.part + (first * G + g) * row;
+        float top = -1e30f, o = 0.f, z = 0.f;
+        for (int s0 = 0; s0 < n; s0 += GR) {
+            float m_[GR], z_[GR], o_[GR];
+#pragma unroll
+            for (int k = 0; k < GR; ++k) {
+                const float *y = x + (int64_t)(s0 + k < n ? s0 + k : s0) * G * row;
+                m_[k] = y[d_k];
+                z_[k] = y[d_k + 1];
+                o_[k] = y[d];
+            }
+            float to = top;
+#pragma unroll
+            for (int k = 0; k < GR; ++k)
+                to = fmaxf(to, m_[k]);
+            const float fix = fast_exp2(top - to);
+            o *= fix;
+            z *= fix;
+#pragma unroll
+            for (int k = 0; k < GR; ++k) {
+                const float f = s0 + k < n ? fast_exp2(m_[k] - to) : 0.f;
+                o = fmaf(f, o_[k], o);
+                z = fmaf(f, z_[k], z);
+            }
+            top = to;
+        }
+        a.out[((int64_t)unit * G + g) * d_k + d] = z > 0.f ? o / z : 0.f;
+    }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
-static int attend_waves(int G, int m)
-{
-    const int tables = G * m;       // KB
-    return tables <= 16 ? 4 : tables <= 32 ? 8 : tables <= 64 ? 16 : 8;
-}
+// Ranges by length: how many, and from how many tokens on.  us a call (int8, d_k = 128, m = 8 unless said) for 512 / 1024 / 2048 / 4096 ranges in all,
+// not under 1024 tokens each: 8 x 32 heads x 32768 tokens 174.7 / 171.8 / 169.0 / 171.2 (the more, the less the last ones run alone; two
+// workgroups on a compute unit do not share it evenly); 32 x 8 x up to 8192 34.0 / 34.2 / 33.4 / 35.0; 16 x 12 x 4096 (d_k = 64, m = 4)
+// 16.1 / 14.6 / 15.3 / 17.4; 28 x 25 x up to 4859 (same) 30.5 / 28.7 / 30.4 / 30.7; 1 x 8 x 32768 in groups of 4 15.4 / 15.3 / 15.8 / 18.3.
+// So 1024, and 2048 where those still have 4096 tokens.  Least range of 512 / 1024 / 2048 tokens (1024 ranges): 2 heads in groups of 8 x 3000
+// 10.3 / 11.6 / 13.6; 1 x 32 x 8192 13.5 / 13.4 / 15.5; 8 x 32 x up to 1500 16.7 / 14.8 / 14.0; 64 KB of tables (groups of 8, m = 8), which every
+// range fetches: 12 x 8 x up to 8191 25.3 / 21.1 / 20.3, 64 x 4 x up to 2048 27.6 / 23.0 / 21.9.  So 1024, and 2048 from 64 KB on.
+static int least_range(int G, int m) { return G * m >= 64 ? 2048 : 1024; }
 
-// Ranges per (sequence, key/value head).
-static int attend_auto_splits(const lookat_page_pool *p, int32_t B, int32_t G, int64_t longest)
+// How a call is cut up.
+struct Cut {
+    int per_head;     // ranges by length: ranges per head, or 0
+    int splits;       // equal ranges
+    int64_t groups;   // workgroups
+    int64_t ranges;   // ranges whose results the workspace holds (0: none)
+};
+static Cut cut_of(const lookat_page_pool *p, int32_t B, int32_t G, int64_t longest, int32_t num_splits)
 {
     const int64_t units = (int64_t)B * p->H;
-    int64_t want = (1024 + units - 1) / units;
-    const int64_t cap = (longest + 1023) / 1024;
-    want = want < cap ? want : cap;
-    return (int)(want < 1 ? 1 : want);
+    Cut c;
+    c.per_head = 0;
+    c.splits = num_splits ? num_splits : 1;
+    if (num_splits == 0 && longest > least_range(G, p->m) && B <= kMostPlanned) {
+        const int64_t target = units * longest >= 2048LL * 4096 ? 2048 : 1024;
+        c.per_head = (int)((target + p->H - 1) / p->H);
+        c.ranges = (int64_t)p->H * (c.per_head + 1 + B);
+        c.groups = (c.ranges + kXcds - 1) / kXcds * kXcds;
+        return c;
+    }
+    c.ranges = c.splits == 1 ? 0 : units * c.splits;
+    c.groups = (units + kXcds - 1) / kXcds * kXcds * c.splits;
+    return c;
+}
+static size_t cut_bytes(const lookat_page_pool *p, int32_t B, int32_t G, const Cut &c)
+{
+    const size_t plan = c.per_head ? ((size_t)B * sizeof(int2) + 15) / 16 * 16 : 0;
+    return plan + (size_t)c.ranges * G * (p->d_k + 2) * sizeof(float);
 }
 
 static int check_attend(const lookat_page_pool *pool, int32_t B, int32_t group, int32_t W, int64_t max_length, int32_t num_splits)
@@ -376,8 +673,7 @@ static int64_t longest_of(const lookat_page_pool *pool, int32_t W, int64_t max_l
 template <int DK, int M, int G>
 static int launch_attend(const PoolArgs &p, const AttendArgs &a, bool fp8, dim3 grid, hipStream_t st)
 {
-    const int waves = attend_waves(G, M);
-    const size_t lds = attend_lds_bytes(G, M, DK, waves);
+    const size_t lds = attend_lds_bytes(G, M, DK);
     const void *f = fp8 ? reinterpret_cast<const void *>(&attend_pages_kernel<DK, M, G, true>)
                         : reinterpret_cast<const void *>(&attend_pages_kernel<DK, M, G, false>);
     if (lds > 64 * 1024) {
@@ -386,9 +682,9 @@ static int launch_attend(const PoolArgs &p, const AttendArgs &a, bool fp8, dim3 
             return fail(LOOKAT_ERR_HIP, "lookat_attend_pages: %s", hipGetErrorString(e));
     }
     if (fp8)
-        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, true>), grid, dim3(waves * kWave), lds, st, p, a);
+        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, true>), grid, dim3(kAttendThreads), lds, st, p, a);
     else
-        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, false>), grid, dim3(waves * kWave), lds, st, p, a);
+        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, false>), grid, dim3(kAttendThreads), lds, st, p, a);
     return check_launch("lookat_attend_pages");
 }
 template <int DK, int M>
@@ -414,15 +710,6 @@ static int launch_attend_m(int G, const PoolArgs &p, const AttendArgs &a, bool f
 
 }  // namespace lookat
 
-extern "C" int32_t lookat_attend_pages_auto_splits(const lookat_page_pool *pool, int32_t B, int32_t group, int32_t W, int64_t max_length)
-{
-    using namespace lookat;
-    clear_error();
-    if (check_attend(pool, B, group, W, max_length, 0) != LOOKAT_OK)
-        return 0;
-    return attend_auto_splits(pool, B, group, longest_of(pool, W, max_length));
-}
-
 extern "C" size_t lookat_attend_pages_workspace_bytes(const lookat_page_pool *pool, int32_t B, int32_t group, int32_t W, int64_t max_length,
                                                       int32_t num_splits)
 {
@@ -430,8 +717,7 @@ extern "C" size_t lookat_attend_pages_workspace_bytes(const lookat_page_pool *po
     clear_error();
     if (check_attend(pool, B, group, W, max_length, num_splits) != LOOKAT_OK)
         return 0;
-    const int S = num_splits ? num_splits : attend_auto_splits(pool, B, group, longest_of(pool, W, max_length));
-    return S == 1 ? 0 : (size_t)B * pool->H * group * S * (pool->d_k + 2) * sizeof(float);
+    return cut_bytes(pool, B, group, cut_of(pool, B, group, longest_of(pool, W, max_length), num_splits));
 }
 
 extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int32_t group, const float *lut, const int32_t *table, int32_t W,
@@ -451,38 +737,41 @@ extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int3
     if (reinterpret_cast<uintptr_t>(lengths) & 3u)
         return fail(LOOKAT_ERR_ALIGN, "lengths must be 4-byte aligned");
     const int64_t longest = longest_of(pool, W, max_length);
-    const int S = num_splits ? num_splits : attend_auto_splits(pool, B, group, longest);
-    const size_t need = lookat_attend_pages_workspace_bytes(pool, B, group, W, max_length, S);
+    const Cut cut = cut_of(pool, B, group, longest, num_splits);
+    const size_t need = cut_bytes(pool, B, group, cut);
     if (need) {
         if (!workspace || workspace_bytes < need)
-            return fail(LOOKAT_ERR_WORKSPACE, "workspace of %zu bytes needed for %d splits, got %zu", need, S, workspace ? workspace_bytes : (size_t)0);
+            return fail(LOOKAT_ERR_WORKSPACE, "workspace of %zu bytes needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
         if (!aligned16(workspace))
             return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
     }
     const int64_t units = (int64_t)B * pool->H;
-    const int64_t groups = (units + kXcds - 1) / kXcds * kXcds * S;
-    if (groups > 0x7fffffffLL || units * group > 0x7fffffffLL)
-        return fail(LOOKAT_ERR_UNSUPPORTED, "B*H*num_splits=%lld workgroups exceed one launch", (long long)groups);
+    if (cut.groups > 0x7fffffffLL || units * group > 0x7fffffffLL)
+        return fail(LOOKAT_ERR_UNSUPPORTED, "B*H*num_splits: %lld workgroups exceed one launch", (long long)cut.groups);
     const PoolArgs p = pool_args(pool);
     AttendArgs a;
     a.lut = lut;
     a.table = table;
     a.lengths = lengths;
-    a.part = static_cast<float *>(workspace);
+    const size_t plan_bytes = cut.per_head ? ((size_t)B * sizeof(int2) + 15) / 16 * 16 : 0;
+    a.plan = static_cast<int2 *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan_bytes);
     a.out = out;
     a.table_stride = table_stride;
     a.W = W;
+    a.B = B;
     a.units = (int32_t)units;
-    a.splits = S;
-    a.chunk = (int32_t)(((longest + S - 1) / S + kTile - 1) / kTile * kTile);
+    a.per_head = cut.per_head;
+    a.least = least_range(group, p.m);
+    a.splits = cut.splits;
+    a.chunk = (int32_t)(((longest + cut.splits - 1) / cut.splits + kTile - 1) / kTile * kTile);
     a.scale_log2e = scale * kLog2e;
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)groups);
+    const dim3 grid((unsigned)cut.groups);
     const int rc = p.d_k == 64 ? launch_attend_m<64>(group, p, a, fp8, grid, st) : launch_attend_m<128>(group, p, a, fp8, grid, st);
-    if (rc != LOOKAT_OK || S == 1)
+    if (rc != LOOKAT_OK || !need)
         return rc;
-    hipLaunchKernelGGL(attend_pages_merge_kernel, dim3((unsigned)(units * group)), dim3(p.d_k), 0, st, a.part, out, lengths, S, a.chunk, p.d_k,
-                       pool->H * group, W, p.page_log2);
+    hipLaunchKernelGGL(attend_pages_merge_kernel, dim3((unsigned)units, group), dim3(p.d_k), 0, st, a, pool->H, group, p.d_k, p.page_log2);
     return check_launch("lookat_attend_pages (merge)");
 }

@@ -211,6 +211,18 @@ def test_attend_long(lk, kind):
         assert_attend(attend_case(lk, rng, c, lengths, 1, 0.2, num_splits=splits), f"one long row, {kind}")
 
 
+@pytest.mark.parametrize("B", [63, 64, 65, 300, 1024, 1025, 1500])
+def test_attend_many_sequences(lk, B):
+    """Ranges by length over few and many sequences (a lane, a thread or several sequences a thread look at them), and equal ranges beyond."""
+    rng = np.random.default_rng(B)
+    lengths = (np.exp(rng.uniform(0, np.log(5000 if B < 200 else 300), B))).astype(int)
+    lengths[rng.integers(0, B, B // 5)] = 0
+    lengths[[0, B // 2, B - 1]] = [4500, 2049, 6001]      # cut into ranges, whatever the others are
+    lengths = lengths.tolist()
+    c = random_cache(rng, sum(-(-n // 128) for n in lengths), 1, 64, 2, 128, "int8")
+    assert_attend(attend_case(lk, rng, c, lengths, 1), "many sequences")
+
+
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 def test_attend_peaked_and_flat(lk, kind):
     """Logits from nothing to hundreds, rising and falling along the row (the reference has to follow)."""

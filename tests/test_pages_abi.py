@@ -103,12 +103,10 @@ def test_attend_refusals_and_workspace(lib):  # noqa: F811
     assert need(ctypes.byref(p), 5, 2, 7, 0, 3) == 5 * H * 2 * 3 * (D + 2) * 4
     assert call(p, ws=None) == E_WS and call(p, wsb=need(ctypes.byref(p), 5, 2, 7, 0, 3) - 1) == E_WS
     assert call(p, ws=FAKE + 4) == E_ALIGN
-    auto = lib.lookat_attend_pages_auto_splits
-    assert auto(ctypes.byref(p), 5, 2, 7, 0) >= 1
-    assert auto(ctypes.byref(p), 5, 3, 7, 0) == 0 and auto(None, 5, 1, 7, 0) == 0
-    # one user with a long cache is cut into ranges, unless the caller knows that it is short
-    assert auto(ctypes.byref(p), 1, 1, 1024, 0) > 1 and auto(ctypes.byref(p), 1, 1, 1024, 64) == 1
-    assert need(ctypes.byref(p), 1, 1, 1024, 0, 0) == H * auto(ctypes.byref(p), 1, 1, 1024, 0) * (D + 2) * 4
+    assert need(ctypes.byref(p), 5, 3, 7, 0, 0) == 0 and need(None, 5, 1, 7, 0, 3) == 0           # (refused by the call)
+    # long caches are cut into ranges, unless the caller knows that they are short
+    assert need(ctypes.byref(p), 1, 1, 1024, 0, 0) > 0 and need(ctypes.byref(p), 1, 1, 1024, 64, 0) == 0
+    assert call(p, W=1024, stride=1024, splits=0, wsb=need(ctypes.byref(p), 5, 2, 1024, 0, 0) - 1) == E_WS
 
 
 def test_upkeep_refusals(lib):  # noqa: F811
