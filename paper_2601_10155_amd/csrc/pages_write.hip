@@ -3,10 +3,10 @@
 //   e = min { e : max |v| <= Q 2^e } (Q = 127 or 448),   q = round(v 2^-e)      (kept tokens: q' = round(q 2^(e_old - e)))
 //
 // v 2^-e is exact in fp32, so every stored number is one rounding (to nearest, ties to even) away from its value, whatever computes it.
-// Memory-bound: each value is read once (2 or 4 bytes) and written once (1 byte).  A thread owns 8 tokens x 8 coordinates: it
-// loads 8 rows of 16 (fp16) or 32 (fp32) bytes, all requested before the first is used, keeps them in registers while the page's
-// threads agree on the exponent, and writes the 64 bytes that those numbers occupy in the page ([octet][coordinate][token]) as
-// four 16-byte stores: the transposition costs no shared memory.
+// Memory-bound: each value is read once (2 or 4 bytes) and written once (1 byte).  A thread owns 8 tokens x 16 bytes of coordinates (8 in
+// fp16, 4 in fp32): it loads 8 rows of 16 bytes, all requested before the first is used, keeps them in registers while the page's threads
+// agree on the exponent, and writes what those numbers occupy in the page ([octet][coordinate][token]: 64 or 32 consecutive bytes) as 16-byte
+// stores: the transposition costs no shared memory.  A single token (a decode step's) has a kernel of its own, a wavefront per head.
 #include "pages.h"
 
 namespace lookat {
@@ -67,84 +67,138 @@ __device__ __forceinline__ void unpack4(uint32_t w, float (&x)[4])
     }
 }
 
-constexpr int kWriteThreads = 256;
+// Where the tokens of a sequence go: row 0 at position `first`, positions [start, end) are written (all in 64 bits: lengths and counts may be
+// any 32-bit numbers).
+struct Span {
+    int64_t first;
+    int start, end;
+};
+__device__ __forceinline__ Span span_of(const WriteArgs &a, int b, int page_log2)
+{
+    const int64_t given = a.lengths[b] < 0 ? 0 : a.lengths[b], most = (int64_t)a.W << page_log2;
+    int64_t count = a.counts ? a.counts[b] : a.N;
+    count = count < 0 ? 0 : count;
+    Span s;
+    s.first = given - count;
+    int64_t end = s.first + (count < a.N ? count : a.N);
+    end = end < most ? end : most;
+    const int64_t start = s.first > 0 ? s.first : 0;
+    s.end = (int)(end > 0 ? end : 0);
+    s.start = (int)(start < s.end ? start : s.end);
+    return s;
+}
+
+template <typename FT>
+__device__ __forceinline__ void to_f32(const u32x4 &raw, float (&x)[16 / sizeof(FT)])
+{
+    if constexpr (sizeof(FT) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = raw[k];                            // (a bit cast of the element itself takes element 0 for every k)
+            const float2 f = __half22float2(__builtin_bit_cast(__half2, w));
+            x[2 * k] = f.x;
+            x[2 * k + 1] = f.y;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            x[k] = __uint_as_float(raw[k]);
+    }
+}
+
+// The largest value of the caller's aligned group of 2^n lanes, n in 4 to 6.
+__device__ __forceinline__ float group_top(float x, int n)
+{
+    float a, b;
+    x = fmaxf(x, dpp_mov<0xB1>(x, x));
+    x = fmaxf(x, dpp_mov<0x4E>(x, x));
+    x = fmaxf(x, dpp_mov<0x141>(x, x));
+    x = fmaxf(x, dpp_mov<0x140>(x, x));
+    if (n > 4) {
+        lanes_xor16(x, a, b);
+        x = fmaxf(a, b);
+    }
+    if (n > 5) {
+        lanes_xor32(x, a, b);
+        x = fmaxf(a, b);
+    }
+    return x;
+}
+
+// An exponent that these kernels did not write may be any int8: 2^(old - e) is then below 2^-126, whose products round to zero too.
+__device__ __forceinline__ float rescale(int old_e, int e) { return two_to(old_e - e < -126 ? -126 : old_e - e); }
+
+// codes of one token, m bytes, aligned to m
+__device__ __forceinline__ void copy_code(uint8_t *dst, const uint8_t *src, int m, int t)
+{
+    if (m == 2)
+        reinterpret_cast<uint16_t *>(dst)[t] = reinterpret_cast<const uint16_t *>(src)[t];
+    else if (m == 4)
+        reinterpret_cast<uint32_t *>(dst)[t] = reinterpret_cast<const uint32_t *>(src)[t];
+    else if (m == 8)
+        reinterpret_cast<uint2 *>(dst)[t] = reinterpret_cast<const uint2 *>(src)[t];
+    else
+        reinterpret_cast<u32x4 *>(dst)[t] = reinterpret_cast<const u32x4 *>(src)[t];
+}
+
+constexpr int kWriteThreads = 512;
 
 // grid: (touched page of the sequence, group of heads, sequence)
 template <int DK, typename FT, bool FP8>
 __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(PoolArgs p, WriteArgs a)
 {
+    constexpr int CW = 16 / sizeof(FT);                           // coordinates of a thread
+    constexpr int groups = DK / CW, groups_log2 = groups == 8 ? 3 : groups == 16 ? 4 : 5;
     const int b = blockIdx.z, tid = threadIdx.x;
     const int page = 1 << p.page_log2;
-    // threads per page: (page / 8) octets x (DK / 8) coordinate groups, 16 to 256
-    const int per_page_log2 = p.page_log2 - 3 + (DK == 128 ? 4 : 3);
+    const int per_page_log2 = p.page_log2 - 3 + groups_log2;      // threads per page: 16 to 512
     const int item = tid & ((1 << per_page_log2) - 1);
     const int h = blockIdx.y * (kWriteThreads >> per_page_log2) + (tid >> per_page_log2);
-    const int most = a.W << p.page_log2;
-    // all positions in 64 bits: lengths and counts may be any 32-bit numbers
-    const int64_t given = a.lengths[b] < 0 ? 0 : a.lengths[b];
-    int64_t count = a.counts ? a.counts[b] : a.N;
-    count = count < 0 ? 0 : count;
-    const int64_t first = given - count;                          // position of row 0
-    int64_t end = first + (count < a.N ? count : a.N);            // behind the last row's
-    end = end < most ? end : most;
-    const int start = (int)(first > 0 ? first : 0);
-    if (end <= start)
+    const Span span = span_of(a, b, p.page_log2);
+    const int slot = (span.start >> p.page_log2) + blockIdx.x;    // entry of the sequence's row
+    if (slot >= a.W)
         return;
-    const int slot = (start >> p.page_log2) + blockIdx.x;         // entry of the sequence's row
     const int p0 = slot << p.page_log2;
-    if (p0 >= end)
+    if (p0 >= span.end || span.end <= span.start)
         return;
     const int id = a.table[b * a.table_stride + slot];
+    const bool mine = h < p.H;
+    const int from = span.start > p0 ? span.start - p0 : 0;       // tokens [from, to) of the page are new, [0, from) are kept
+    const int to = span.end - p0 < page ? span.end - p0 : page;
+    const int octet = item >> groups_log2, t0 = octet * 8, col = (item & (groups - 1)) * CW;
+    const bool fresh = mine && t0 < to && t0 + 8 > from, whole = t0 >= from && t0 + 8 <= to;
+    const FT *rows = static_cast<const FT *>(a.values) + ((int64_t)b * p.H + h) * a.value_stride + (p0 - span.first) * DK + col;
+
+    u32x4 raw[8];
+    if (fresh) {
+        // (rows outside the new ones repeat the nearest new one: no branch between the loads, and the maximum does not mind)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const int at = t0 + t < from ? from : t0 + t >= to ? to - 1 : t0 + t;
+            raw[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(rows + (int64_t)at * DK));
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            raw[t] = (u32x4){0, 0, 0, 0};
+    }
     if ((uint32_t)id >= (uint32_t)p.pages)
         return;
-    const bool mine = h < p.H;
-    const int from = start > p0 ? start - p0 : 0;                 // tokens [from, to) of the page are new, [0, from) are kept
-    const int to = (int)(end - p0 < page ? end - p0 : page);
-    const int octet = item / (DK / 8), col = (item % (DK / 8)) * 8;
     const int64_t place = (int64_t)id * p.H + h;
-    const FT *rows = static_cast<const FT *>(a.values) + ((int64_t)b * p.H + h) * a.value_stride + (p0 - first + octet * 8) * DK + col;
-
-    float v[8][8];                                                // [token][coordinate]
-    float top = 0.f;
-    const bool fresh = mine && octet * 8 < to && octet * 8 + 8 > from;
-    uint4 raw[8][sizeof(FT) / 2];
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-#pragma unroll
-        for (int k = 0; k < (int)sizeof(FT) / 2; ++k) {
-            raw[t][k] = make_uint4(0, 0, 0, 0);
-            if (fresh && octet * 8 + t >= from && octet * 8 + t < to)
-                raw[t][k] = reinterpret_cast<const uint4 *>(rows + (int64_t)t * DK)[k];
-        }
+    u32x4 *bytes = reinterpret_cast<u32x4 *>(p.values + place * ((int64_t)page * DK) + (t0 * DK + col * 8));
     int old_e = kLowExponent;
     if (mine && from > 0)
         old_e = p.exponents[place];
+    float top = 0.f;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-        if constexpr (sizeof(FT) == 2) {
-            const __half2 *x = reinterpret_cast<const __half2 *>(&raw[t][0]);
+        float x[CW];
+        to_f32<FT>(raw[t], x);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 f = __half22float2(x[k]);
-                v[t][2 * k] = f.x;
-                v[t][2 * k + 1] = f.y;
-            }
-        } else {
-            const float *x = reinterpret_cast<const float *>(&raw[t][0]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                v[t][k] = x[k];
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            top = fmaxf(top, fabsf(v[t][k]));                     // (a NaN is not the larger one)
+        for (int k = 0; k < CW; ++k)
+            top = fmaxf(top, fabsf(x[k]));                        // (a NaN is not the larger one)
     }
-    // the page's threads are 16, 32 or 64 lanes of a wavefront, or 2 or 4 wavefronts
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const float other = __shfl_xor(top, d);
-        top = d < (1 << per_page_log2) ? fmaxf(top, other) : top;
-    }
+    top = group_top(top, per_page_log2);
     if (per_page_log2 > 6) {
         // (the old exponent goes through shared memory too: every wavefront has it before one of them writes the new one)
         __shared__ float tops[kWriteThreads / kWave];
@@ -165,81 +219,143 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(PoolArgs p, 
     e = from > 0 && old_e > e ? old_e : e;
     if (item == 0)
         p.exponents[place] = (int8_t)e;
-    const bool again = from > octet * 8 && e != old_e;            // kept tokens of this octet get the new exponent
+    const bool again = t0 < from && e != old_e;                   // kept tokens of this octet get the new exponent
     if (fresh || again) {
-        uint4 *bytes = reinterpret_cast<uint4 *>(p.values + place * ((int64_t)page * DK) + (octet * DK + col) * 8);
-        uint4 was[4];
-        const bool partly = octet * 8 < from || octet * 8 + 8 > to;
-        if (partly) {
+        const float down = two_to(-e), back = rescale(old_e, e);
+        u32x4 out[CW / 2];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                was[k] = bytes[k];
+        for (int t = 0; t < 8; t += 4) {
+            float x[4][CW];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                to_f32<FT>(raw[t + i], x[i]);
+#pragma unroll
+            for (int c = 0; c < CW; ++c)
+                out[c / 2][2 * (c % 2) + t / 4] = pack4<FP8>(x[0][c] * down, x[1][c] * down, x[2][c] * down, x[3][c] * down);
         }
-        // (an exponent that this kernel did not write may be any int8: 2^(old - e) down to 2^-168, the lowest rounds everything to zero too)
-        const float down = two_to(-e), back = two_to(old_e - e < -126 ? -126 : old_e - e);
+        if (!whole) {
+            // kept tokens, in the new exponent, and what lies behind the last token, as it was
+            uint32_t is_new[2], is_kept[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t w[4];
+            for (int w = 0; w < 2; ++w) {
+                is_new[w] = is_kept[w] = 0;
 #pragma unroll
-            for (int c2 = 0; c2 < 2; ++c2) {
-                const int c = 2 * k + c2;
-#pragma unroll
-                for (int t4 = 0; t4 < 2; ++t4) {
-                    const int t = 4 * t4;
-                    w[2 * c2 + t4] = pack4<FP8>(v[t][c] * down, v[t + 1][c] * down, v[t + 2][c] * down, v[t + 3][c] * down);
-                    if (partly) {
-                        const uint32_t old = reinterpret_cast<const uint32_t *>(&was[k])[2 * c2 + t4];
-                        uint32_t kept = old;
-                        if (again) {
-                            float x[4];
-                            unpack4<FP8>(old, x);
-                            kept = pack4<FP8>(x[0] * back, x[1] * back, x[2] * back, x[3] * back);
-                        }
-                        uint32_t out = 0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int token = octet * 8 + t + i;
-                            const uint32_t from_which = token < from ? kept : token < to ? w[2 * c2 + t4] : old;
-                            out |= from_which & (0xffu << (8 * i));
-                        }
-                        w[2 * c2 + t4] = out;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const int token = t0 + 4 * w + i;
+                    is_kept[w] |= token < from ? 0xffu << (8 * i) : 0u;
+                    is_new[w] |= token >= from && token < to ? 0xffu << (8 * i) : 0u;
                 }
             }
-            bytes[k] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+            for (int k = 0; k < CW / 2; ++k) {
+                const u32x4 was = bytes[k];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t kept = was[j];
+                    if (again) {
+                        float x[4];
+                        unpack4<FP8>(was[j], x);
+                        kept = pack4<FP8>(x[0] * back, x[1] * back, x[2] * back, x[3] * back);
+                    }
+                    out[k][j] = (out[k][j] & is_new[j & 1]) | (kept & is_kept[j & 1]) | (was[j] & ~(is_new[j & 1] | is_kept[j & 1]));
+                }
+            }
         }
+#pragma unroll
+        for (int k = 0; k < CW / 2; ++k)
+            bytes[k] = out[k];
     }
     // codes: m bytes a token, one after another on both sides
-    const int m = p.m;
-    const uint8_t *src = a.codes + ((int64_t)b * p.H + h) * a.code_stride + (p0 - first) * m;
-    uint8_t *dst = p.codes + (place << p.page_log2) * m;
-    for (int t = from + item; t < to; t += 1 << per_page_log2) {
-        if (m == 2)
-            reinterpret_cast<uint16_t *>(dst)[t] = reinterpret_cast<const uint16_t *>(src)[t];
-        else if (m == 4)
-            reinterpret_cast<uint32_t *>(dst)[t] = reinterpret_cast<const uint32_t *>(src)[t];
-        else if (m == 8)
-            reinterpret_cast<uint2 *>(dst)[t] = reinterpret_cast<const uint2 *>(src)[t];
-        else
-            reinterpret_cast<uint4 *>(dst)[t] = reinterpret_cast<const uint4 *>(src)[t];
-    }
+    const uint8_t *src = a.codes + ((int64_t)b * p.H + h) * a.code_stride + (p0 - span.first) * p.m;
+    uint8_t *dst = p.codes + (place << p.page_log2) * p.m;
+    for (int t = from + item; t < to; t += 1 << per_page_log2)
+        copy_code(dst, src, p.m, t);
 }
 
-template <typename FT>
-static void launch_write(const PoolArgs &p, const WriteArgs &a, bool fp8, dim3 grid, hipStream_t st)
+// One token per sequence: a wavefront per head, a lane per DK / 64 coordinates; nothing but the token is touched unless the exponent grows.
+constexpr int kTokenThreads = 256;
+template <int DK, typename FT, bool FP8>
+__global__ __launch_bounds__(kTokenThreads) void pages_write_token_kernel(PoolArgs p, WriteArgs a)
 {
-    const dim3 block(kWriteThreads);
-    if (p.d_k == 64) {
-        if (fp8)
-            hipLaunchKernelGGL((pages_write_kernel<64, FT, true>), grid, block, 0, st, p, a);
-        else
-            hipLaunchKernelGGL((pages_write_kernel<64, FT, false>), grid, block, 0, st, p, a);
-    } else {
-        if (fp8)
-            hipLaunchKernelGGL((pages_write_kernel<128, FT, true>), grid, block, 0, st, p, a);
-        else
-            hipLaunchKernelGGL((pages_write_kernel<128, FT, false>), grid, block, 0, st, p, a);
+    constexpr int CL = DK / kWave;
+    const int lane = threadIdx.x & (kWave - 1), b = blockIdx.y, h = blockIdx.x * (kTokenThreads / kWave) + threadIdx.x / kWave;
+    if (h >= p.H)
+        return;
+    const int64_t head = (int64_t)b * p.H + h;
+    float x[CL];
+#pragma unroll
+    for (int c = 0; c < CL; ++c)
+        x[c] = (float)(static_cast<const FT *>(a.values)[head * a.value_stride + lane * CL + c]);
+    const Span span = span_of(a, b, p.page_log2);
+    if (span.end <= span.start || span.first < 0)                 // (first < 0: row 0 is not among the tokens that have a place)
+        return;
+    const int pos = span.start;
+    const int id = a.table[b * a.table_stride + (pos >> p.page_log2)];
+    if ((uint32_t)id >= (uint32_t)p.pages)
+        return;
+    const int page = 1 << p.page_log2, t = pos & (page - 1);
+    const int64_t place = (int64_t)id * p.H + h;
+    uint8_t *bytes = p.values + place * ((int64_t)page * DK);
+    const int old_e = p.exponents[place];
+    if (lane == 0)
+        copy_code(p.codes + ((place << p.page_log2) + t) * p.m, a.codes + head * a.code_stride, p.m, 0);
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < CL; ++c)
+        top = fmaxf(top, fabsf(x[c]));
+    int e = exponent_of<FP8>(wave_max(top));
+    e = t > 0 && old_e > e ? old_e : e;
+    const float down = two_to(-e);
+    if (t > 0 && e != old_e) {
+        // the tokens that the page holds, in the new exponent: an octet's bytes in pieces of two coordinates
+        const float back = rescale(old_e, e);
+        const int pieces = ((t + 7) >> 3) * (DK / 2);
+        for (int j = lane; j < pieces; j += kWave) {
+            u32x4 w = reinterpret_cast<u32x4 *>(bytes)[j];
+            const int t0 = j / (DK / 2) * 8;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float y[4];
+                unpack4<FP8>(w[k], y);
+                const uint32_t again = pack4<FP8>(y[0] * back, y[1] * back, y[2] * back, y[3] * back);
+                const int n = t - t0 - 4 * (k & 1);               // kept tokens among these four
+                const uint32_t kept = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+                w[k] = (again & kept) | (w[k] & ~kept);
+            }
+            reinterpret_cast<u32x4 *>(bytes)[j] = w;
+        }
+        // (the token's own bytes lie in words that other lanes have just written: after them)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_wave_barrier();
     }
+    if (lane == 0)
+        p.exponents[place] = (int8_t)e;
+    uint8_t *own = bytes + (t >> 3) * (DK * 8) + (t & 7);
+#pragma unroll
+    for (int c = 0; c < CL; ++c)
+        own[(lane * CL + c) * 8] = (uint8_t)pack4<FP8>(x[c] * down, 0.f, 0.f, 0.f);
+}
+
+template <int DK, typename FT, bool FP8>
+static void launch_write(const PoolArgs &p, const WriteArgs &a, int B, int64_t touched, hipStream_t st)
+{
+    if (a.N == 1) {
+        const int heads = kTokenThreads / kWave;
+        hipLaunchKernelGGL((pages_write_token_kernel<DK, FT, FP8>), dim3((unsigned)((p.H + heads - 1) / heads), (unsigned)B), dim3(kTokenThreads), 0, st, p, a);
+        return;
+    }
+    const int per_page = (1 << p.page_log2) / 8 * (DK / (16 / (int)sizeof(FT))), heads = kWriteThreads / per_page;
+    hipLaunchKernelGGL((pages_write_kernel<DK, FT, FP8>), dim3((unsigned)touched, (unsigned)((p.H + heads - 1) / heads), (unsigned)B), dim3(kWriteThreads),
+                       0, st, p, a);
+}
+template <typename FT>
+static void launch_write_any(const PoolArgs &p, const WriteArgs &a, bool fp8, int B, int64_t touched, hipStream_t st)
+{
+    if (p.d_k == 64)
+        fp8 ? launch_write<64, FT, true>(p, a, B, touched, st) : launch_write<64, FT, false>(p, a, B, touched, st);
+    else
+        fp8 ? launch_write<128, FT, true>(p, a, B, touched, st) : launch_write<128, FT, false>(p, a, B, touched, st);
 }
 
 }  // namespace lookat
@@ -288,13 +404,11 @@ extern "C" int lookat_pages_write(const lookat_page_pool *pool, int32_t B, int64
     a.W = W;
     int64_t touched = (N + pool->page - 2) / pool->page + 1;      // N tokens from anywhere in a page on
     touched = touched < W ? touched : W;
-    const int per_page = pool->page / 8 * (pool->d_k / 8), heads = kWriteThreads / per_page;
-    const dim3 grid((unsigned)touched, (unsigned)((p.H + heads - 1) / heads), (unsigned)B);
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (value_dtype == LOOKAT_F16)
-        launch_write<__half>(p, a, fp8, grid, st);
+        launch_write_any<__half>(p, a, fp8, B, touched, st);
     else
-        launch_write<float>(p, a, fp8, grid, st);
+        launch_write_any<float>(p, a, fp8, B, touched, st);
     return check_launch("lookat_pages_write");
 }
