@@ -78,22 +78,32 @@ __device__ __forceinline__ int pages_of(int length, const BookArgs &a)
 
 constexpr int kBookThreads = 256;
 
-// Sum over the workgroup; every thread ends with it.  `s`: one int per wavefront in LDS.
+// Sums over the workgroup of two numbers; every thread ends with them.  `s`: two ints per wavefront in LDS.
+template <int THREADS>
+__device__ __forceinline__ int2 block_sums(int x, int y, int *s)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        x += __shfl_xor(x, d);
+        y += __shfl_xor(y, d);
+    }
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0)
+        reinterpret_cast<int2 *>(s)[threadIdx.x / kWave] = make_int2(x, y);
+    __syncthreads();
+    int2 t = make_int2(0, 0);
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w) {
+        const int2 v = reinterpret_cast<const int2 *>(s)[w];
+        t.x += v.x;
+        t.y += v.y;
+    }
+    return t;
+}
 template <int THREADS>
 __device__ __forceinline__ int block_sum(int v, int *s)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1)
-        v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0)
-        s[threadIdx.x / kWave] = v;
-    __syncthreads();
-    int t = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / kWave; ++w)
-        t += s[w];
-    return t;
+    return block_sums<THREADS>(v, 0, s).x;
 }
 // Sum over the threads before this one in the workgroup; *total = over all.
 template <int THREADS>
@@ -136,7 +146,7 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PoolArgs p, co
 // writes: a source that is somebody's destination is out, a destination belongs to the first pair that names it.
 __global__ __launch_bounds__(kBookThreads) void pages_fork_kernel(BookArgs a, int n, const int32_t *__restrict__ src, const int32_t *__restrict__ dst)
 {
-    __shared__ int s[kBookThreads / kWave];
+    __shared__ __align__(8) int s[2 * kBookThreads / kWave];
     const int i = blockIdx.x, tid = threadIdx.x;
     const int from = src[i], to = dst[i];
     if ((uint32_t)from >= (uint32_t)a.S || (uint32_t)to >= (uint32_t)a.S)
@@ -168,7 +178,7 @@ __global__ __launch_bounds__(kBookThreads) void pages_fork_kernel(BookArgs a, in
 // ---- free -------------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(kBookThreads) void pages_free_kernel(BookArgs a, const int32_t *__restrict__ slots)
 {
-    __shared__ int s[kBookThreads / kWave];
+    __shared__ __align__(8) int s[2 * kBookThreads / kWave];
     const int i = blockIdx.x, tid = threadIdx.x;
     const int slot = slots[i];
     if ((uint32_t)slot >= (uint32_t)a.S)
@@ -202,28 +212,45 @@ struct ReservePlan {
     int32_t *count;      // [0]: free pages
 };
 
-// What needs x pages of refs: counts of (refs[j] > 0) over [0, end) by the whole workgroup, 16 bytes a load.
-template <int THREADS>
-__device__ __forceinline__ int live_before(const int32_t *__restrict__ refs, int end, int *s)
-{
-    int n = 0;
-    const int whole = (reinterpret_cast<uintptr_t>(refs) & 15u) ? 0 : end & ~3;
-    for (int j = threadIdx.x * 4; j < whole; j += THREADS * 4) {
-        const int4 r = *reinterpret_cast<const int4 *>(refs + j);
-        n += (r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0);
-    }
-    for (int j = whole + threadIdx.x; j < end; j += THREADS)
-        n += refs[j] > 0;
-    return block_sum<THREADS>(n, s);
-}
-
 constexpr int kRankThreads = 1024;
 constexpr int kSegments = 64;            // workgroups over the pages, at most
 
+// Which pages are in use, for a whole workgroup of kRankThreads: bit k of a thread's word is page kRankThreads * k + its index.  One pass of
+// independent loads, and everything below is counted from registers: a pool of up to PIECES * kRankThreads pages.
+template <int PIECES>
+__device__ __forceinline__ uint64_t pages_in_use(const int32_t *__restrict__ refs, int pages)
+{
+    uint64_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int j = k * kRankThreads + (int)threadIdx.x;
+        const int r = refs[j < pages ? j : pages - 1];
+        bits |= (uint64_t)(j < pages && r > 0) << k;
+    }
+    return bits;
+}
+// Those of a thread's pages in use that lie below `end`.
+__device__ __forceinline__ int in_use_below(uint64_t bits, int end)
+{
+    const int k = end / kRankThreads, r = end % kRankThreads;
+    const uint64_t whole = k >= 64 ? bits : bits & ((1ull << k) - 1);
+    return __popcll(whole) + (k < 64 && (int)threadIdx.x < r ? (int)(bits >> k & 1) : 0);
+}
+// A thread's pages in use below `end` in a pool of any size, by a loop.
+__device__ __forceinline__ int in_use_below(const int32_t *__restrict__ refs, int end)
+{
+    int n = 0;
+    for (int j = threadIdx.x; j < end; j += kRankThreads)
+        n += refs[j] > 0;
+    return n;
+}
+
+// PIECES: 1, 4, 16 or 64 (pools of up to 65536 pages), 0: any size.
+template <int PIECES>
 __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookArgs a, const int32_t *__restrict__ new_lengths, ReservePlan plan,
                                                                           int segments, int segment)
 {
-    __shared__ int s[kRankThreads / kWave];
+    __shared__ __align__(8) int s[2 * kRankThreads / kWave];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= segments) {
         const int slot = ((int)blockIdx.x - segments) * kRankThreads + tid;
@@ -249,10 +276,18 @@ __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookAr
         return;
     }
     const int begin = blockIdx.x * segment, end = begin + segment < a.pages ? begin + segment : a.pages;
-    int free_before = begin - live_before<kRankThreads>(a.refs, begin, s);
+    uint64_t bits = 0;
+    int used;
+    if constexpr (PIECES != 0) {
+        bits = pages_in_use<PIECES>(a.refs, a.pages);
+        used = in_use_below(bits, begin);
+    } else {
+        used = in_use_below(a.refs, begin);
+    }
+    int free_before = begin - block_sum<kRankThreads>(used, s);
     for (int j0 = begin; j0 < end; j0 += kRankThreads) {
         const int j = j0 + tid;
-        const bool is_free = j < end && a.refs[j] <= 0;
+        const bool is_free = j < end && (PIECES != 0 ? !(bits >> (j0 / kRankThreads) & 1) : a.refs[j] <= 0);
         int total;
         const int rank = block_before<kRankThreads>(is_free, s, &total);
         if (is_free)
@@ -338,15 +373,27 @@ struct CompactPlan {
     int32_t *count;                   // [0]: moves, [1]: pages in use
 };
 
+template <int PIECES>
 __global__ __launch_bounds__(kRankThreads) void pages_compact_rank_kernel(const int32_t *__restrict__ refs, int pages, CompactPlan plan, int segment,
                                                                           int32_t *__restrict__ live)
 {
-    __shared__ int s[kRankThreads / kWave];
+    __shared__ __align__(8) int s[2 * kRankThreads / kWave];
     const int tid = threadIdx.x;
     const int begin = blockIdx.x * segment, end = begin + segment < pages ? begin + segment : pages;
-    const int n = live_before<kRankThreads>(refs, pages, s);
-    const int below = live_before<kRankThreads>(refs, n, s);
-    int before = live_before<kRankThreads>(refs, begin, s);
+    uint64_t bits = 0;
+    int n, below, before;
+    if constexpr (PIECES != 0) {
+        bits = pages_in_use<PIECES>(refs, pages);
+        const int2 sums = block_sums<kRankThreads>(__popcll(bits), in_use_below(bits, begin), s);
+        n = sums.x;
+        before = sums.y;
+        below = block_sum<kRankThreads>(in_use_below(bits, n), s);
+    } else {
+        const int2 sums = block_sums<kRankThreads>(in_use_below(refs, pages), in_use_below(refs, begin), s);
+        n = sums.x;
+        before = sums.y;
+        below = block_sum<kRankThreads>(in_use_below(refs, n), s);
+    }
     if (blockIdx.x == 0 && tid == 0) {
         plan.count[0] = n - below;
         plan.count[1] = n;
@@ -354,7 +401,7 @@ __global__ __launch_bounds__(kRankThreads) void pages_compact_rank_kernel(const 
     }
     for (int j0 = begin; j0 < end; j0 += kRankThreads) {
         const int j = j0 + tid;
-        const bool used = j < end && refs[j] > 0;
+        const bool used = j < end && (PIECES != 0 ? bits >> (j0 / kRankThreads) & 1 : refs[j] > 0);
         int total;
         const int at = before + block_before<kRankThreads>(used, s, &total);
         before += total;
@@ -558,8 +605,11 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
     int segment;
     const int segments = segments_of(p.pages, &segment);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pages_reserve_rank_kernel, dim3((unsigned)(segments + (S + kRankThreads - 1) / kRankThreads)), dim3(kRankThreads), 0, st, a,
-                       new_lengths, plan, segments, segment);
+    const int pieces = (p.pages + kRankThreads - 1) / kRankThreads;
+    const auto rank = pieces <= 1 ? &pages_reserve_rank_kernel<1> : pieces <= 4 ? &pages_reserve_rank_kernel<4> : pieces <= 16 ? &pages_reserve_rank_kernel<16>
+                    : pieces <= 64 ? &pages_reserve_rank_kernel<64> : &pages_reserve_rank_kernel<0>;
+    hipLaunchKernelGGL(rank, dim3((unsigned)(segments + (S + kRankThreads - 1) / kRankThreads)), dim3(kRankThreads), 0, st, a, new_lengths, plan,
+                       segments, segment);
     if (int rc = check_launch("lookat_pages_reserve (ranks)"))
         return rc;
     hipLaunchKernelGGL(pages_reserve_kernel, dim3((unsigned)S, page_parts(p)), dim3(kBookThreads), 0, st, p, a, new_lengths, plan, missing);
@@ -607,11 +657,14 @@ extern "C" int lookat_pages_compact(const lookat_page_pool *pool, int32_t S, con
     int segment;
     const int segments = segments_of(p.pages, &segment);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(pages_compact_rank_kernel, dim3((unsigned)segments), dim3(kRankThreads), 0, st, refs, p.pages, plan, segment, live);
+    const int pieces = (p.pages + kRankThreads - 1) / kRankThreads;
+    const auto rank = pieces <= 1 ? &pages_compact_rank_kernel<1> : pieces <= 4 ? &pages_compact_rank_kernel<4> : pieces <= 16 ? &pages_compact_rank_kernel<16>
+                    : pieces <= 64 ? &pages_compact_rank_kernel<64> : &pages_compact_rank_kernel<0>;
+    hipLaunchKernelGGL(rank, dim3((unsigned)segments), dim3(kRankThreads), 0, st, refs, p.pages, plan, segment, live);
     if (int rc = check_launch("lookat_pages_compact (ranks)"))
         return rc;
     const int64_t most = ((int64_t)p.pages / 2 + 1) * page_parts(p);     // at most half of the pages move
-    const int move_groups = (int)(most < 2048 ? most : 2048);
+    const int move_groups = (int)(most < 16384 ? most : 16384);
     const int64_t book = ((int64_t)S * W + p.pages + kCopyThreads - 1) / kCopyThreads;
     hipLaunchKernelGGL(pages_compact_kernel, dim3((unsigned)(move_groups + (book < 1024 ? book : 1024))), dim3(kCopyThreads), 0, st, p, a, plan,
                        table_out, table_out_stride, refs_out, page_parts(p), move_groups);
