@@ -40,7 +40,12 @@ struct AttendArgs {
 
 constexpr float kRefLag = 8.f;            // the reference moves when a logit exceeds it by more (log2 units)
 constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, below 2^15: fp16's range, its subnormals far below
-constexpr int kAttendThreads = 512;        // eight wavefronts; 128 registers each: two workgroups to a compute unit
+// Wavefronts of a workgroup: eight of 128 registers, two workgroups to a compute unit.  Four where no sequence is longer than four tiles: the
+// others would only take room from the next workgroups (us, eight / four: 42 x 32 x 157 tokens in groups of 2 15.0 / 10.7, 64 x 32 x 250
+// 14.1 / 11.2, 27 x 32 x 2 in groups of 4 12.3 / 9.9, a few heads the same), unless there are 64 KB of tables to fetch (32 x 8 x 200 in
+// groups of 8, m = 8: 9.2 / 10.9).
+constexpr int kAttendWaves = 8, kShortWaves = 4;
+__host__ __device__ constexpr bool few_waves(int G, int m, int64_t longest) { return G * m < 64 && longest <= kShortWaves * kTile; }
 constexpr int kMostPlanned = 1024;        // sequences whose ranges are cut by their lengths
 
 // Ranges by length.  Sequences of unequal length cut into equally many ranges leave most of the chip waiting for the longest one, and the host
@@ -254,20 +259,21 @@ __device__ __forceinline__ void over_wave(const float (&y)[G], float (&m)[G], Op
 }
 
 // LDS of a workgroup: tables (afterwards the wavefronts' results), then the wavefronts' staged weights (afterwards their references and sums).
-constexpr int kAttendWaves = kAttendThreads / kWave;
-__host__ __device__ constexpr size_t attend_front_bytes(int G, int M, int d_k)
+__host__ __device__ constexpr size_t attend_front_bytes(int G, int M, int d_k, int waves)
 {
-    const size_t tables = (size_t)G * M * kCentroids * 4, results = (size_t)kAttendWaves * G * (d_k + 2) * 4;
+    const size_t tables = (size_t)G * M * kCentroids * 4, results = (size_t)waves * G * (d_k + 2) * 4;
     return tables > results ? tables : results;
 }
-__host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k)
+__host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k, int waves)
 {
-    return attend_front_bytes(G, M, d_k) + (size_t)kAttendWaves * 2 * G * kTile * 2;
+    return attend_front_bytes(G, M, d_k, waves) + (size_t)waves * 2 * G * kTile * 2;
 }
 
-template <int DK, int M, int G, bool FP8>
-__global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArgs p, AttendArgs a)
+template <int DK, int M, int G, bool FP8, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave, 4) void attend_pages_kernel(PoolArgs p, AttendArgs a)
 {
+    constexpr int threads = WAVES * kWave;
+    constexpr size_t front = attend_front_bytes(G, M, DK, WAVES);
     extern __shared__ __align__(16) char lds[];
     constexpr int GP = G < 4 ? G : 4;                     // query heads whose tables are interleaved
     typedef float vg __attribute__((ext_vector_type(GP)));
@@ -337,25 +343,25 @@ __global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArg
     };
 
     int t = k0 + wave * kWave;
-    const int step = kAttendThreads;
+    const int step = threads;
     int id = page_of(t + lane);
     float *tables = reinterpret_cast<float *>(lds);
     // Tables [query head][i][c] -> [plane of GP heads][i][c][head], scaled; a thread takes four entries of GP heads at a time.  The first tile is
     // requested between the tables' loads and their use.
-    constexpr int quads = G / GP * M * (kCentroids / 4), rounds = (quads + kAttendThreads - 1) / kAttendThreads;
-    constexpr int early = rounds * GP <= 8 ? rounds : 8 / GP;
+    constexpr int quads = G / GP * M * (kCentroids / 4), rounds = (quads + threads - 1) / threads;
+    constexpr int early = rounds * GP <= 8 ? rounds : 8 / GP;         // (rounds is a multiple of it: both are powers of two)
     const v4f *lut = reinterpret_cast<const v4f *>(a.lut + (int64_t)unit * G * M * kCentroids);
     v4f x[early][GP];
     auto table_load = [&](int round, int n) {
-        const int j = tid + round * kAttendThreads, at = quads % kAttendThreads && j >= quads ? quads - 1 : j;
+        const int j = tid + round * threads, at = quads % threads && j >= quads ? quads - 1 : j;
         const int plane = at / (M * (kCentroids / 4)), entry = at % (M * (kCentroids / 4));
 #pragma unroll
         for (int g = 0; g < GP; ++g)
             x[n][g] = lut[(plane * GP + g) * (M * (kCentroids / 4)) + entry];
     };
     auto table_store = [&](int round, int n) {
-        const int j = tid + round * kAttendThreads;
-        if (quads % kAttendThreads == 0 || j < quads) {
+        const int j = tid + round * threads;
+        if (quads % threads == 0 || j < quads) {
 #pragma unroll
             for (int k = 0; k < GP; ++k) {                // GP * 4 floats as GP 16-byte stores, ordered entry, head
                 v4f y;
@@ -392,7 +398,7 @@ __global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArg
 
     // staged weights: a row of 64 tokens per column, 128 bytes; its 16-byte pieces are permuted (xor with the row) so that neither side conflicts
     constexpr int staged = 2 * G * kTile * 2;
-    char *weights = lds + attend_front_bytes(G, M, DK) + wave * staged;
+    char *weights = lds + front + wave * staged;
     int w_at = (lane >> 3) << 4 | (lane & 7) << 1;
     auto weight = [&](int row) -> _Float16 & { return *reinterpret_cast<_Float16 *>(weights + row * (kTile * 2) + (w_at ^ ((row & 7) << 4))); };
     v4f acc[2 * CB];
@@ -509,16 +515,16 @@ __global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArg
     }
     __syncthreads();                                      // and every wavefront is done with the tables
     const int mine = col & (G - 1);
-    v2f stat[kAttendWaves];
+    v2f stat[WAVES];
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w)
-        stat[w] = *reinterpret_cast<const v2f *>(lds + attend_front_bytes(G, M, DK) + w * staged + mine * 8);
+    for (int w = 0; w < WAVES; ++w)
+        stat[w] = *reinterpret_cast<const v2f *>(lds + front + w * staged + mine * 8);
     float top = stat[0].x, sum = 0.f, own = lift[0];
 #pragma unroll
-    for (int w = 1; w < kAttendWaves; ++w)
+    for (int w = 1; w < WAVES; ++w)
         top = fmaxf(top, stat[w].x);
 #pragma unroll
-    for (int w = 0; w < kAttendWaves; ++w)
+    for (int w = 0; w < WAVES; ++w)
         sum = fmaf(fast_exp2(stat[w].x - top), stat[w].y, sum);
 #pragma unroll
     for (int g = 1; g < G; ++g)
@@ -544,11 +550,11 @@ __global__ __launch_bounds__(kAttendThreads, 4) void attend_pages_kernel(PoolArg
     float *to = r.splits == 1 ? a.out + (int64_t)unit * G * DK : a.part + (int64_t)r.index * G * (DK + 2);
     const int row_to = r.splits == 1 ? DK : DK + 2;
 #pragma unroll
-    for (int j = tid; j < G * DK / 2; j += kAttendThreads) {
+    for (int j = tid; j < G * DK / 2; j += threads) {
         const int g = j / (DK / 2), d = j % (DK / 2) * 2;
         v2f o = {0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w)
+        for (int w = 0; w < WAVES; ++w)
             o += *reinterpret_cast<const v2f *>(results + (w * G + g) * (DK + 2) + d);
         *reinterpret_cast<v2f *>(to + g * row_to + d) = o;
     }
@@ -615,25 +621,36 @@ __global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, i
 // So 1024, and 2048 where those still have 4096 tokens.  Least range of 512 / 1024 / 2048 tokens (1024 ranges): 2 heads in groups of 8 x 3000
 // 10.3 / 11.6 / 13.6; 1 x 32 x 8192 13.5 / 13.4 / 15.5; 8 x 32 x up to 1500 16.7 / 14.8 / 14.0; 64 KB of tables (groups of 8, m = 8), which every
 // range fetches: 12 x 8 x up to 8191 25.3 / 21.1 / 20.3, 64 x 4 x up to 2048 27.6 / 23.0 / 21.9.  So 1024, and 2048 from 64 KB on.
-static int least_range(int G, int m) { return G * m >= 64 ? 2048 : 1024; }
+// Sequences of up to 2048 tokens are not cut at all: the merge is a launch more (8 x 32 x up to 1500 14.0 whole, 14.8 cut).  Where 1024 tokens a
+// range would make fewer than 128 ranges, 512.
+constexpr int kWholeLength = 2048;
+static int least_range(int G, int m, int64_t units, int64_t room)
+{
+    return G * m >= 64 ? 2048 : units * room < 128 * 1024 ? 512 : 1024;
+}
 
 // How a call is cut up.
 struct Cut {
     int per_head;     // ranges by length: ranges per head, or 0
+    int least;        // ... of at least so many tokens
     int splits;       // equal ranges
     int64_t groups;   // workgroups
     int64_t ranges;   // ranges whose results the workspace holds (0: none)
 };
-static Cut cut_of(const lookat_page_pool *p, int32_t B, int32_t G, int64_t longest, int32_t num_splits)
+static Cut cut_of(const lookat_page_pool *p, int32_t B, int32_t G, int32_t W, int64_t longest, int32_t num_splits)
 {
     const int64_t units = (int64_t)B * p->H;
     Cut c;
-    c.per_head = 0;
+    c.per_head = c.least = 0;
     c.splits = num_splits ? num_splits : 1;
-    if (num_splits == 0 && longest > least_range(G, p->m) && B <= kMostPlanned) {
+    if (num_splits == 0 && longest > kWholeLength && B <= kMostPlanned) {
+        // (from the rows' room where the number of ranges has to hold them all: a sequence may be longer than the caller knows)
+        const int64_t room = (int64_t)W * p->page;
         const int64_t target = units * longest >= 2048LL * 4096 ? 2048 : 1024;
         c.per_head = (int)((target + p->H - 1) / p->H);
-        c.ranges = (int64_t)p->H * (c.per_head + 1 + B);
+        c.least = least_range(G, p->m, units, longest);
+        const int64_t fit = (int64_t)B * ((room + c.least - 1) / c.least), most = c.per_head + 1 + B;
+        c.ranges = p->H * (fit < most ? fit : most);
         c.groups = (c.ranges + kXcds - 1) / kXcds * kXcds;
         return c;
     }
@@ -671,40 +688,39 @@ static int64_t longest_of(const lookat_page_pool *pool, int32_t W, int64_t max_l
 }
 
 template <int DK, int M, int G>
-static int launch_attend(const PoolArgs &p, const AttendArgs &a, bool fp8, dim3 grid, hipStream_t st)
+static int launch_attend(const PoolArgs &p, const AttendArgs &a, bool fp8, bool brief, dim3 grid, hipStream_t st)
 {
-    const size_t lds = attend_lds_bytes(G, M, DK);
-    const void *f = fp8 ? reinterpret_cast<const void *>(&attend_pages_kernel<DK, M, G, true>)
-                        : reinterpret_cast<const void *>(&attend_pages_kernel<DK, M, G, false>);
+    constexpr int brief_waves = few_waves(G, M, 0) ? kShortWaves : kAttendWaves;
+    const int waves = brief ? brief_waves : kAttendWaves;
+    const size_t lds = attend_lds_bytes(G, M, DK, waves);
+    const auto f = brief ? (fp8 ? &attend_pages_kernel<DK, M, G, true, brief_waves> : &attend_pages_kernel<DK, M, G, false, brief_waves>)
+                         : (fp8 ? &attend_pages_kernel<DK, M, G, true, kAttendWaves> : &attend_pages_kernel<DK, M, G, false, kAttendWaves>);
     if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
             return fail(LOOKAT_ERR_HIP, "lookat_attend_pages: %s", hipGetErrorString(e));
     }
-    if (fp8)
-        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, true>), grid, dim3(kAttendThreads), lds, st, p, a);
-    else
-        hipLaunchKernelGGL((attend_pages_kernel<DK, M, G, false>), grid, dim3(kAttendThreads), lds, st, p, a);
+    hipLaunchKernelGGL(f, grid, dim3(waves * kWave), lds, st, p, a);
     return check_launch("lookat_attend_pages");
 }
 template <int DK, int M>
-static int launch_attend_g(int G, const PoolArgs &p, const AttendArgs &a, bool fp8, dim3 grid, hipStream_t st)
+static int launch_attend_g(int G, const PoolArgs &p, const AttendArgs &a, bool fp8, bool brief, dim3 grid, hipStream_t st)
 {
     switch (G) {
-    case 1: return launch_attend<DK, M, 1>(p, a, fp8, grid, st);
-    case 2: return launch_attend<DK, M, 2>(p, a, fp8, grid, st);
-    case 4: return launch_attend<DK, M, 4>(p, a, fp8, grid, st);
-    default: return launch_attend<DK, M, 8>(p, a, fp8, grid, st);
+    case 1: return launch_attend<DK, M, 1>(p, a, fp8, brief, grid, st);
+    case 2: return launch_attend<DK, M, 2>(p, a, fp8, brief, grid, st);
+    case 4: return launch_attend<DK, M, 4>(p, a, fp8, brief, grid, st);
+    default: return launch_attend<DK, M, 8>(p, a, fp8, brief, grid, st);
     }
 }
 template <int DK>
-static int launch_attend_m(int G, const PoolArgs &p, const AttendArgs &a, bool fp8, dim3 grid, hipStream_t st)
+static int launch_attend_m(int G, const PoolArgs &p, const AttendArgs &a, bool fp8, bool brief, dim3 grid, hipStream_t st)
 {
     switch (p.m) {
-    case 2: return launch_attend_g<DK, 2>(G, p, a, fp8, grid, st);
-    case 4: return launch_attend_g<DK, 4>(G, p, a, fp8, grid, st);
-    case 8: return launch_attend_g<DK, 8>(G, p, a, fp8, grid, st);
-    default: return launch_attend_g<DK, 16>(G, p, a, fp8, grid, st);
+    case 2: return launch_attend_g<DK, 2>(G, p, a, fp8, brief, grid, st);
+    case 4: return launch_attend_g<DK, 4>(G, p, a, fp8, brief, grid, st);
+    case 8: return launch_attend_g<DK, 8>(G, p, a, fp8, brief, grid, st);
+    default: return launch_attend_g<DK, 16>(G, p, a, fp8, brief, grid, st);
     }
 }
 
@@ -717,7 +733,7 @@ extern "C" size_t lookat_attend_pages_workspace_bytes(const lookat_page_pool *po
     clear_error();
     if (check_attend(pool, B, group, W, max_length, num_splits) != LOOKAT_OK)
         return 0;
-    return cut_bytes(pool, B, group, cut_of(pool, B, group, longest_of(pool, W, max_length), num_splits));
+    return cut_bytes(pool, B, group, cut_of(pool, B, group, W, longest_of(pool, W, max_length), num_splits));
 }
 
 extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int32_t group, const float *lut, const int32_t *table, int32_t W,
@@ -737,7 +753,7 @@ extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int3
     if (reinterpret_cast<uintptr_t>(lengths) & 3u)
         return fail(LOOKAT_ERR_ALIGN, "lengths must be 4-byte aligned");
     const int64_t longest = longest_of(pool, W, max_length);
-    const Cut cut = cut_of(pool, B, group, longest, num_splits);
+    const Cut cut = cut_of(pool, B, group, W, longest, num_splits);
     const size_t need = cut_bytes(pool, B, group, cut);
     if (need) {
         if (!workspace || workspace_bytes < need)
@@ -762,14 +778,15 @@ extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int3
     a.B = B;
     a.units = (int32_t)units;
     a.per_head = cut.per_head;
-    a.least = least_range(group, p.m);
+    a.least = cut.least;
     a.splits = cut.splits;
     a.chunk = (int32_t)(((longest + cut.splits - 1) / cut.splits + kTile - 1) / kTile * kTile);
     a.scale_log2e = scale * kLog2e;
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)cut.groups);
-    const int rc = p.d_k == 64 ? launch_attend_m<64>(group, p, a, fp8, grid, st) : launch_attend_m<128>(group, p, a, fp8, grid, st);
+    const bool brief = cut.splits == 1 && cut.per_head == 0 && few_waves(group, p.m, longest);
+    const int rc = p.d_k == 64 ? launch_attend_m<64>(group, p, a, fp8, brief, grid, st) : launch_attend_m<128>(group, p, a, fp8, brief, grid, st);
     if (rc != LOOKAT_OK || !need)
         return rc;
     hipLaunchKernelGGL(attend_pages_merge_kernel, dim3((unsigned)units, group), dim3(p.d_k), 0, st, a, pool->H, group, p.d_k, p.page_log2);

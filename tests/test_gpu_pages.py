@@ -197,6 +197,20 @@ def test_attend(lk, d_k, m, page, group, kind):
 
 
 @pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group", [1, 2, 4, 8])
+@pytest.mark.parametrize("d_k,m,page", [(64, 2, 16), (64, 16, 64), (128, 4, 128), (128, 16, 32)])
+def test_attend_short(lk, d_k, m, page, group, kind):
+    """Rows of four tiles at most (workgroups of four wavefronts), and a host that takes longer ones for such."""
+    rng = np.random.default_rng(d_k + m + page + group)
+    lengths = [1, 0, 64, 65, 128, 127, 3, 100]
+    c = random_cache(rng, 64, 3, d_k, m, page, kind)
+    for kw in ({"W": 128 // page}, {"W": 128 // page, "num_splits": 1}, {"W": 128 // page, "num_splits": 2}):
+        assert_attend(attend_case(lk, rng, c, lengths, group, 3.0, **kw), f"short rows, {kind}")
+    assert_attend(attend_case(lk, rng, c, [256, 255, 193, 1], group, 3.0, W=256 // page), f"short rows, {kind}")
+    assert_attend(attend_case(lk, rng, c, [333, 5, 190], group, 3.0, max_length=256), f"short rows, {kind}")
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
 def test_attend_long(lk, kind):
     """Long rows in many ranges, short ones beside them, a table wider than any sequence and a host that knows less than is there."""
     rng = np.random.default_rng(11)
@@ -502,11 +516,12 @@ def test_a_search_over_continuations(lk, kind):
         same_books((table, lengths, refs), b)
 
 
-def test_a_captured_decode_step(lk):
+@pytest.mark.parametrize("group,d_k,m,splits", [(4, 128, 8, 2), (8, 128, 8, 0), (1, 64, 4, 0)])
+def test_a_captured_decode_step(lk, group, d_k, m, splits):
     """Reserve, encode, write, tables, attention and compaction's ranking of books captured once, replayed for many tokens, each
     replay against the same calls made eagerly on a second cache; eager work between the replays."""
     rng = np.random.default_rng(31)
-    B, H, group, d_k, m, page, W = 3, 2, 4, 128, 8, 16, 6
+    B, H, page, W = 3, 2, 16, 6 if splits else 140          # (140 pages: 2240 tokens, cut by length)
     P = B * W
     books = dev((rng.standard_normal((H, m, 256, d_k // m)) * 2).astype(np.float32))
     scale = 1 / math.sqrt(d_k)
@@ -526,7 +541,7 @@ def test_a_captured_decode_step(lk):
             codes = lk.lookat_encode_keys(self.k, books)
             lk.lookat_pages_write(self.pool, codes, self.v, self.table, self.lengths, one)
             lut = lk.lookat_build_lut(self.q, books).view(B, H * group, m, 256)
-            lk.lookat_attend_pages(lut, self.pool, self.table, self.lengths, scale, num_splits=2, out=self.out)
+            lk.lookat_attend_pages(lut, self.pool, self.table, self.lengths, scale, num_splits=splits, out=self.out)
             self.compacted = lk.lookat_pages_compact(self.pool, self.table, self.lengths, self.refs)
 
         def state(self):
