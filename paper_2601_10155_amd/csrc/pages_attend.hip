@@ -7,7 +7,16 @@
 // So the stored integers enter the product as they are (exact in fp16), the weights are as precise as the largest contribution to the result
 // needs whatever the pages' exponents are, and no per-page rescaling is done.
 //
-// Bound: the stream of codes and values from HBM, m + d_k bytes per token and key/value head.
+// Bound: the stream of codes and values from HBM, m + d_k bytes per token and key/value head, where there is much of it: 8 x 32 x 32768
+// tokens (d_k = 128, m = 8, int8; 1.14 GB, fetched once) take 166 us in the kernel, 6.9 TB/s (a plain read of 1 GiB: 7.0 to 7.1), 169 a call.
+// Below some 50 MB the chain of dependent steps counts instead: lengths, page id, codes and values, reduction, merge.  12 x 1024 tokens
+// (0.8 MB) 5.1 us in the kernel: 0.4 until the range is known, 0.3 until the first tile is requested, 1.5 until it is weighted, 1.2 for the
+// results.  12 x 8 x up to 8191 in groups of 8 (52 MB) 16.8 us and 3.8 for the merge: eight query heads are 270 vector instructions a tile.
+//
+// Weighted sums on the matrix cores at every group, also for one query head: 1 + 1/2 vector instructions a stored value (int8; 1/2 in e4m3)
+// instead of 2.  What was tried and not kept: four or sixteen wavefronts to a workgroup (long contexts 178.9 / 179.8 us, eight 177.4, groups of 8
+// 30.6 / 41.0, eight 27.7, at an earlier stage), a second tile in registers at d_k = 64 (16 x 12 x 4096 14.8 -> 17.1 us: fewer wavefronts fit),
+// ranges of whole steps of eight tiles (no change), a product with integer weights (the tables' scores need 22 bits).
 //
 // One workgroup = one (sequence, key/value head, range); its wavefronts take the range's 64-token tiles in turn.  In a tile
 //   * scoring: a lane per token: its page from the table, its codes (one load), m look-ups per query head in the head's table in LDS.  The
