@@ -13,6 +13,9 @@
  * page table[t / page] at t % page.  Rows are W entries long, table_stride apart; a sequence's tokens behind W * page, and
  * those in pages whose id is outside [0, pages), are neither read nor written (attention passes over them).  A length
  * below zero counts as zero.  `refs` counts, for every page, the sequences that hold it; 0 is a free page.
+ * A model keeps a pool for each layer and one set of books (table, lengths, refs) for all of them: lookat_pages_reserve copies shared pages in
+ * the pool it is given and says which, for lookat_pages_copy on the others; lookat_pages_compact, which leaves the books that it reads as they
+ * are, is called for each pool; fork and free touch the books alone.
  *
  * Exponents lie in [-40, 40]: values up to 1.4e14 (I8) or 4.9e14 (E4M3) are kept, and below 2^-41 (I8) or 2^-50 (E4M3) nothing but
  * zero.  Scales are powers of two on purpose: the division v / 2^e and the widening q * 2^e are exact, so a value is rounded
@@ -134,12 +137,14 @@ int lookat_pages_free(const lookat_page_pool *pool, int32_t S, int32_t *table, i
  * missing[0] says by how many pages, else missing[0] = 0.
  * (Of several sequences that share a last page and all grow, all get a copy; the page itself becomes free.)
  *   new_lengths  [S] int32, must not overlap lengths;  missing  [1] int32
+ *   copies       NULL, or [2, S] int32: copies[0,s] the page that was copied for sequence s and copies[1,s] the one it was copied to, -1
+ *                where none was: what lookat_pages_copy takes to do the same in the pools of other layers that share these books
  *   workspace    lookat_pages_reserve_workspace_bytes(pool, S) bytes, 16-byte aligned
  */
 size_t lookat_pages_reserve_workspace_bytes(const lookat_page_pool *pool, int32_t S);
 
 int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int32_t *table, int32_t W, int64_t table_stride,
-                         int32_t *lengths, int32_t *refs, const int32_t *new_lengths, int32_t *missing,
+                         int32_t *lengths, int32_t *refs, const int32_t *new_lengths, int32_t *missing, int32_t *copies,
                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*

@@ -124,7 +124,7 @@ def load_library():
         lib.lookat_pages_free.restype = ctypes.c_int
         lib.lookat_pages_reserve_workspace_bytes.argtypes = [pp, i32]
         lib.lookat_pages_reserve_workspace_bytes.restype = sz
-        lib.lookat_pages_reserve.argtypes = [pp, i32, vp, i32, i64, vp, vp, vp, vp, vp, sz, vp]
+        lib.lookat_pages_reserve.argtypes = [pp, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lookat_pages_reserve.restype = ctypes.c_int
         lib.lookat_pages_compact_workspace_bytes.argtypes = [pp]
         lib.lookat_pages_compact_workspace_bytes.restype = sz
@@ -846,10 +846,13 @@ def lookat_pages_free(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor
 
 
 def lookat_pages_reserve(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, new_lengths: torch.Tensor,
-                         missing: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+                         missing: torch.Tensor | None = None, copies: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Room for the sequences to grow to new_lengths [S] int32 (not above lengths: as it is): free pages in ascending order, shared last
-    pages copied, lengths set.  Returns `missing` [1] int32: 0, or how many pages are lacking and nothing was changed."""
-    rc = _native().pages_reserve(pool, table, lengths, refs, new_lengths, missing, workspace)
+    pages copied, lengths set.  Returns `missing` [1] int32: 0, or how many pages are lacking and nothing was changed.
+    `copies` [2,S] int32, if given, gets the pages that were copied and their copies (-1: none), for lookat_pages_copy(pool, *copies) on the
+    pools of other layers that share these books."""
+    rc = _native().pages_reserve(pool, table, lengths, refs, new_lengths, missing, copies, workspace)
     if rc is not None:
         if missing is None and rc.__class__ is not int:
             return rc                # allocated there
@@ -863,9 +866,12 @@ def lookat_pages_reserve(pool: PagePool, table: torch.Tensor, lengths: torch.Ten
     if missing is None:
         missing = torch.empty(1, dtype=torch.int32, device=pool.codes.device)
     m_ptr = _int_array(missing, "missing", pool, 1)
+    if copies is not None and (copies.dtype != torch.int32 or tuple(copies.shape) != (2, books[0]) or not copies.is_contiguous()
+                               or copies.device != pool.codes.device):
+        raise ValueError("copies must be a contiguous int32 [2,S] tensor on the pool's device")
     with _OnDevice(pool) as stream:
         workspace = _scratch(workspace, lib.lookat_pages_reserve_workspace_bytes(ctypes.byref(c_pool), books[0]), pool)
-        _check(lib.lookat_pages_reserve(ctypes.byref(c_pool), *books, ptr, m_ptr, _ptr(workspace), _bytes(workspace), stream))
+        _check(lib.lookat_pages_reserve(ctypes.byref(c_pool), *books, ptr, m_ptr, _ptr(copies), _ptr(workspace), _bytes(workspace), stream))
     return missing
 
 

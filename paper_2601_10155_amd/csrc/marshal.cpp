@@ -550,25 +550,32 @@ PyObject *pages_free(PyObject *const *args, Py_ssize_t n)
     return status(rc);
 }
 
-// pool, table, lengths, refs, new_lengths, missing | None, workspace | None
+// pool, table, lengths, refs, new_lengths, missing | None, copies | None, workspace | None
 PyObject *pages_reserve(PyObject *const *args, Py_ssize_t n)
 {
     Books b;
-    if (n != 7 || !books_of(args, b))
+    if (n != 8 || !books_of(args, b))
         GIVE_UP;
     const int32_t *wanted = ints(args[4], b.p, b.t.rows);
     int32_t *missing = args[5] == Py_None ? nullptr : ints(args[5], b.p, 1);
     at::Tensor own, made;
     void *ws, *stream;
     size_t bytes;
+    int32_t *copies = nullptr;
+    if (args[6] != Py_None) {
+        const at::Tensor *c = dense(args[6], at::kInt);
+        if (!c || c->dim() != 2 || c->size(0) != 2 || c->size(1) != b.t.rows || !beside(b.p, *c))
+            GIVE_UP;
+        copies = static_cast<int32_t *>(c->data_ptr());
+    }
     if (!wanted || (args[5] != Py_None && !missing) ||
-        !scratch_of(args[6], pages.reserve_workspace_bytes(&b.p.c, b.t.rows), b.p, own, ws, bytes) || !current_stream(*b.p.codes, stream))
+        !scratch_of(args[7], pages.reserve_workspace_bytes(&b.p.c, b.t.rows), b.p, own, ws, bytes) || !current_stream(*b.p.codes, stream))
         GIVE_UP;
     if (!missing) {
         made = at::empty({1}, b.p.codes->options().dtype(at::kInt));
         missing = static_cast<int32_t *>(made.data_ptr());
     }
-    CALL(rc, pages.reserve(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, wanted, missing, ws, bytes, stream));
+    CALL(rc, pages.reserve(&b.p.c, b.t.rows, b.t.ptr, b.t.W, b.t.stride, b.lengths, b.refs, wanted, missing, copies, ws, bytes, stream));
     return rc == LOOKAT_OK && made.defined() ? THPVariable_Wrap(std::move(made)) : status(rc);
 }
 

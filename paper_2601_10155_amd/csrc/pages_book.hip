@@ -211,6 +211,7 @@ struct ReservePlan {
     int32_t *need;       // [S] pages
     int32_t *shared;     // [S] the page to copy, or -1
     int32_t *count;      // [0]: free pages
+    int32_t *copies;     // [2][S] for the caller, or NULL
 };
 
 constexpr int kRankThreads = 1024;
@@ -274,6 +275,10 @@ __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookAr
         }
         plan.need[slot] = need;
         plan.shared[slot] = shared;
+        if (plan.copies) {
+            plan.copies[slot] = -1;
+            plan.copies[a.S + slot] = -1;
+        }
         return;
     }
     const int begin = blockIdx.x * segment, end = begin + segment < a.pages ? begin + segment : a.pages;
@@ -360,8 +365,13 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(PoolArgs p,
     }
     if (tid == 0) {
         a.lengths[slot] = wanted;
-        if (shared >= 0)
+        if (shared >= 0) {
             atomicSub(a.refs + shared, 1);
+            if (plan.copies) {
+                plan.copies[slot] = shared;
+                plan.copies[a.S + slot] = plan.free_ids[before];
+            }
+        }
     }
 }
 
@@ -581,8 +591,8 @@ extern "C" size_t lookat_pages_reserve_workspace_bytes(const lookat_page_pool *p
 }
 
 extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int32_t *table, int32_t W, int64_t table_stride, int32_t *lengths,
-                                    int32_t *refs, const int32_t *new_lengths, int32_t *missing, void *workspace, size_t workspace_bytes,
-                                    void *stream)
+                                    int32_t *refs, const int32_t *new_lengths, int32_t *missing, int32_t *copies, void *workspace,
+                                    size_t workspace_bytes, void *stream)
 {
     using namespace lookat;
     clear_error();
@@ -590,8 +600,8 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
         return rc;
     if (!new_lengths || !missing)
         return fail(LOOKAT_ERR_NULL, "new_lengths and missing must be non-NULL");
-    if ((reinterpret_cast<uintptr_t>(new_lengths) | reinterpret_cast<uintptr_t>(missing)) & 3u)
-        return fail(LOOKAT_ERR_ALIGN, "new_lengths and missing must be 4-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(new_lengths) | reinterpret_cast<uintptr_t>(missing) | reinterpret_cast<uintptr_t>(copies)) & 3u)
+        return fail(LOOKAT_ERR_ALIGN, "new_lengths, missing and copies must be 4-byte aligned");
     if (new_lengths < lengths + S && lengths < new_lengths + S)
         return fail(LOOKAT_ERR_SHAPE, "new_lengths and lengths must not overlap");
     if (int rc = check_workspace(lookat_pages_reserve_workspace_bytes(pool, S), workspace, workspace_bytes))
@@ -603,6 +613,7 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
     plan.need = plan.count + 4;
     plan.shared = plan.need + S;
     plan.free_ids = plan.shared + S;
+    plan.copies = copies;
     int segment;
     const int segments = segments_of(p.pages, &segment);
     hipStream_t st = static_cast<hipStream_t>(stream);

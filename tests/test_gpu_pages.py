@@ -375,7 +375,7 @@ def test_books(lk, S, W, P, page):
     wide = torch.full((S, W + 3), -9, dtype=torch.int32, device="cuda")
     wide[:, 1: 1 + W] = dev(b.table)
     table, lengths, refs = wide[:, 1: 1 + W], dev(b.lengths), dev(b.refs)
-    short = 0
+    other = on_gpu(lk, c)
     for turn in range(8):
         n = int(rng.integers(1, S + 1))
         slots = rng.integers(-1, S + 1, n).astype(np.int32)               # repeated ones and ones that do not exist among them
@@ -388,9 +388,16 @@ def test_books(lk, S, W, P, page):
         same_books((table, lengths, refs), b)
         more = rng.integers(-3, page + 2, S) if turn % 3 else rng.integers(0, W * page, S) * (rng.random(S) < 0.2)
         wanted = np.minimum(b.lengths + more, W * page + (turn == 5)).astype(np.int32)
-        missing = lk.lookat_pages_reserve(pool, table, lengths, refs, dev(wanted))
+        copies = torch.full((2, S), -5, dtype=torch.int32, device="cuda")
+        missing = lk.lookat_pages_reserve(pool, table, lengths, refs, dev(wanted), copies=copies)
+        lk.lookat_pages_copy(other, *copies)                              # a second layer's pool with the same books
+        before = b.table.copy()
         expected = b.reserve(wanted, c)
-        short += expected > 0
+        moved = [(s, before[s, w], b.table[s, w]) for s, w in np.argwhere((before != b.table) & (before >= 0)).tolist() if b.lengths[s] > 0]
+        pairs = np.full((2, S), -1)
+        for s, old, new in moved:
+            pairs[:, s] = old, new
+        assert np.array_equal(copies.cpu().numpy(), pairs)
         assert int(missing) == expected
         same_books((table, lengths, refs), b)
         assert_pool(pool, c)
@@ -400,6 +407,9 @@ def test_books(lk, S, W, P, page):
             same_books((table, lengths, refs), b)                         # the old ones stay
             assert int(live) == n and np.array_equal(new_refs.cpu().numpy(), r) and np.array_equal(new_table.cpu().numpy(), t)
             assert_pool(pool, c)
+            again = lk.lookat_pages_compact(other, table, lengths, refs)
+            assert all(torch.equal(x, y) for x, y in zip(again, (new_table, new_refs, live)))
+            assert_pool(other, c)
             b.table, b.refs = t, r
             table.copy_(new_table), refs.copy_(new_refs)
     assert torch.all(wide[:, 0] == -9) and torch.all(wide[:, 1 + W:] == -9)
@@ -606,7 +616,7 @@ def test_native_and_python_marshalling_agree(lk, monkeypatch):
         missing = lk.lookat_pages_reserve(pool, table, n, refs, n + 9)
         given = torch.full((1,), 7, dtype=torch.int32, device="cuda")
         ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
-        assert lk.lookat_pages_reserve(pool, table, n, refs, n.clone(), given, ws) is given
+        assert lk.lookat_pages_reserve(pool, table, n, refs, n.clone(), given, workspace=ws) is given
         codes = dev(rng.integers(0, 256, (5, 3, 12, 4), dtype=np.uint8))[:, :, 2:11]
         for dtype in (np.float16, np.float32):
             values = dev(rng.standard_normal((5, 3, 9, 64)).astype(dtype))

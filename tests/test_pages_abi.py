@@ -45,7 +45,7 @@ def calls(lib):
         "copy": entry(lib.lookat_pages_copy, ("n", "src", "dst", "stream"), (4, FAKE, FAKE, None)),
         "fork": entry(lib.lookat_pages_fork, books + ("n", "src", "dst", "stream"), good + (2, FAKE, FAKE, None)),
         "free": entry(lib.lookat_pages_free, books + ("n", "slots", "stream"), good + (2, FAKE, None)),
-        "reserve": entry(lib.lookat_pages_reserve, books + ("new", "missing", "ws", "wsb", "stream"), good + (FAKE + 64, FAKE, FAKE, big, None)),
+        "reserve": entry(lib.lookat_pages_reserve, books + ("new", "missing", "copies", "ws", "wsb", "stream"), good + (FAKE + 64, FAKE, None, FAKE, big, None)),
         "compact": entry(lib.lookat_pages_compact, ("S", "table", "W", "stride", "lengths", "refs", "table_out", "out_stride", "refs_out", "live", "ws", "wsb", "stream"),
                          good + (FAKE + 4096, 7, FAKE + 4096, FAKE, FAKE, big, None)),
     }
@@ -119,7 +119,7 @@ def test_upkeep_refusals(lib):  # noqa: F811
         assert c[name](pool(), **{key: FAKE + 1}) == E_ALIGN
     assert c["copy"](pool(H=4096, page=128, d_k=128, m=16), n=1 << 30) == E_UNSUP
     r = c["reserve"]
-    assert r(pool(), new=None) == E_NULL and r(pool(), missing=None) == E_NULL
+    assert r(pool(), new=None) == E_NULL and r(pool(), missing=None) == E_NULL and r(pool(), copies=FAKE + 2) == E_ALIGN
     assert r(pool(), new=FAKE) == E_SHAPE and r(pool(), new=FAKE + 16) == E_SHAPE and r(pool(), new=FAKE - 4) == E_SHAPE      # over lengths
     need = lib.lookat_pages_reserve_workspace_bytes(ctypes.byref(pool()), 5)
     assert need > 0 and r(pool(), wsb=need - 1) == E_WS and r(pool(), ws=None) == E_WS and r(pool(), ws=FAKE + 4) == E_ALIGN
