@@ -48,6 +48,7 @@ struct AttendArgs {
 };
 
 constexpr float kRefLag = 8.f;            // the reference moves when a logit exceeds it by more (log2 units)
+constexpr float kNoReference = -3e38f;    // before the first token; below every logit, and finite: -inf less it is -inf
 constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, below 2^15: fp16's range, its subnormals far below
 // Wavefronts of a workgroup: eight of 128 registers, two workgroups to a compute unit.  Four where no sequence is longer than four tiles: the
 // others would only take room from the next workgroups (us, eight / four: 42 x 32 x 157 tokens in groups of 2 15.0 / 10.7, 64 x 32 x 250
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void attend_pages_kernel(PoolArgs 
     float lift[G], z[G];                                  // the reference less kRefLift (one value for the wavefront), the sum
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        lift[g] = -1e30f;
+        lift[g] = kNoReference;
         z[g] = 0.f;
     }
 
@@ -573,7 +574,7 @@ __global__ __launch_bounds__(WAVES *kWave, 4) void attend_pages_kernel(PoolArgs 
         *reinterpret_cast<v2f *>(to + tid * row_to + DK) = (v2f){top, sum};
 }
 
-// Merges the ranges of one (sequence, key/value head): a thread per query head and coordinate, the ranges' loads issued eight at a time.
+// Merges the ranges of one (sequence, query head): a thread per coordinate, the ranges' loads issued eight at a time.
 __global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, int H, int G, int d_k, int page_log2)
 {
     constexpr int GR = 8;
@@ -591,37 +592,34 @@ __global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, i
         n = n < 1 ? 1 : n > a.splits ? a.splits : n;
         first = (int64_t)unit * a.splits;
     }
-    const int row = d_k + 2;
-    {
-        const int g = blockIdx.y, d = threadIdx.x;
-        const float *x = a.part + (first * G + g) * row;
-        float top = -1e30f, o = 0.f, z = 0.f;
-        for (int s0 = 0; s0 < n; s0 += GR) {
-            float m_[GR], z_[GR], o_[GR];
+    const int row = d_k + 2, g = blockIdx.y, d = threadIdx.x;
+    const float *x = a.part + (first * G + g) * row;
+    float top = kNoReference, o = 0.f, z = 0.f;
+    for (int s0 = 0; s0 < n; s0 += GR) {
+        float m_[GR], z_[GR], o_[GR];
 #pragma unroll
-            for (int k = 0; k < GR; ++k) {
-                const float *y = x + (int64_t)(s0 + k < n ? s0 + k : s0) * G * row;
-                m_[k] = y[d_k];
-                z_[k] = y[d_k + 1];
-                o_[k] = y[d];
-            }
-            float to = top;
-#pragma unroll
-            for (int k = 0; k < GR; ++k)
-                to = fmaxf(to, m_[k]);
-            const float fix = fast_exp2(top - to);
-            o *= fix;
-            z *= fix;
-#pragma unroll
-            for (int k = 0; k < GR; ++k) {
-                const float f = s0 + k < n ? fast_exp2(m_[k] - to) : 0.f;
-                o = fmaf(f, o_[k], o);
-                z = fmaf(f, z_[k], z);
-            }
-            top = to;
+        for (int k = 0; k < GR; ++k) {
+            const float *y = x + (int64_t)(s0 + k < n ? s0 + k : s0) * G * row;
+            m_[k] = y[d_k];
+            z_[k] = y[d_k + 1];
+            o_[k] = y[d];
         }
-        a.out[((int64_t)unit * G + g) * d_k + d] = z > 0.f ? o / z : 0.f;
+        float to = top;
+#pragma unroll
+        for (int k = 0; k < GR; ++k)
+            to = fmaxf(to, m_[k]);
+        const float fix = fast_exp2(top - to);
+        o *= fix;
+        z *= fix;
+#pragma unroll
+        for (int k = 0; k < GR; ++k) {
+            const float f = s0 + k < n ? fast_exp2(m_[k] - to) : 0.f;
+            o = fmaf(f, o_[k], o);
+            z = fmaf(f, z_[k], z);
+        }
+        top = to;
     }
+    a.out[((int64_t)unit * G + g) * d_k + d] = z > 0.f ? o / z : 0.f;
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------

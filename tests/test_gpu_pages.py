@@ -244,6 +244,16 @@ def test_attend_peaked_and_flat(lk, kind):
     for sharp in (0.0, 1e-3, 40.0, 400.0):
         c = random_cache(rng, 30, 2, 64, 4, 64, kind)
         assert_attend(attend_case(lk, rng, c, [700, 900], 2, sharp), f"peaked, {kind}")
+    # equal logits, low or high, up to the ends of fp32 (where no weights are left to tell apart, but numbers)
+    c = random_cache(rng, 40, 1, 64, 4, 16, kind)
+    table = np.arange(40, dtype=np.int32)[None]
+    for level in (-1e3, 1e3, -1e31, 1e31, -3e37, 3e37):
+        lut = np.full((1, 1, 4, 256), level, np.float32)
+        for splits in (1, 3):
+            out = lk.lookat_attend_pages(dev(lut), on_gpu(lk, c), dev(table), i32(600), 0.125, num_splits=splits).cpu().numpy()
+            if abs(level) < 1e4:
+                assert_attend((out, *c.attend(lut, table, [600], 0.125)), f"equal logits, {kind}")
+            assert np.isfinite(out).all() and np.abs(out).max() > 0
     # a table whose entries grow with the code, and codes that grow along the row
     c = random_cache(rng, 16, 1, 64, 2, 64, kind)
     table = np.arange(16, dtype=np.int32)[None]
