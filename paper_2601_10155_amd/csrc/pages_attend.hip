@@ -56,6 +56,9 @@ constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, b
 // groups of 8, m = 8: 9.2 / 10.9).
 constexpr int kAttendWaves = 8, kShortWaves = 4;
 __host__ __device__ constexpr bool few_waves(int G, int m, int64_t longest) { return G * m < 64 && longest <= kShortWaves * kTile; }
+// Wavefronts to a SIMD that the registers have to allow: six (80 registers) where they do without spilling; us, four / six: d_k = 64, groups of 2
+// x 32 x 6 x 4096, m = 8 18.3 / 17.0, 16 x 12 x 4096, m = 16 e4m3 18.9 / 17.0, m = 4 14.9 / 14.9; groups of 4 x 16 x 4 x 8192 13.4 / 13.8.
+__host__ __device__ constexpr int min_waves(int d_k, int G) { return d_k == 64 && G <= 2 ? 6 : 4; }
 constexpr int kMostPlanned = 1024;        // sequences whose ranges are cut by their lengths
 
 // Ranges by length.  Sequences of unequal length cut into equally many ranges leave most of the chip waiting for the longest one, and the host
@@ -280,7 +283,7 @@ __host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k, int
 }
 
 template <int DK, int M, int G, bool FP8, int WAVES>
-__global__ __launch_bounds__(WAVES *kWave, 4) void attend_pages_kernel(PoolArgs p, AttendArgs a)
+__global__ __launch_bounds__(WAVES *kWave, min_waves(DK, G)) void attend_pages_kernel(PoolArgs p, AttendArgs a)
 {
     constexpr int threads = WAVES * kWave;
     constexpr size_t front = attend_front_bytes(G, M, DK, WAVES);
