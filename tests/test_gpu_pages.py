@@ -478,6 +478,60 @@ def test_compact_large_pools(lk):
         assert np.array_equal(pool.exponents.cpu().numpy()[:, 0], expected % 100)
 
 
+# ---- sizes that pass 32 bits ----------------------------------------------------------------------------------------
+def test_pools_beyond_four_gib(lk):
+    """Pages whose values lie 2^32 bytes and more behind the pool's start: written, attended to, copied, reserved and compacted."""
+    rng = np.random.default_rng(50)
+    P, H, d_k, m, page = 40000, 8, 128, 16, 128                          # 131 KB of values a page: 5.2 GB
+    pool = lk.PagePool(torch.empty((P, H, page, m), dtype=torch.uint8, device="cuda"),
+                       torch.empty((P, H, page // 8, d_k, 8), dtype=torch.int8, device="cuda"), torch.empty((P, H), dtype=torch.int8, device="cuda"))
+    ids = np.array([P - 1, 0, 33001, 17, 32768, 39000, 5, 36000])        # (2^32 bytes are 32768 pages)
+    c = random_cache(rng, len(ids), H, d_k, m, page, "int8")
+    at = torch.from_numpy(ids).cuda()
+    for x, y in zip(pool, (c.codes, c.values.view(np.int8), c.exponents)):
+        x[at] = dev(y)
+
+    def assert_pages():
+        torch.cuda.synchronize()
+        for x, y in zip(pool, (c.codes, c.values.view(np.int8), c.exponents)):
+            assert np.array_equal(x[at].cpu().numpy(), y)
+
+    small = np.array([[0, 1, 2], [4, 3, 5]], np.int32)                    # the reference's page numbers
+    table, lengths, counts = dev(ids[small].astype(np.int32)), [300, 290], [200, 33]
+    codes = rng.integers(0, 256, (2, H, 200, m), dtype=np.uint8)
+    values = rng.standard_normal((2, H, 200, d_k)).astype(np.float16)
+    lk.lookat_pages_write(pool, dev(codes), dev(values), table, i32(*lengths), i32(*counts))
+    c.write(codes, values, small, lengths, counts)
+    lk.lookat_pages_write(pool, dev(codes[:, :, :1]), dev(values[:, :, :1]), table, i32(301, 291))
+    c.write(codes[:, :, :1], values[:, :, :1], small, [301, 291])
+    assert_pages()
+    lut = (rng.standard_normal((2, H * 2, m, 256)) * 2).astype(np.float32)
+    for splits in (0, 1, 2):
+        out = lk.lookat_attend_pages(dev(lut), pool, table, i32(301, 291), 0.1, num_splits=splits)
+        assert_attend((out.cpu().numpy(), *c.attend(lut, small, [301, 291], 0.1)), "a large pool")
+    lk.lookat_pages_copy(pool, i32(P - 1, 5), i32(36000, 39000))
+    for x in (c.codes, c.values, c.exponents):
+        x[[7, 5]] = x[[0, 6]]
+    assert_pages()
+    # both sequences forked and grown by one token: the shared last pages (33001, 39000) go to the two lowest free ones
+    refs = torch.zeros(P, dtype=torch.int32, device="cuda")
+    refs[:32000] = 1
+    refs[table.long()] = 1
+    books = torch.cat([table, torch.full_like(table, -1)])
+    n = i32(301, 291, 0, 0)
+    lk.lookat_pages_fork(pool, books, n, refs, i32(0, 1), i32(2, 3))
+    assert int(lk.lookat_pages_reserve(pool, books, n, refs, i32(0, 0, 302, 292))) == 0
+    assert books[2:, 2].tolist() == [32000, 32001] and refs[[33001, 39000]].tolist() == [1, 1]
+    for x in pool:
+        assert torch.equal(x[books[2:, 2].long()], x[books[:2, 2].long()])
+    # 32007 pages in use: those above move down
+    before = [x[books.clamp(min=0).long()].clone() for x in pool]
+    moved, _, live = lk.lookat_pages_compact(pool, books, n, refs)
+    assert int(live) == 32006 and int(moved.max()) < 32006
+    for x, y in zip(pool, before):
+        assert torch.equal(x[moved.long()], y)
+
+
 # ---- together -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 def test_a_search_over_continuations(lk, kind):
