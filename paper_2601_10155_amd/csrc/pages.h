@@ -20,6 +20,8 @@ int check_pool(const lookat_page_pool *p);
 // Checks a table of `rows` rows (host).
 int check_table(const lookat_page_pool *p, const char *rows_name, int32_t rows, const int32_t *table, int32_t W, int64_t stride);
 PoolArgs pool_args(const lookat_page_pool *p);
+// One launch counts its threads along x in 32 bits.
+inline bool fits_launch(int64_t groups, int threads) { return groups * threads <= 0xffffffffLL; }
 
 // Why not the whole of int8: attention adds a page's exponent to its logits (base 2) and takes it off the weight again for the softmax sum, in
 // fp32.  A token of the lowest exponent beside one of the highest keeps its weight down to 2^-126 + 80 - 15 = 2^-61 of the largest.

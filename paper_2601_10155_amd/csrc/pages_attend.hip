@@ -774,7 +774,7 @@ extern "C" int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int3
             return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
     }
     const int64_t units = (int64_t)B * pool->H;
-    if (cut.groups > 0x7fffffffLL || units * group > 0x7fffffffLL)
+    if (!fits_launch(cut.groups, kAttendWaves * kWave) || !fits_launch(units, pool->d_k))
         return fail(LOOKAT_ERR_UNSUPPORTED, "B*H*num_splits: %lld workgroups exceed one launch", (long long)cut.groups);
     const PoolArgs p = pool_args(pool);
     AttendArgs a;

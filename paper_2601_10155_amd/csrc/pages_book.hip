@@ -542,7 +542,7 @@ extern "C" int lookat_pages_copy(const lookat_page_pool *pool, int32_t n, const 
         return LOOKAT_OK;
     const PoolArgs p = pool_args(pool);
     const int64_t groups = (int64_t)n * page_parts(p);
-    if (groups > 0x7fffffffLL)
+    if (!fits_launch(groups, kCopyThreads))
         return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d pages of %u parts exceed one launch", n, page_parts(p));
     hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)groups), dim3(kCopyThreads), 0, static_cast<hipStream_t>(stream), p, src, dst, n,
                        page_parts(p));
@@ -560,6 +560,8 @@ extern "C" int lookat_pages_fork(const lookat_page_pool *pool, int32_t S, int32_
         return rc;
     if (n == 0)
         return LOOKAT_OK;
+    if (!fits_launch(n, kBookThreads))
+        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d slots exceed one launch", n);
     hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)n), dim3(kBookThreads), 0, static_cast<hipStream_t>(stream),
                        book_args(pool, S, table, W, table_stride, lengths, refs), n, src, dst);
     return check_launch("lookat_pages_fork");
@@ -576,6 +578,8 @@ extern "C" int lookat_pages_free(const lookat_page_pool *pool, int32_t S, int32_
         return rc;
     if (n == 0)
         return LOOKAT_OK;
+    if (!fits_launch(n, kBookThreads))
+        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d slots exceed one launch", n);
     hipLaunchKernelGGL(pages_free_kernel, dim3((unsigned)n), dim3(kBookThreads), 0, static_cast<hipStream_t>(stream),
                        book_args(pool, S, table, W, table_stride, lengths, refs), slots);
     return check_launch("lookat_pages_free");

@@ -407,6 +407,8 @@ extern "C" int lookat_pages_write(const lookat_page_pool *pool, int32_t B, int64
     a.W = W;
     int64_t touched = (N + pool->page - 2) / pool->page + 1;      // N tokens from anywhere in a page on
     touched = touched < W ? touched : W;
+    if (!fits_launch(touched, kWriteThreads))
+        return fail(LOOKAT_ERR_UNSUPPORTED, "N=%lld: %lld pages of a sequence exceed one launch", (long long)N, (long long)touched);
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (value_dtype == LOOKAT_F16)

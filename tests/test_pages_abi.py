@@ -131,6 +131,18 @@ def test_upkeep_refusals(lib):  # noqa: F811
     assert need > 0 and k(pool(), wsb=need - 1) == E_WS
 
 
+def test_more_threads_than_one_launch_counts(lib):  # noqa: F811
+    """2^32 threads along x: refused by name, not by whatever a launch of them would do."""
+    c, many = calls(lib), 1 << 24                                         # workgroups of 256
+    for name in ("copy", "fork", "free"):
+        assert c[name](pool(), n=many) == E_UNSUP and b"launch" in lib.lookat_last_error()
+    assert c["write"](pool(page=16), N=1 << 28, cs=M << 28, vs=D << 28, W=1 << 26, stride=1 << 26) == E_UNSUP
+    assert b"launch" in lib.lookat_last_error()
+    for splits in (0, 1):                                                 # (65535 * 129 and not more than 4096 heads: 2^23 workgroups of 512)
+        assert c["attend"](pool(H=129), B=65535, W=4, stride=4, splits=splits) == E_UNSUP
+        assert b"launch" in lib.lookat_last_error()
+
+
 def test_binding_refuses_what_is_not_a_pool():
     p = binding.PagePool(torch.zeros((4, 2, 16, 4), dtype=torch.uint8), torch.zeros((4, 2, 2, 64, 8), dtype=torch.int8),
                          torch.zeros((4, 2), dtype=torch.int8))
