@@ -710,6 +710,8 @@ def _scratch(workspace, need: int, pool: PagePool) -> torch.Tensor | None:
         return workspace
     if workspace is not None and workspace.device != pool.codes.device:
         raise ValueError("workspace must live on the pool's device")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     if workspace is None or workspace.numel() * workspace.element_size() < need:
         workspace = torch.empty(need, dtype=torch.uint8, device=pool.codes.device)
     return workspace

@@ -422,7 +422,7 @@ bool scratch_of(PyObject *o, size_t need, const Pool &p, at::Tensor &own, void *
 {
     if (o != Py_None) {
         const at::Tensor *w = plain(o);
-        if (!w || !beside(p, *w))
+        if (!w || !w->is_contiguous() || !beside(p, *w))
             return false;
         ptr = w->data_ptr();
         bytes = (size_t)w->numel() * w->element_size();

@@ -734,3 +734,18 @@ def test_what_the_binding_refuses(lk, monkeypatch, native):
             bad()
     torch.cuda.synchronize()
     assert torch.all(table == -1) and torch.all(n == 0)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_the_binding_refuses_a_workspace_with_less_memory_than_elements(lk, monkeypatch, native):
+    from paper_2601_10155_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", Watch(None))
+    pool = lk.page_pool(10, 2, 64, 4, 16)
+    table, n, refs = torch.full((3, 4), -1, dtype=torch.int32, device="cuda"), i32(0, 0, 0), i32(*[0] * 10)
+    lut, few = torch.zeros((3, 2, 4, 256), device="cuda"), torch.empty(1, dtype=torch.uint8, device="cuda").expand(1 << 20)
+    for bad in (lambda: lk.lookat_attend_pages(lut, pool, table, n, 1.0, num_splits=2, workspace=few),
+                lambda: lk.lookat_pages_reserve(pool, table, n, refs, i32(1, 1, 1), workspace=few),
+                lambda: lk.lookat_pages_compact(pool, table, n, refs, workspace=few)):
+        with pytest.raises(ValueError):
+            bad()

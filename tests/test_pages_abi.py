@@ -162,6 +162,14 @@ def test_binding_refuses_what_is_not_a_pool():
 
 
 # ---- the reference's own pins ---------------------------------------------------------------------------------------
+def test_binding_refuses_a_workspace_with_less_memory_than_elements():
+    p = binding.page_pool(4, 2, 64, 4, 16, device="cpu")
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._scratch(torch.empty(1, dtype=torch.uint8).expand(4096), 1024, p)
+    given = torch.empty(4096, dtype=torch.uint8)
+    assert binding._scratch(given, 1024, p) is given and binding._scratch(given, 8192, p).numel() == 8192
+
+
 def test_reference_e4m3_against_torch():
     every = torch.arange(256, dtype=torch.uint8)
     values = every.view(torch.float8_e4m3fn).double().numpy()
