@@ -16,7 +16,9 @@
 // Weighted sums on the matrix cores at every group, also for one query head: 1 + 1/2 vector instructions a stored value (int8; 1/2 in e4m3)
 // instead of 2.  What was tried and not kept: four or sixteen wavefronts to a workgroup (long contexts 178.9 / 179.8 us, eight 177.4, groups of 8
 // 30.6 / 41.0, eight 27.7, at an earlier stage), a second tile in registers at d_k = 64 (16 x 12 x 4096 14.8 -> 17.1 us: fewer wavefronts fit),
-// ranges of whole steps of eight tiles (no change), a product with integer weights (the tables' scores need 22 bits).
+// ranges of whole steps of eight tiles (no change), a product with integer weights (the tables' scores need 22 bits), tables loaded straight into
+// LDS (a lane names one word where heads are interleaved: groups of 8 20.1 / 22.2, of 4 17.5 / 18.8, one head 15.9 / 16.6 us).  Neither side of the
+// tables' LDS traffic counts: without bank conflicts in the stores 20.2, in the look-ups 19.7 instead of 20.1.
 //
 // One workgroup = one (sequence, key/value head, range); its wavefronts take the range's 64-token tiles in turn.  In a tile
 //   * scoring: a lane per token: its page from the table, its codes (one load), m look-ups per query head in the head's table in LDS.  The
