@@ -60,7 +60,10 @@ constexpr int kAttendWaves = 8, kShortWaves = 4;
 __host__ __device__ constexpr bool few_waves(int G, int m, int64_t longest) { return G * m < 64 && longest <= kShortWaves * kTile; }
 // Wavefronts to a SIMD that the registers have to allow: six (80 registers) where they do without spilling; us, four / six: d_k = 64, groups of 2
 // x 32 x 6 x 4096, m = 8 18.3 / 17.0, 16 x 12 x 4096, m = 16 e4m3 18.9 / 17.0, m = 4 14.9 / 14.9; groups of 4 x 16 x 4 x 8192 13.4 / 13.8.
-__host__ __device__ constexpr int min_waves(int d_k, int G) { return d_k == 64 && G <= 2 ? 6 : 4; }
+// Two where 128 KB of tables leave room for one workgroup only: the other registers hold look-ups in flight (8 x 4 x 65536 84.5 / 81.6).
+__host__ __device__ constexpr int min_waves(int d_k, int m, int G) { return G * m >= 128 ? 2 : d_k == 64 && G <= 2 ? 6 : 4; }
+// Tables of 32 KB and more: every range fetches them, so there are as many ranges as the chip holds at once and no second round (see cut_of).
+__host__ __device__ constexpr bool one_round(int m, int G) { return G * m >= 32; }
 constexpr int kMostPlanned = 1024;        // sequences whose ranges are cut by their lengths
 
 // Ranges by length.  Sequences of unequal length cut into equally many ranges leave most of the chip waiting for the longest one, and the host
@@ -109,6 +112,7 @@ __device__ __forceinline__ int upto_lane(int v)
     return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // row_bcast:31 into rows 2 and 3
 }
 // (all threads of the workgroup; s: 36 ints of LDS; B <= kMostPlanned; false: no range)
+template <bool ONE_ROUND>
 __device__ __forceinline__ bool range_by_length(const AttendArgs &a, int H, int page_log2, int *s, Range &r)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, waves = blockDim.x / kWave;
@@ -116,9 +120,17 @@ __device__ __forceinline__ bool range_by_length(const AttendArgs &a, int H, int 
     if (a.B <= kWave) {
         // a lane per sequence, every wavefront for itself
         const int length = lane < a.B ? clamp_length(a.lengths[lane], a.W, page_log2) : 0;
-        const int c = range_tokens(wave_sum((float)length), a.per_head, a.least);
-        const int n = lane < a.B ? ranges_of(length, c) : 0;
-        const int upto = upto_lane(n);
+        const float total = wave_sum((float)length);
+        int c = range_tokens(total, a.per_head, a.least);
+        int n = lane < a.B ? ranges_of(length, c) : 0;
+        int upto = upto_lane(n);
+        const int extra = ONE_ROUND ? __builtin_amdgcn_readlane(upto, kWave - 1) - a.per_head : 0;
+        if (extra > 0 && 2 * extra < a.per_head) {
+            // (longer ones instead of as many more as the sequences' last ranges made: a few too many wait for a round of their own)
+            c = range_tokens(total, a.per_head - extra, a.least);
+            n = lane < a.B ? ranges_of(length, c) : 0;
+            upto = upto_lane(n);
+        }
         const int ranges = __builtin_amdgcn_readlane(upto, kWave - 1) * H, per_die = (ranges + kXcds - 1) / kXcds, index = die * per_die + nth;
         if (nth >= per_die || index >= ranges)
             return false;
@@ -285,7 +297,7 @@ __host__ __device__ constexpr size_t attend_lds_bytes(int G, int M, int d_k, int
 }
 
 template <int DK, int M, int G, bool FP8, int WAVES>
-__global__ __launch_bounds__(WAVES *kWave, min_waves(DK, G)) void attend_pages_kernel(PoolArgs p, AttendArgs a)
+__global__ __launch_bounds__(WAVES *kWave, min_waves(DK, M, G)) void attend_pages_kernel(PoolArgs p, AttendArgs a)
 {
     constexpr int threads = WAVES * kWave;
     constexpr size_t front = attend_front_bytes(G, M, DK, WAVES);
@@ -296,7 +308,7 @@ __global__ __launch_bounds__(WAVES *kWave, min_waves(DK, G)) void attend_pages_k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     Range r;
     if (a.per_head) {
-        if (!range_by_length(a, p.H, p.page_log2, reinterpret_cast<int *>(lds), r))
+        if (!range_by_length<one_round(M, G)>(a, p.H, p.page_log2, reinterpret_cast<int *>(lds), r))
             return;
     } else {
         // ranges of one (sequence, head) on one die: its tables are fetched into one L2
@@ -434,8 +446,9 @@ __global__ __launch_bounds__(WAVES *kWave, min_waves(DK, G)) void attend_pages_k
 #pragma unroll
         for (int g = 0; g < G; ++g)
             y[g] = (float)exponent;
-        // (LDS reads in flight at once: 16 registers of them, 8 where the others take what is left: groups of 8 x 8191 tokens 20.4 / 19.7 us)
-        constexpr int planes = G / GP, most_reads = (DK == 128 && (G == 8 || M == 16) ? 8 : 16) / GP;
+        // (LDS reads in flight at once: 16 registers of them, 8 where the others take what is left: groups of 8 x 8191 tokens 20.4 / 19.7 us; 32
+        // where one workgroup has the compute unit: 8 / 16 / 32 / 64 84.2 / 81.9 / 81.5 / 81.5 us for 128 KB of tables x 4 heads x 8 x 65536)
+        constexpr int planes = G / GP, most_reads = (G * M >= 128 ? 32 : DK == 128 && (G == 8 || M == 16) ? 8 : 16) / GP;
         constexpr int together = M * planes < most_reads ? M * planes : most_reads;
 #pragma unroll
         for (int n0 = 0; n0 < M * planes; n0 += together) {
@@ -635,6 +648,11 @@ __global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, i
 // So 1024, and 2048 where those still have 4096 tokens.  Least range of 512 / 1024 / 2048 tokens (1024 ranges): 2 heads in groups of 8 x 3000
 // 10.3 / 11.6 / 13.6; 1 x 32 x 8192 13.5 / 13.4 / 15.5; 8 x 32 x up to 1500 16.7 / 14.8 / 14.0; 64 KB of tables (groups of 8, m = 8), which every
 // range fetches: 12 x 8 x up to 8191 25.3 / 21.1 / 20.3, 64 x 4 x up to 2048 27.6 / 23.0 / 21.9.  So 1024, and 2048 from 64 KB on.
+// Tables of 32 KB and more (G m >= 32): 512 ranges, two for each compute unit, and 256 from 128 KB on, of which one workgroup fills a
+// compute unit; the target is not passed (range_by_length; for up to 64 sequences), so that nothing waits for a second round.  us, 1024 or 2048 ranges / so:
+// groups of 8 x 4 heads, m = 16, 8 x 65536 81.6 / 57.6, 16 x up to 65536 104.9 / 72.3, m = 8 59.5 / 54.4 and 76.1 / 64.2; groups of 4 x 8, m = 8,
+// 8 x 32768 52.9 / 51.2, 16 x up to 32768 66.8 / 61.9; groups of 8 x 8, d_k = 64, m = 4, 16 x up to 16384 31.4 / 24.0.  With 16 KB it costs: one
+// head, m = 16, 16 x 32 x up to 16384 114.9 / 119.9; d_k = 64, 16 x 12 x 4096 17.0 / 18.8.
 // Sequences of up to 2048 tokens are not cut at all: the merge is a launch more (8 x 32 x up to 1500 14.0 whole, 14.8 cut).  Where 1024 tokens a
 // range would make fewer than 128 ranges, 512.
 constexpr int kWholeLength = 2048;
@@ -660,8 +678,13 @@ static Cut cut_of(const lookat_page_pool *p, int32_t B, int32_t G, int32_t W, in
     if (num_splits == 0 && longest > kWholeLength && B <= kMostPlanned) {
         // (from the rows' room where the number of ranges has to hold them all: a sequence may be longer than the caller knows)
         const int64_t room = (int64_t)W * p->page;
-        const int64_t target = units * longest >= 2048LL * 4096 ? 2048 : 1024;
-        c.per_head = (int)((target + p->H - 1) / p->H);
+        if (one_round(p->m, G)) {
+            const int target = G * p->m >= 128 ? 256 : 512;
+            c.per_head = target > p->H ? target / p->H : 1;
+        } else {
+            const int64_t target = units * longest >= 2048LL * 4096 ? 2048 : 1024;
+            c.per_head = (int)((target + p->H - 1) / p->H);
+        }
         c.least = least_range(G, p->m, units, longest);
         const int64_t fit = (int64_t)B * ((room + c.least - 1) / c.least), most = c.per_head + 1 + B;
         c.ranges = p->H * (fit < most ? fit : most);

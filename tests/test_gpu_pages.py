@@ -237,6 +237,19 @@ def test_attend_many_sequences(lk, B):
     assert_attend(attend_case(lk, rng, c, lengths, 1), "many sequences")
 
 
+@pytest.mark.parametrize("H,group,d_k,m,lengths", [
+    (128, 8, 64, 4, [3500, 2500]),                        # 4 ranges a head wanted, 5 at first: longer ones, 4
+    (128, 8, 64, 4, [3500, 2500, 0, 1, 700]),             # 8 at first: left so
+    (520, 8, 64, 4, [2100, 40]),                          # more heads than ranges wanted
+    (32, 8, 128, 16, [8000, 5200, 5200]),                 # 128 KB of tables: 8 wanted, 10 at first, 7
+    (7, 4, 128, 8, [30001, 2049, 15000])])
+def test_attend_large_tables(lk, H, group, d_k, m, lengths):
+    """Ranges that the chip holds at once: fewer and longer ones where the sequences' last ranges would make too many."""
+    rng = np.random.default_rng(H + m)
+    c = random_cache(rng, sum(-(-n // 128) for n in lengths) + 2, H, d_k, m, 128, "int8")
+    assert_attend(attend_case(lk, rng, c, lengths, group), "large tables")
+
+
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 def test_attend_peaked_and_flat(lk, kind):
     """Logits from nothing to hundreds, rising and falling along the row (the reference has to follow)."""
