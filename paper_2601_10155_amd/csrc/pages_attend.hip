@@ -562,7 +562,7 @@ __global__ __launch_bounds__(WAVES *kWave, min_waves(DK, M, G)) void attend_page
     // one range: results are divided by the sum here; several: the merge does it
     float f = fast_exp2(own - top);
     if (r.splits == 1)
-        f = sum > 0.f ? f / sum : 0.f;
+        f = sum == 0.f ? 0.f : f / sum;                   // (nothing to sum: zeros; a sum that is NaN stays one)
     float *results = reinterpret_cast<float *>(lds);
 #pragma unroll
     for (int c = 0; c < 2 * CB; c += 2)
@@ -637,7 +637,7 @@ __global__ __launch_bounds__(128) void attend_pages_merge_kernel(AttendArgs a, i
         }
         top = to;
     }
-    a.out[((int64_t)unit * G + g) * d_k + d] = z > 0.f ? o / z : 0.f;
+    a.out[((int64_t)unit * G + g) * d_k + d] = z == 0.f ? 0.f : o / z;
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------

@@ -1,0 +1,83 @@
+"""The paged cache on the GPU at the edges: tables that are not finite, the ends of fp32, many sequences, what a weight has to be worth."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import pages_ref as pr
+from test_gpu_pages import dev, i32, lk, on_gpu, random_cache, random_table  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+CUTS = [{"num_splits": 1}, {"num_splits": 3}, {}, {"max_length": 64}]
+
+
+# ---- tables that are not finite -----------------------------------------------------------------------------------
+def not_finite_case(kind, group, d_k, m):
+    """One short and one long sequence (cut by length where the call chooses), a cache of two heads, finite tables."""
+    rng = np.random.default_rng(group + d_k + m)
+    lengths, H = [70, 2500], 2
+    c = random_cache(rng, 50, H, d_k, m, 64, kind)
+    table = random_table(rng, lengths, 64, 40, 50)
+    lut = (rng.standard_normal((2, H * group, m, 256)) * 2).astype(np.float32)
+    return c, table, lengths, lut
+
+
+def a_code(c, table, length, b, h, i):
+    """The code of subspace i that the token in the middle of sequence b has in head h."""
+    t = length // 2
+    return int(c.codes[table[b, t // c.page], h, t % c.page, i])
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group,d_k,m", [(1, 64, 4), (2, 128, 8), (4, 64, 2), (8, 128, 8)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_attend_shows_scores_that_are_no_numbers(lk, kind, group, d_k, m, value):  # noqa: F811
+    """A NaN or +inf score: its row is NaN, cut or not, and no other one."""
+    c, table, lengths, lut = not_finite_case(kind, group, d_k, m)
+    hit = [(0, 0), (1, 2 * group - 1)]                    # (sequence, query head)
+    broken = lut.copy()
+    for b, hq in hit:
+        broken[b, hq, m - 1, a_code(c, table, lengths[b], b, hq // group, m - 1)] = value
+    ref, bound = c.attend(lut, table, lengths, 0.1)
+    for kw in CUTS:
+        out = lk.lookat_attend_pages(dev(broken), on_gpu(lk, c), dev(table), i32(*lengths), 0.1, **kw).cpu().numpy()
+        for b in range(2):
+            for hq in range(2 * group):
+                if (b, hq) in hit:
+                    assert np.isnan(out[b, hq]).all(), (b, hq, kw)
+                else:
+                    assert np.all(np.abs(out[b, hq] - ref[b, hq]) <= bound[b, hq]), (b, hq, kw)
+
+
+class WithoutTokens(pr.Cache):
+    """One head of a cache, without the tokens whose code of subspace i is even."""
+
+    def __init__(self, c, h, i):
+        super().__init__(c.codes[:, h: h + 1], c.values[:, h: h + 1], c.exponents[:, h: h + 1], c.kind)
+        self.i = i
+
+    def tokens(self, table_row, length, exponents=False):
+        every = super().tokens(table_row, length, True)
+        return tuple(x[:, every[0][0, :, self.i] % 2 == 1] for x in every)
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group,d_k,m", [(1, 64, 4), (2, 128, 8), (8, 128, 8)])
+def test_attend_minus_infinity_is_a_token_without_weight(lk, kind, group, d_k, m):  # noqa: F811
+    """Half of the codes of one subspace at -inf: the tokens that have them count for nothing.  All of them: zeros."""
+    c, table, lengths, lut = not_finite_case(kind, group, d_k, m)
+    lut[0, 0, 1, ::2] = lut[1, 1, 0, ::2] = -math.inf
+    nothing = group * 2 - 1
+    lut[1, nothing, 0, :] = -math.inf
+    scale = 0.1
+    for kw in CUTS:
+        out = lk.lookat_attend_pages(dev(lut), on_gpu(lk, c), dev(table), i32(*lengths), scale, **kw).cpu().numpy()
+        assert np.isfinite(out).all() and np.all(out[1, nothing] == 0)
+        for b, hq, i in ((0, 0, 1), (1, 1, 0)):
+            if (b, hq) == (1, nothing):
+                continue
+            few = WithoutTokens(c, hq // group, i)
+            ref, bound = few.attend(lut[b: b + 1, hq: hq + 1], table[b: b + 1], [lengths[b]], scale)
+            assert np.all(np.abs(out[b, hq] - ref[0, 0]) <= bound[0, 0]), (b, hq, kw)
