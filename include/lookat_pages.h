@@ -83,8 +83,8 @@ int lookat_pages_write(const lookat_page_pool *pool, int32_t B, int64_t N,
  *     out[b,hq,:] = sum_l softmax_l(scale * s[b,hq,:]) * value(b, hq/group, l, :)       l < lengths[b]
  * A sequence without tokens gives zeros, and so does one whose tokens all have a score of -inf (a -inf in a table is a token
  * without weight).  A NaN score, or one of +inf, makes its query head's row NaN, however the sequence is cut; other rows are
- * not touched by it.  Scores, softmax statistics and sums are held in fp32; a weight enters the product with the values as two
- * fp16 terms (22 bits), the stored 8-bit numbers exactly.
+ * not touched by it.  Scores (times scale and log2(e), so that 2.35e38 is their end), softmax statistics and sums are held
+ * in fp32; a weight enters the product with the values as two fp16 terms (22 bits), the stored 8-bit numbers exactly.
  *   lut           [B, H*group, m, 256] fp32, 16-byte aligned, from lookat_build_lut
  *   max_length    the longest length the host knows of, or 0 for W * page: it sizes the launch alone; longer sequences are
  *                 right too

@@ -50,7 +50,7 @@ struct AttendArgs {
 };
 
 constexpr float kRefLag = 8.f;            // the reference moves when a logit exceeds it by more (log2 units)
-constexpr float kNoReference = -3e38f;    // before the first token; below every logit, and finite: -inf less it is -inf
+constexpr float kNoReference = -3.402823466e38f;   // before the first token: fp32's lowest, so no logit is below it, and finite: -inf less it is -inf
 constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, below 2^15: fp16's range, its subnormals far below
 // Wavefronts of a workgroup: eight of 128 registers, two workgroups to a compute unit.  Four where no sequence is longer than four tiles: the
 // others would only take room from the next workgroups (us, eight / four: 42 x 32 x 157 tokens in groups of 2 15.0 / 10.7, 64 x 32 x 250

@@ -81,3 +81,24 @@ def test_attend_minus_infinity_is_a_token_without_weight(lk, kind, group, d_k, m
             few = WithoutTokens(c, hq // group, i)
             ref, bound = few.attend(lut[b: b + 1, hq: hq + 1], table[b: b + 1], [lengths[b]], scale)
             assert np.all(np.abs(out[b, hq] - ref[0, 0]) <= bound[0, 0]), (b, hq, kw)
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group,d_k,m", [(1, 64, 4), (2, 128, 8), (4, 64, 2), (8, 128, 8)])
+@pytest.mark.parametrize("level", [-2.0e38, -2.1e38, -2.358e38, 2.358e38])
+def test_attend_equal_scores_at_the_ends_of_fp32(lk, kind, group, d_k, m, level):  # noqa: F811
+    """Scores that are the same to the last bit are equal weights, down to the lowest number: the mean of the values.  All exponents are
+    equal, every weight is a power of two, the same for all tokens, and the sums are of whole numbers (int8) or of multiples of 2^-9 below
+    448 * 2500: 24 bits hold int8's sums exactly and e4m3's to 2500 roundings of half a step.  The quotient, its product and the merge's weights:
+    four roundings.  2^-20 (int8) or 2500 * 2^-24 of the mean size, doubled for the hardware's reciprocal and exponential."""
+    c, table, lengths, lut = not_finite_case(kind, group, d_k, m)
+    c.exponents[:] = -3
+    lut[:] = 0
+    lut[:, :, 1] = level
+    for kw in CUTS:
+        out = lk.lookat_attend_pages(dev(lut), on_gpu(lk, c), dev(table), i32(*lengths), 1.0, **kw).cpu().numpy()
+        for b in range(2):
+            _, v = c.tokens(table[b], lengths[b])
+            ref = np.repeat(v.mean(1), group, 0)
+            bound = np.repeat(np.abs(v).mean(1), group, 0) * (2 ** -19 if kind == "int8" else 2 * 2500 * 2.0 ** -24)
+            assert np.all(np.abs(out[b] - ref) <= bound), (b, kw)
