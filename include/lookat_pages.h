@@ -24,8 +24,8 @@
  *
  * Supported: d_k in {64, 128}, m in {2, 4, 8, 16} dividing d_k, page in {16, 32, 64, 128}, at most 2^30 pages of
  * at most 4096 heads, at most 65535 sequences, W * page at most 2^30, and per call fewer than 2^23 workgroups
- * (sequences * heads * num_splits of attention, 16 KB pieces of pages to copy, pages of one sequence written) and 2^24 list entries of a fork
- * or free; otherwise LOOKAT_ERR_UNSUPPORTED or LOOKAT_ERR_SHAPE.
+ * (sequences * heads * num_splits of attention, pages of one sequence written), fewer than 2^24 16 KB pieces of pages to copy and at most
+ * 65535 list entries of a fork or free; otherwise LOOKAT_ERR_UNSUPPORTED or LOOKAT_ERR_SHAPE.
  */
 #ifndef LOOKAT_PAGES_H
 #define LOOKAT_PAGES_H

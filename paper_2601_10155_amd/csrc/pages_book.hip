@@ -142,6 +142,11 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PoolArgs p, co
     copy_page_part(p, from, to, part);
 }
 
+// Lists of slots: every workgroup of a fork or free looks through the call's list for its own slot, so the work grows with the
+// square of it (us for 1500 / 16384 / 65535 entries: fork 14 / 90 / 1100, free 8 / 44 / 490).  A list as long as there can be sequences
+// names everything that can take effect.
+constexpr int kMostListed = 65535;
+
 // ---- fork -------------------------------------------------------------------------------------------------------
 // One workgroup per pair.  Which pairs count is decided from the call's own arguments and from lengths that no other pair of the call
 // writes: a source that is somebody's destination is out, a destination belongs to the first pair that names it.
@@ -560,8 +565,8 @@ extern "C" int lookat_pages_fork(const lookat_page_pool *pool, int32_t S, int32_
         return rc;
     if (n == 0)
         return LOOKAT_OK;
-    if (!fits_launch(n, kBookThreads))
-        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d slots exceed one launch", n);
+    if (n > kMostListed)
+        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d: one launch takes at most %d slots", n, kMostListed);
     hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)n), dim3(kBookThreads), 0, static_cast<hipStream_t>(stream),
                        book_args(pool, S, table, W, table_stride, lengths, refs), n, src, dst);
     return check_launch("lookat_pages_fork");
@@ -578,8 +583,8 @@ extern "C" int lookat_pages_free(const lookat_page_pool *pool, int32_t S, int32_
         return rc;
     if (n == 0)
         return LOOKAT_OK;
-    if (!fits_launch(n, kBookThreads))
-        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d slots exceed one launch", n);
+    if (n > kMostListed)
+        return fail(LOOKAT_ERR_UNSUPPORTED, "n=%d: one launch takes at most %d slots", n, kMostListed);
     hipLaunchKernelGGL(pages_free_kernel, dim3((unsigned)n), dim3(kBookThreads), 0, static_cast<hipStream_t>(stream),
                        book_args(pool, S, table, W, table_stride, lengths, refs), slots);
     return check_launch("lookat_pages_free");

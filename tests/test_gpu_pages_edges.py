@@ -102,3 +102,26 @@ def test_attend_equal_scores_at_the_ends_of_fp32(lk, kind, group, d_k, m, level)
             ref = np.repeat(v.mean(1), group, 0)
             bound = np.repeat(np.abs(v).mean(1), group, 0) * (2 ** -19 if kind == "int8" else 2 * 2500 * 2.0 ** -24)
             assert np.all(np.abs(out[b] - ref) <= bound), (b, kw)
+
+
+# ---- the books at their limits --------------------------------------------------------------------------------------
+def test_lists_as_long_as_there_can_be_sequences(lk):  # noqa: F811
+    """65535 sequences and lists of as many entries, every pair and slot named twice: the first one counts."""
+    S, n, P = 65535, 32767, 40000
+    pool = lk.page_pool(P, 1, 64, 2, 16)
+    table = torch.full((S, 1), -1, dtype=torch.int32, device="cuda")
+    lengths, refs = torch.zeros(S, dtype=torch.int32, device="cuda"), torch.zeros(P, dtype=torch.int32, device="cuda")
+    held = torch.arange(n, device="cuda")
+    table[:n, 0], lengths[:n], refs[:n] = held.flip(0).int() + 100, (held % 16 + 1).int(), 0
+    refs[100: 100 + n] = 1
+    src = torch.cat([held, held.roll(1), held[:1]]).int()                 # the second half names other parents for the same children
+    dst = torch.cat([held + n, held + n, held[:1] + n]).int()
+    lk.lookat_pages_fork(pool, table, lengths, refs, src, dst)
+    torch.cuda.synchronize()
+    assert torch.equal(table[n: 2 * n], table[:n]) and torch.equal(lengths[n: 2 * n], lengths[:n])
+    assert int(refs.sum()) == 2 * n and torch.all(refs[100: 100 + n] == 2) and int(lengths[-1]) == 0 and int(table[-1]) == -1
+    slots = torch.cat([held.flip(0), held, held[:1]]).int()
+    lk.lookat_pages_free(pool, table, lengths, refs, slots)
+    torch.cuda.synchronize()
+    assert torch.all(lengths[:n] == 0) and torch.all(table[:n] == -1) and torch.all(refs[100: 100 + n] == 1) and int(refs.sum()) == n
+    assert torch.all(lengths[n: 2 * n] > 0)
