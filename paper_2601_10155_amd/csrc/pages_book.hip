@@ -131,6 +131,37 @@ __device__ __forceinline__ int block_before(int v, int *s, int *total)
     return before;
 }
 
+// For two numbers of every thread: the sum of x over the threads before this one, and the sums of both over the workgroup.  `s`: two numbers
+// per wavefront in LDS, not in use yet.
+struct Sums {
+    long long before, x, y;
+};
+template <int THREADS>
+__device__ __forceinline__ Sums block_before_and_sums(long long x, long long y, long long *s)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    long long up = x;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const long long t = __shfl_up(up, d);
+        up += lane >= d ? t : 0;
+        y += __shfl_xor(y, d);
+    }
+    if (lane == kWave - 1) {
+        s[2 * wave] = up;
+        s[2 * wave + 1] = y;
+    }
+    __syncthreads();
+    Sums r = {up - x, 0, 0};
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w) {
+        r.before += w < wave ? s[2 * w] : 0;
+        r.x += s[2 * w];
+        r.y += s[2 * w + 1];
+    }
+    return r;
+}
+
 // ---- copy -------------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PoolArgs p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
                                                                   int n, uint32_t parts)
@@ -210,11 +241,14 @@ __global__ __launch_bounds__(kBookThreads) void pages_free_kernel(BookArgs a, co
 // ---- reserve ----------------------------------------------------------------------------------------------------
 // Two launches.  The first ranks: its page workgroups write the free pages' ids in ascending order (each counts the free pages
 // ahead of its segment by itself: the counts are read from L2 a few times over instead of a chain of launches), its slot workgroups what each
-// sequence needs.  The second gives them out, a workgroup per sequence and part of a page to copy.
+// sequence needs, summed up within kRankThreads sequences.  The second adds up those at most 64 sums and gives the pages out, a workgroup per
+// sequence and part of a page to copy.
 struct ReservePlan {
     int32_t *free_ids;   // [pages]
     int32_t *need;       // [S] pages
     int32_t *shared;     // [S] the page to copy, or -1
+    int32_t *before;     // [S] pages needed by the sequences ahead in the same kRankThreads (right where no page is missing)
+    long long *sums;     // [S / kRankThreads, rounded up][2] pages needed, entries that rows are short of
     int32_t *count;      // [0]: free pages
     int32_t *copies;     // [2][S] for the caller, or NULL
 };
@@ -260,12 +294,13 @@ __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookAr
     __shared__ __align__(8) int s[2 * kRankThreads / kWave];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= segments) {
-        const int slot = ((int)blockIdx.x - segments) * kRankThreads + tid;
-        if (slot >= a.S)
-            return;
+        __shared__ long long sums[2 * kRankThreads / kWave];
+        const int group = (int)blockIdx.x - segments, slot = group * kRankThreads + tid;
+        const bool there = slot < a.S;
         const int page = 1 << a.page_log2;
-        const int length = a.lengths[slot] < 0 ? 0 : a.lengths[slot], wanted = new_lengths[slot];
+        const int length = there && a.lengths[slot] > 0 ? a.lengths[slot] : 0, wanted = there ? new_lengths[slot] : 0;
         int need = 0, shared = -1;
+        long long over = 0;                                       // entries that the row is short of
         if (wanted > length) {
             // (64-bit: lengths up to 2^31 - 1)
             const int64_t has = ((int64_t)length + page - 1) >> a.page_log2, needs = ((int64_t)wanted + page - 1) >> a.page_log2;
@@ -277,9 +312,18 @@ __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookAr
                     ++need;
                 }
             }
+            over = need > 0 && needs > a.W ? needs - a.W : 0;
         }
+        const Sums t = block_before_and_sums<kRankThreads>(need, over, sums);
+        if (tid == 0) {
+            plan.sums[2 * group] = t.x;
+            plan.sums[2 * group + 1] = t.y;
+        }
+        if (!there)
+            return;
         plan.need[slot] = need;
         plan.shared[slot] = shared;
+        plan.before[slot] = (int32_t)t.before;
         if (plan.copies) {
             plan.copies[slot] = -1;
             plan.copies[a.S + slot] = -1;
@@ -312,49 +356,38 @@ __global__ __launch_bounds__(kRankThreads) void pages_reserve_rank_kernel(BookAr
 __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(PoolArgs p, BookArgs a, const int32_t *__restrict__ new_lengths, ReservePlan plan,
                                                                      int32_t *__restrict__ missing)
 {
-    __shared__ long long s[3][kBookThreads / kWave];
     const int slot = blockIdx.x, part = blockIdx.y, tid = threadIdx.x;
     const int need = plan.need[slot], shared = plan.shared[slot];
     const int wanted = new_lengths[slot];
+    const int length = part > 0 || a.lengths[slot] < 0 ? 0 : a.lengths[slot];        // (the first part's workgroup alone writes it)
     const bool report = slot == 0 && part == 0;
     if (!report && (part > 0 ? shared < 0 : need == 0 && wanted <= 0))
         return;
-    // pages needed ahead of this sequence, and by all; how far the longest rows are short
-    long long before = 0, all = 0, over = 0;
-    for (int j = tid; j < a.S; j += kBookThreads) {
-        const int x = plan.need[j];
-        before += j < slot ? x : 0;
-        all += x;
-        const int w = new_lengths[j];
-        const long long pages = ((long long)w + (1 << a.page_log2) - 1) >> a.page_log2;
-        over += x > 0 && pages > a.W ? pages - a.W : 0;
+    // pages needed ahead of this sequence, and by all; how far rows are short
+    long long before = plan.before[slot], all, over;
+    const int groups = (a.S + kRankThreads - 1) / kRankThreads;          // (at most 64: a lane each)
+    if (groups == 1) {
+        all = plan.sums[0];
+        over = plan.sums[1];
+    } else {
+        const int lane = tid & (kWave - 1);
+        all = lane < groups ? plan.sums[2 * lane] : 0;
+        over = lane < groups ? plan.sums[2 * lane + 1] : 0;
+        long long ahead = lane < slot / kRankThreads ? all : 0;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            ahead += __shfl_xor(ahead, d);
+            all += __shfl_xor(all, d);
+            over += __shfl_xor(over, d);
+        }
+        before += ahead;
     }
     const int free_pages = plan.count[0];
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        before += __shfl_xor(before, d);
-        all += __shfl_xor(all, d);
-        over += __shfl_xor(over, d);
-    }
-    if ((tid & (kWave - 1)) == 0) {
-        s[0][tid / kWave] = before;
-        s[1][tid / kWave] = all;
-        s[2][tid / kWave] = over;
-    }
-    __syncthreads();
-    before = all = over = 0;
-#pragma unroll
-    for (int w = 0; w < kBookThreads / kWave; ++w) {
-        before += s[0][w];
-        all += s[1][w];
-        over += s[2][w];
-    }
     const long long short_of = (all > free_pages ? all - free_pages : 0) + over;
     if (report && tid == 0)
         missing[0] = short_of > 0x7fffffff ? 0x7fffffff : (int)short_of;
     if (short_of || (part > 0 && shared < 0))
         return;
-    const int length = a.lengths[slot] < 0 ? 0 : a.lengths[slot];
     if (shared >= 0)
         copy_page_part(p, shared, plan.free_ids[before], part);
     if (part > 0 || wanted <= length)
@@ -596,7 +629,8 @@ extern "C" size_t lookat_pages_reserve_workspace_bytes(const lookat_page_pool *p
     clear_error();
     if (check_pool(pool) != LOOKAT_OK || S <= 0)
         return 0;
-    return ((size_t)pool->pages + 2 * (size_t)S + 4) * sizeof(int32_t);
+    // (count, sums, need, shared, before, free_ids)
+    return ((size_t)pool->pages + 3 * (size_t)S + 4) * sizeof(int32_t) + ((size_t)S + kRankThreads - 1) / kRankThreads * 2 * sizeof(long long);
 }
 
 extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int32_t *table, int32_t W, int64_t table_stride, int32_t *lengths,
@@ -619,9 +653,12 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
     const BookArgs a = book_args(pool, S, table, W, table_stride, lengths, refs);
     ReservePlan plan;
     plan.count = static_cast<int32_t *>(workspace);
-    plan.need = plan.count + 4;
+    const int groups = (S + kRankThreads - 1) / kRankThreads;
+    plan.sums = reinterpret_cast<long long *>(plan.count + 4);
+    plan.need = reinterpret_cast<int32_t *>(plan.sums + 2 * groups);
     plan.shared = plan.need + S;
-    plan.free_ids = plan.shared + S;
+    plan.before = plan.shared + S;
+    plan.free_ids = plan.before + S;
     plan.copies = copies;
     int segment;
     const int segments = segments_of(p.pages, &segment);
@@ -629,7 +666,7 @@ extern "C" int lookat_pages_reserve(const lookat_page_pool *pool, int32_t S, int
     const int pieces = (p.pages + kRankThreads - 1) / kRankThreads;
     const auto rank = pieces <= 1 ? &pages_reserve_rank_kernel<1> : pieces <= 4 ? &pages_reserve_rank_kernel<4> : pieces <= 16 ? &pages_reserve_rank_kernel<16>
                     : pieces <= 64 ? &pages_reserve_rank_kernel<64> : &pages_reserve_rank_kernel<0>;
-    hipLaunchKernelGGL(rank, dim3((unsigned)(segments + (S + kRankThreads - 1) / kRankThreads)), dim3(kRankThreads), 0, st, a, new_lengths, plan,
+    hipLaunchKernelGGL(rank, dim3((unsigned)(segments + groups)), dim3(kRankThreads), 0, st, a, new_lengths, plan,
                        segments, segment);
     if (int rc = check_launch("lookat_pages_reserve (ranks)"))
         return rc;

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import pages_ref as pr
-from test_gpu_pages import dev, i32, lk, on_gpu, random_cache, random_table  # noqa: F401
+from test_gpu_pages import assert_pool, dev, i32, lk, on_gpu, random_cache, random_table, same_books  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,71 @@ def test_lists_as_long_as_there_can_be_sequences(lk):  # noqa: F811
     torch.cuda.synchronize()
     assert torch.all(lengths[:n] == 0) and torch.all(table[:n] == -1) and torch.all(refs[100: 100 + n] == 1) and int(refs.sum()) == n
     assert torch.all(lengths[n: 2 * n] > 0)
+
+
+@pytest.mark.parametrize("S", [1023, 1025, 5000, 65535])
+def test_reserve_for_many_sequences(lk, S):  # noqa: F811
+    """Needs that are summed up over several workgroups: pages in order over all sequences, shared last pages copied, rows that are too short and
+    pages that are too few reported."""
+    rng = np.random.default_rng(S)
+    W, page, half = 3, 16, S // 2
+    lengths = np.zeros(S, np.int32)
+    lengths[:half] = rng.integers(0, 2 * page + 1, half)
+    used = int((-(-lengths // page)).sum())
+    P = used + 2 * S
+    table = random_table(rng, lengths.tolist(), page, W, P)
+    shared = rng.random(half) < 0.5                       # the second half begins as some of the first
+    table[half: 2 * half][shared], lengths[half: 2 * half][shared] = table[:half][shared], lengths[:half][shared]
+    refs = np.bincount(table[table >= 0], minlength=P).astype(np.int32)
+    c = random_cache(rng, P, 1, 64, 2, page, "int8")
+    b, pool = pr.Books(table, lengths, refs, page), on_gpu(lk, c)
+    books = dev(table), dev(lengths), dev(refs)
+
+    def reserve(wanted, label):
+        copies = torch.full((2, S), -5, dtype=torch.int32, device="cuda")
+        was = b.table.copy()
+        missing = int(lk.lookat_pages_reserve(pool, *books, dev(wanted.astype(np.int32)), copies=copies))
+        assert missing == b.reserve(wanted, c), label
+        same_books(books, b)
+        assert_pool(pool, c)
+        moved = (was != b.table) & (was >= 0)
+        s, w = np.nonzero(moved)
+        pairs = np.full((2, S), -1)
+        pairs[0, s], pairs[1, s] = was[s, w], b.table[s, w]
+        assert np.array_equal(copies.cpu().numpy(), pairs), label
+        return missing
+
+    grow = lengths + rng.integers(-2, page + 2, S) * (rng.random(S) < 0.8)
+    short = grow.copy()
+    short[[0, S // 3, S - 1]] = [W * page + 1, 2 ** 31 - 1, W * page + page + 1]
+    assert reserve(short, "short rows") > 2 ** 26
+    assert reserve(grow, "a token too many in the fullest rows") == int((grow > W * page).sum())
+    assert reserve(np.minimum(grow, W * page), "room") == 0
+    # all but a few of the pages taken by others: nothing is changed
+    need = int((-(-W * page // page) - -(-b.lengths // page)).sum())
+    free = np.flatnonzero(b.refs == 0)
+    b.refs[free[: len(free) - need + 5]] += 1
+    books[2].copy_(dev(b.refs))
+    assert reserve(np.full(S, W * page), "few pages") >= 5
+
+
+def test_the_books_work_grows_with_the_number_of_sequences(lk):  # noqa: F811
+    """Four times the sequences, all growing into a new page: four times the workgroups, each with the same work (if each looked at all of the
+    sequences, sixteen times: it took twelve)."""
+    best = []
+    for S in (16384, 65535):
+        pool = lk.page_pool(S, 1, 64, 2, 16)
+        table, zeros = torch.full((S, 1), -1, dtype=torch.int32, device="cuda"), torch.zeros(S, dtype=torch.int32, device="cuda")
+        ones, missing = torch.ones_like(zeros), torch.empty(1, dtype=torch.int32, device="cuda")
+        times = []
+        for _ in range(8):
+            lengths, refs = zeros.clone(), zeros.clone()
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            lk.lookat_pages_reserve(pool, table, lengths, refs, ones, missing)
+            end.record()
+            torch.cuda.synchronize()
+            assert int(missing) == 0 and int(refs.sum()) == S and torch.equal(table[:, 0], torch.arange(S, device="cuda", dtype=torch.int32))
+            times.append(begin.elapsed_time(end))
+        best.append(min(times))
+    assert best[1] < 7 * best[0], best
