@@ -775,6 +775,8 @@ def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, 
     c_pool = _pool(pool)
     B, W, stride, t_ptr = _table(table, "table", pool)
     H, d_k, m = c_pool.H, c_pool.d_k, c_pool.m
+    if not H:
+        raise ValueError("the pool has no heads")
     if lut.dim() != 4 or lut.shape[0] != B or lut.shape[1] % H or tuple(lut.shape[2:]) != (m, 256) or lut.dtype != torch.float32 \
             or not lut.is_contiguous():
         raise ValueError("lut must be contiguous fp32 [B,H*g,m,256]")

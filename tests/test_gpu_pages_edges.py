@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import pages_ref as pr
-from test_gpu_pages import assert_pool, dev, i32, lk, on_gpu, random_cache, random_table, same_books  # noqa: F401
+from test_gpu_pages import Watch, assert_pool, dev, i32, lk, on_gpu, random_cache, random_table, same_books  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -193,3 +193,24 @@ def test_the_books_work_grows_with_the_number_of_sequences(lk):  # noqa: F811
             times.append(begin.elapsed_time(end))
         best.append(min(times))
     assert best[1] < 7 * best[0], best
+
+
+# ---- pools without anything in them -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("pages,H,d_k,m,page", [(0, 2, 64, 4, 16), (10, 0, 64, 4, 16), (10, 2, 0, 4, 16), (10, 2, 64, 0, 16), (10, 2, 64, 4, 0)])
+def test_empty_pools_are_refused(lk, monkeypatch, native, pages, H, d_k, m, page):  # noqa: F811
+    from paper_2601_10155_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_marshal", Watch(None))
+    pool = lk.page_pool(pages, H, d_k, m, page)
+    table, n, refs = torch.full((3, 4), -1, dtype=torch.int32, device="cuda"), i32(0, 0, 0), torch.zeros(pages, dtype=torch.int32, device="cuda")
+    lut = torch.zeros((3, 2, m, 256), device="cuda")
+    codes, values = torch.zeros((3, H, 1, m), dtype=torch.uint8, device="cuda"), torch.zeros((3, H, 1, d_k), device="cuda")
+    for call in (lambda: lk.lookat_attend_pages(lut, pool, table, n, 1.0), lambda: lk.lookat_attend_pages(lut[:, :H].contiguous(), pool, table, n, 1.0),
+                 lambda: lk.lookat_pages_write(pool, codes, values, table, n), lambda: lk.lookat_pages_copy(pool, n, n),
+                 lambda: lk.lookat_pages_fork(pool, table, n, refs, n, n), lambda: lk.lookat_pages_free(pool, table, n, refs, n),
+                 lambda: lk.lookat_pages_reserve(pool, table, n, refs, i32(1, 1, 1)), lambda: lk.lookat_pages_compact(pool, table, n, refs)):
+        with pytest.raises((ValueError, lk.LookatError)):
+            call()
+    torch.cuda.synchronize()
+    assert torch.all(table == -1) and torch.all(n == 0)
