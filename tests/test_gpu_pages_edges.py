@@ -6,7 +6,9 @@ import pytest
 import torch
 
 import pages_ref as pr
+from bars import record
 from test_gpu_pages import Watch, assert_pool, dev, i32, lk, on_gpu, random_cache, random_table, same_books  # noqa: F401
+from test_pages_weights import FORMS, LENGTHS, weights_case, weights_reference
 
 pytestmark = pytest.mark.gpu
 
@@ -214,3 +216,18 @@ def test_empty_pools_are_refused(lk, monkeypatch, native, pages, H, d_k, m, page
             call()
     torch.cuda.synchronize()
     assert torch.all(table == -1) and torch.all(n == 0)
+
+
+# ---- what a weight is worth -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group,d_k,m", FORMS)
+def test_attend_weights_have_two_terms(lk, group, d_k, m, kind):  # noqa: F811
+    c, table, lut = weights_case(group, d_k, m, kind)
+    ref, bound = weights_reference(c, table, lut)
+    for kw in ({}, {"max_length": 5000, "W": 100}, {"num_splits": 2}):
+        wide = np.full((len(LENGTHS), kw.pop("W", 1)), -1, np.int32)
+        wide[:, :1] = table
+        out = lk.lookat_attend_pages(dev(lut), on_gpu(lk, c), dev(wide), i32(*LENGTHS), 1.0, **kw).cpu().numpy()
+        off = np.abs(out - ref)
+        record("attend_pages, weights (of the close bound)", float(np.max(off / np.maximum(bound, 1e-30))))
+        assert np.all(off <= bound), f"{np.max(off / np.maximum(bound, 1e-30))} times the bound"
