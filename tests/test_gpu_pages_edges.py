@@ -1,5 +1,7 @@
 """The paged cache on the GPU at the edges: tables that are not finite, the ends of fp32, many sequences, what a weight has to be worth."""
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -231,3 +233,33 @@ def test_attend_weights_have_two_terms(lk, group, d_k, m, kind):  # noqa: F811
         off = np.abs(out - ref)
         record("attend_pages, weights (of the close bound)", float(np.max(off / np.maximum(bound, 1e-30))))
         assert np.all(off <= bound), f"{np.max(off / np.maximum(bound, 1e-30))} times the bound"
+
+
+# ---- the timed cases' search step, over several passes ------------------------------------------------------------------
+@pytest.mark.parametrize("case", [
+    {"S": 16, "fan": 4, "L": 1000, "ragged": 0.2, "H": 3, "d_k": 64, "m": 4, "page": 16, "type": "int8"},
+    {"S": 75, "fan": 2, "L": 333, "ragged": 0.9, "H": 2, "d_k": 128, "m": 8, "page": 64, "type": "float8"},
+    {"S": 9, "fan": 1, "L": 32, "ragged": 0.0, "H": 1, "d_k": 64, "m": 2, "page": 32, "type": "int8"}])
+def test_search_steps_that_give_up_real_children(lk, case):  # noqa: F811
+    """perf/operators.py's search step three times over: from the second pass on the children that are given up hold pages.  Its plain form
+    beside it, books and pools equal after each."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "perf", "operators.py")
+    spec = importlib.util.spec_from_file_location("operators_of_the_paged_cache", path)
+    operators = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(operators)
+    case = {"kind": "turn", "spare": 1.5, **case}
+    here, plain = operators.prepare(case, 1), operators.prepare(case, 1)
+    for n in range(3):
+        held = here["lengths"][case["S"]:] > 0
+        assert torch.all(held) if n else not torch.any(held)
+        results = []
+        for operators.own, state in ((True, here), (False, plain)):
+            out = operators.run(state)
+            results.append([out["table"], out["lengths"], out["refs"], out["missing"], *(out["pool"][k].view(torch.uint8) for k in ("codes", "values", "exponents"))])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(*results)), f"pass {n}"
+        assert int(results[0][3]) == 0
+        # other parents: a child may take over a longer or a shorter beginning than the one it had
+        for state in (here, plain):
+            state["parents"] = state["parents"].roll(1).contiguous()
+            state["wanted"][case["S"]:] = state["lengths"][state["parents"].long()] + 1
