@@ -58,10 +58,13 @@ constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, b
 // groups of 8, m = 8: 9.2 / 10.9).
 constexpr int kAttendWaves = 8, kShortWaves = 4;
 __host__ __device__ constexpr bool few_waves(int G, int m, int64_t longest) { return G * m < 64 && longest <= kShortWaves * kTile; }
-// Wavefronts to a SIMD that the registers have to allow: six (80 registers) where they do without spilling; us, four / six: d_k = 64, groups of 2
-// x 32 x 6 x 4096, m = 8 18.3 / 17.0, 16 x 12 x 4096, m = 16 e4m3 18.9 / 17.0, m = 4 14.9 / 14.9; groups of 4 x 16 x 4 x 8192 13.4 / 13.8.
+// Wavefronts to a SIMD that the registers have to allow.  Six (80 registers) at d_k = 64 for one or two query heads, whose instances fit, but for
+// two heads at m = 8: those spill 2 to 6 registers and gain all the same.  us, four / six: groups of 2 x 32 x 6 x 4096, m = 8 int8 18.1 / 17.0,
+// e4m3 18.1 / 16.6, 16 x 12 x 4096, m = 16 e4m3 18.9 / 17.0, m = 4 14.9 / 14.9.  Not two heads at m = 16, which would spill up to 8 (x 32 x 6 x 4096
+// 21.9 / 22.2, x 8 x 6 x 32768 34.4 / 35.6, x 32 x 6 x 700 7.3 / 7.8), nor four heads (16 x 4 x 8192 13.4 / 13.8).
 // Two where 128 KB of tables leave room for one workgroup only: the other registers hold look-ups in flight (8 x 4 x 65536 84.5 / 81.6).
-__host__ __device__ constexpr int min_waves(int d_k, int m, int G) { return G * m >= 128 ? 2 : d_k == 64 && G <= 2 ? 6 : 4; }
+// (At four, 128 registers, two heads at d_k = 128, m = 16 spill 3 or 4; with more registers one workgroup would have the compute unit to itself.)
+__host__ __device__ constexpr int min_waves(int d_k, int m, int G) { return G * m >= 128 ? 2 : d_k == 64 && G <= 2 && G * m <= 16 ? 6 : 4; }
 // Tables of 32 KB and more: every range fetches them, so there are as many ranges as the chip holds at once and no second round (see cut_of).
 __host__ __device__ constexpr bool one_round(int m, int G) { return G * m >= 32; }
 constexpr int kMostPlanned = 1024;        // sequences whose ranges are cut by their lengths
