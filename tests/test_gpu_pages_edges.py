@@ -89,6 +89,31 @@ def test_attend_minus_infinity_is_a_token_without_weight(lk, kind, group, d_k, m
 
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 @pytest.mark.parametrize("group,d_k,m", [(1, 64, 4), (2, 128, 8), (4, 64, 2), (8, 128, 8)])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_attend_table_entries_that_no_token_has(lk, kind, group, d_k, m, value):  # noqa: F811
+    """Every entry that no token of the sequence looks up is not finite; what lies behind the last token and in the pool's first page (which lanes
+    without a token read) has such codes."""
+    rng = np.random.default_rng(group + d_k + m)
+    lengths, H, page = [70, 1, 33, 0, 130, 64], 2, 32
+    c = random_cache(rng, 20, H, d_k, m, page, kind)
+    table = random_table(rng, lengths, page, 6, 19) + 1   # (page 0 is nobody's)
+    table[table == 0] = -1
+    table[4, 2] = 20                                      # a hole: tokens 64 to 95
+    c.codes[:] |= 1
+    c.codes[0] = 0
+    for b, n in enumerate(lengths):
+        if n % page:
+            c.codes[table[b, n // page], :, n % page:] &= 0xfe
+    lut = (rng.standard_normal((len(lengths), H * group, m, 256)) * 2).astype(np.float32)
+    ref, bound = c.attend(lut, table, lengths, 0.1)
+    lut[..., ::2] = value                                 # the tokens' codes are odd
+    for kw in CUTS:
+        out = lk.lookat_attend_pages(dev(lut), on_gpu(lk, c), dev(table), i32(*lengths), 0.1, **kw).cpu().numpy()
+        assert np.all(np.abs(out - ref) <= bound), kw
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("group,d_k,m", [(1, 64, 4), (2, 128, 8), (4, 64, 2), (8, 128, 8)])
 @pytest.mark.parametrize("level", [-2.0e38, -2.1e38, -2.358e38, 2.358e38])
 def test_attend_equal_scores_at_the_ends_of_fp32(lk, kind, group, d_k, m, level):  # noqa: F811
     """Scores that are the same to the last bit are equal weights, down to the lowest number: the mean of the values.  All exponents are
