@@ -87,10 +87,11 @@ int lookat_pages_write(const lookat_page_pool *pool, int32_t B, int64_t N,
  * in fp32; a weight enters the product with the values as two fp16 terms (22 bits), the stored 8-bit numbers exactly.
  *   lut           [B, H*group, m, 256] fp32, 16-byte aligned, from lookat_build_lut
  *   max_length    the longest length the host knows of, or 0 for W * page: it sizes the launch alone; longer sequences are
- *                 right too
+ *                 right too.  Above 2048, sequences may be cut, which costs a second launch (3 to 4 us) in every call
  *   group         1, 2, 4 or 8, otherwise LOOKAT_ERR_UNSUPPORTED
- *   num_splits    0: the sequences are cut into ranges by their lengths, on the device, where they are long enough to gain from it; >= 1: that
- *                 many equal ranges of max_length per (b, key/value head).  The result does not depend on it beyond fp32 rounding
+ *   num_splits    0: the sequences are cut into ranges by their lengths, on the device, where they are long enough to gain from it and there
+ *                 are at most 1024 of them (more are not cut); >= 1: that many equal ranges of max_length per (b, key/value head).
+ *                 The result does not depend on it beyond fp32 rounding
  *   workspace     lookat_attend_pages_workspace_bytes(pool, B, group, W, max_length, num_splits) bytes, 16-byte aligned (NULL when 0);
  *                 calls in flight at once must not share one
  *   out           [B, H*group, d_k] fp32, 16-byte aligned
@@ -137,10 +138,10 @@ int lookat_pages_free(const lookat_page_pool *pool, int32_t S, int32_t *table, i
  * a page for every entry of its row that new tokens reach first, and one more if they begin inside a page that was counted more
  * than once when the call began: that page's content is copied to the new one, which takes its place in the row.
  * The needed entries, in row-major order of the table, get the free pages in ascending order, each counted once; the
- * lengths become the new ones.  If there are too few free pages, or a row is too short, NOTHING is changed and
+ * lengths become the new ones.  If there are too few free pages, or a row is too short for a page it needs, NOTHING is changed and
  * missing[0] says by how many pages, else missing[0] = 0.
  * (Of several sequences that share a last page and all grow, all get a copy; the page itself becomes free.)
- *   new_lengths  [S] int32, must not overlap lengths;  missing  [1] int32
+ *   new_lengths  [S] int32, must not overlap lengths;  missing  [1] int32.  Neither missing nor copies overlaps another array of the call
  *   copies       NULL, or [2, S] int32: copies[0,s] the page that was copied for sequence s and copies[1,s] the one it was copied to, -1
  *                where none was: what lookat_pages_copy takes to do the same in the pools of other layers that share these books
  *   workspace    lookat_pages_reserve_workspace_bytes(pool, S) bytes, 16-byte aligned

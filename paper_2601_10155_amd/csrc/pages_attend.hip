@@ -8,10 +8,11 @@
 // needs whatever the pages' exponents are, and no per-page rescaling is done.
 //
 // Bound: the stream of codes and values from HBM, m + d_k bytes per token and key/value head, where there is much of it: 8 x 32 x 32768
-// tokens (d_k = 128, m = 8, int8; 1.14 GB, fetched once) take 166 us in the kernel, 6.9 TB/s (a plain read of 1 GiB: 7.0 to 7.1), 169 a call.
+// tokens (d_k = 128, m = 8, int8; 1.14 GB, fetched once) take 165 us in the kernel, 6.9 TB/s (a plain read of 1 GiB: 7.0 to 7.1), 169 a call.
 // Below some 50 MB the chain of dependent steps counts instead: lengths, page id, codes and values, reduction, merge.  12 x 1024 tokens
-// (0.8 MB) 5.1 us in the kernel: 0.4 until the range is known, 0.3 until the first tile is requested, 1.5 until it is weighted, 1.2 for the
-// results.  12 x 8 x up to 8191 in groups of 8 (52 MB) 16.8 us and 3.8 for the merge: eight query heads are 270 vector instructions a tile.
+// (0.8 MB) 5.2 us in the kernel: 0.4 until the range is known, 0.3 until the first tile is requested, 1.5 until it is weighted, 1.2 for the
+// results.  12 x 8 x up to 8191 in groups of 8 (52 MB) 16.9 us and 3.8 for the merge: 224 ranges, one of eight wavefronts to a compute unit, whose
+// wavefronts take four tiles one after the other and wait for them during 61% of their cycles; vector issue (270 instructions a tile) is 5 us of it.
 //
 // Weighted sums on the matrix cores at every group, also for one query head: 1 + 1/2 vector instructions a stored value (int8; 1/2 in e4m3)
 // instead of 2.  What was tried and not kept: four or sixteen wavefronts to a workgroup (long contexts 178.9 / 179.8 us, eight 177.4, groups of 8

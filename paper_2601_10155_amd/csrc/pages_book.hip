@@ -4,9 +4,9 @@
 // to the host.  Every result is a function of the books alone: free pages are taken in ascending order by rank (a prefix sum over
 // the counts), never by an atomic race; the only atomics are integer additions to counts, whose order does not matter.
 //
-// What bounds these kernels is the launch and a few dependent memory round trips (the books are tens of kilobytes): free 3.2 us, fork 3.3, reserve
-// 3.1 + 5.2 (16 of 32 sequences) and 4.6 + 6.7 (192 of 384, 26 MB of shared last pages); where pages are copied, their bytes once read and once
-// written: 1024 pages of 70 KB 22.5 us (6.3 TB/s), compacting a pool of 16000 pages with 4000 moves 5.4 + 28.8 us (5.1 TB/s).
+// What bounds these kernels is the launch and a few dependent memory round trips (the books are tens of kilobytes): free 3.4 us, fork 3.5, reserve
+// 3.6 + 4.1 (16 of 32 sequences) and 4.6 + 5.5 (192 of 384, 26 MB of shared last pages); where pages are copied, their bytes once read and once
+// written: 1024 pages of 70 KB 22.4 us (6.4 TB/s), compacting a pool of 16000 pages with 4000 moves 5.2 + 28.8 us (5.1 TB/s).
 #include "pages.h"
 
 namespace lookat {
