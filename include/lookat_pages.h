@@ -109,6 +109,40 @@ int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int32_t group,
                         void *stream);
 
 /*
+ * Attention of a chunk of new tokens over the pages: pieces of prompts, drafted tokens to be verified.  Row n of sequence b, n < min(counts[b], N)
+ * (counts NULL: N for every b), stands at position p = lengths[b] - counts[b] + n, as in lookat_pages_write (which comes first: the rows' own
+ * tokens are read from the pages), and sees the tokens l <= p.  With k^ the key that a token's codes stand for (its centroids side by side):
+ *     s[b,hq,n,l]   = sum_j q[b,hq,n,j] * k^(b, hq/group, l)_j
+ *     out[b,hq,n,:] = sum_{l <= p} softmax_l(scale * s[b,hq,n,:]) * value(b, hq/group, l, :)
+ * A row that sees no token gives zeros, and so does one whose tokens all have a score of -inf; other rows of out are left as they were.  A NaN
+ * score or one of +inf makes its row NaN; other rows are not touched by it.  Centroids enter the product as two fp16 terms, scaled by one power
+ * of two per key/value head: exactly to 2^-22 of themselves, or to 2^-40 of the head's largest finite centroid entry where that is more; fp16
+ * queries exactly, fp32 queries to 2^-22 of themselves or 2^-40 of the row's largest entry; weights, sums and values as in lookat_attend_pages.  An
+ * infinite centroid entry makes the scores of the tokens that have it NaN; what centroids hold that no token has does not matter.
+ *   q             [B, H*group, N, d_k] fp16 or fp32: element (b,hq,n,j) at q[b*q_stride_b + hq*q_stride_h + n*q_stride_n + j]; base 16-byte
+ *                 aligned, strides multiples of 8 (fp16) or 4 (fp32) elements
+ *   codebooks     [H, m, 256, d_k/m] fp32, 16-byte aligned
+ *   max_length    as in lookat_attend_pages: it sizes the launch alone
+ *   group         1 to 64;  N * group at most 2^24, H * group at most 65535
+ *   num_splits    0: the library's choice; >= 1: the tokens that a tile of rows sees are cut into that many ranges, merged by another launch
+ *   workspace     lookat_attend_pages_chunk_workspace_bytes(pool, B, N, group, W, max_length, num_splits) bytes, 16-byte aligned; calls in flight
+ *                 at once must not share one
+ *   out           [B, H*group, N, d_k] fp32, 16-byte aligned
+ */
+size_t lookat_attend_pages_chunk_workspace_bytes(const lookat_page_pool *pool, int32_t B, int32_t N, int32_t group, int32_t W,
+                                                 int64_t max_length, int32_t num_splits);
+
+int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B, int32_t N, int32_t group,
+                              const void *q, lookat_dtype q_dtype, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                              const float *codebooks,
+                              const int32_t *table, int32_t W, int64_t table_stride,
+                              const int32_t *lengths, const int32_t *counts, int64_t max_length,
+                              float scale, int32_t num_splits,
+                              void *workspace, size_t workspace_bytes,
+                              float *out,
+                              void *stream);
+
+/*
  * Copies pages src[i] onto pages dst[i] (codes, values, exponents), i < n.  Pairs with an id outside [0, pages) or with
  * src = dst are passed over.  No page may be a destination twice, or both a source and a destination (its content would be
  * unspecified).

@@ -116,6 +116,11 @@ def load_library():
         lib.lookat_attend_pages_workspace_bytes.restype = sz
         lib.lookat_attend_pages.argtypes = [pp, i32, i32, vp, vp, i32, i64, vp, i64, f32, i32, vp, sz, vp, vp]
         lib.lookat_attend_pages.restype = ctypes.c_int
+        lib.lookat_attend_pages_chunk_workspace_bytes.argtypes = [pp, i32, i32, i32, i32, i64, i32]
+        lib.lookat_attend_pages_chunk_workspace_bytes.restype = sz
+        lib.lookat_attend_pages_chunk.argtypes = [pp, i32, i32, i32, vp, ctypes.c_int, i64, i64, i64, vp, vp, i32, i64, vp, vp, i64, f32, i32, vp, sz,
+                                                  vp, vp]
+        lib.lookat_attend_pages_chunk.restype = ctypes.c_int
         lib.lookat_pages_copy.argtypes = [pp, i32, vp, vp, vp]
         lib.lookat_pages_copy.restype = ctypes.c_int
         lib.lookat_pages_fork.argtypes = [pp, i32, vp, i32, i64, vp, vp, i32, vp, vp, vp]
@@ -793,6 +798,57 @@ def lookat_attend_pages(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, 
         workspace = _scratch(workspace, need, pool)
         _check(lib.lookat_attend_pages(ctypes.byref(c_pool), B, g, lut.data_ptr(), t_ptr, W, stride, l_ptr, int(max_length), float(scale),
                                        int(num_splits), _ptr(workspace), _bytes(workspace), out.data_ptr(), stream))
+    return out
+
+
+def attend_pages_chunk_workspace_bytes(pool: PagePool, B: int, N: int, group: int, W: int, max_length: int = 0, num_splits: int = 0) -> int:
+    return int(load_library().lookat_attend_pages_chunk_workspace_bytes(ctypes.byref(_pool(pool)), B, N, group, W, max_length, num_splits))
+
+
+def lookat_attend_pages_chunk(q: torch.Tensor, codebooks: torch.Tensor, pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, scale: float,
+                              counts: torch.Tensor | None = None, max_length: int = 0, num_splits: int = 0,
+                              workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """q [B,H*g,N,d_k] fp16|fp32 (rows dense, other strides as they are: a transposed [B,N,H*g,d_k] is taken without a copy), codebooks
+    [H,m,256,d_k/m] fp32, table [B,W] int32, lengths [B] int32 INCLUDING the chunk's tokens, which the pages hold already, counts [B] int32 (None: N)
+    -> out [B,H*g,N,d_k] fp32: row n of sequence b, at position lengths[b] - counts[b] + n, attends over the tokens up to its own.  Rows from
+    counts[b] on are left as they were (zeros if out is not given).  max_length: as in lookat_attend_pages."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    B, W, stride, t_ptr = _table(table, "table", pool)
+    H, d_k, m = c_pool.H, c_pool.d_k, c_pool.m
+    if not H:
+        raise ValueError("the pool has no heads")
+    if q.dim() != 4 or q.shape[0] != B or not q.shape[1] or q.shape[1] % H or q.shape[3] != d_k:
+        raise ValueError("q must be [B,H*g,N,d_k] with a row of table for every sequence")
+    tag = _dtype_tag(q)
+    Hq, N = q.shape[1], q.shape[2]
+    if codebooks.dtype != torch.float32 or tuple(codebooks.shape) != (H, m, 256, d_k // m) or not codebooks.is_contiguous():
+        raise ValueError("codebooks must be contiguous fp32 [H,m,256,d_k/m] of the pool's heads")
+    if q.device != pool.codes.device or codebooks.device != pool.codes.device:
+        raise ValueError("q and codebooks must live on the pool's device")
+    l_ptr = _int_array(lengths, "lengths", pool, B)
+    n_ptr = None if counts is None else _int_array(counts, "counts", pool, B)
+    unit = 16 // q.element_size()
+    if q.stride(3) != 1 or q.data_ptr() % 16 or any(q.shape[i] > 1 and q.stride(i) % unit for i in range(3)):
+        q = q.contiguous()
+    if q.data_ptr() % 16:
+        q = q.clone()
+    # (a stride that no index uses may be anything)
+    sb, sh, sn = (q.stride(i) if q.shape[i] > 1 else 0 for i in range(3))
+    if out is None:
+        out = (torch.empty if counts is None else torch.zeros)((B, Hq, N, d_k), dtype=torch.float32, device=pool.codes.device)
+    if out.dtype != torch.float32 or tuple(out.shape) != (B, Hq, N, d_k) or not out.is_contiguous():
+        raise ValueError("out must be contiguous fp32 [B,H*g,N,d_k]")
+    if out.device != pool.codes.device:
+        raise ValueError("out must live on the pool's device")
+    if not N or not B:
+        return out
+    with _OnDevice(pool) as stream:
+        need = lib.lookat_attend_pages_chunk_workspace_bytes(ctypes.byref(c_pool), B, N, Hq // H, W, max_length, num_splits)
+        workspace = _scratch(workspace, need, pool)
+        _check(lib.lookat_attend_pages_chunk(ctypes.byref(c_pool), B, N, Hq // H, q.data_ptr(), tag, sb, sh, sn, codebooks.data_ptr(), t_ptr, W, stride,
+                                             l_ptr, n_ptr, int(max_length), float(scale), int(num_splits), _ptr(workspace), _bytes(workspace),
+                                             out.data_ptr(), stream))
     return out
 
 

@@ -13,6 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblookat.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 OBJ_DIR = os.path.join(PKG, "_build")
+HEADERS = ("lookat.h", "lookat_pages.h")
 
 # -packed-fp32-ops off: keeps the compiler from forming packed fp32 instructions.
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
@@ -61,14 +62,14 @@ def build(verbose: bool = True, force: bool = True) -> str:
         objs.append(obj)
         path = os.path.join(CSRC, src)
         deps = [path] + [os.path.join(CSRC, h) for h in os.listdir(CSRC) if h.endswith(".h")] + \
-               [os.path.join(ROOT, "include", h) for h in ("lookat.h", "lookat_pages.h")]
+               [os.path.join(ROOT, "include", h) for h in HEADERS]
         if not force and os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
             continue
         cmd = [cc, *COMMON, *EXTRA.get(src, []), "-c", path, "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    deps = [os.path.join(CSRC, "marshal.cpp")] + [os.path.join(ROOT, "include", h) for h in ("lookat.h", "lookat_pages.h")]
+    deps = [os.path.join(CSRC, "marshal.cpp")] + [os.path.join(ROOT, "include", h) for h in HEADERS]
     if force or not (os.path.exists(MARSHAL) and all(os.path.getmtime(MARSHAL) >= os.path.getmtime(d) for d in deps)):
         cmd = marshal_command()
         if verbose:

@@ -28,13 +28,10 @@
 //     of query head n rounded to fp16, columns G..2G-1 what that left (22 bits together), the other columns repeat them.  Each lane's
 //     operand is eight tokens of one coordinate: eight consecutive bytes of the page as it is stored, widened to fp16 in registers.  The weights
 //     go from a lane per token to that layout through 2 KB of LDS per wavefront.
-#include "pages.h"
-#include "decode_common.h"
+#include "pages_values.h"
 
 namespace lookat {
 
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 
 struct AttendArgs {
@@ -50,9 +47,6 @@ struct AttendArgs {
     float scale_log2e;
 };
 
-constexpr float kRefLag = 8.f;            // the reference moves when a logit exceeds it by more (log2 units)
-constexpr float kNoReference = -3.402823466e38f;   // before the first token: fp32's lowest, so no logit is below it, and finite: -inf less it is -inf
-constexpr float kRefLift = 7.f;           // weights are 2^7 at the reference, below 2^15: fp16's range, its subnormals far below
 // Wavefronts of a workgroup: eight of 128 registers, two workgroups to a compute unit.  Four where no sequence is longer than four tiles: the
 // others would only take room from the next workgroups (us, eight / four: 42 x 32 x 157 tokens in groups of 2 15.0 / 10.7, 64 x 32 x 250
 // 14.1 / 11.2, 27 x 32 x 2 in groups of 4 12.3 / 9.9, a few heads the same), unless there are 64 KB of tables to fetch (32 x 8 x 200 in
@@ -199,33 +193,6 @@ __device__ __forceinline__ bool range_by_length(const AttendArgs &a, int H, int 
     __syncthreads();                                      // (s is free again)
     set_range(r, at, place, mine, length, c, index);
     return true;
-}
-
-// Eight stored bytes (two registers) to eight fp16 numbers, exactly.
-template <bool FP8>
-__device__ __forceinline__ v8h widen(uint32_t lo, uint32_t hi)
-{
-    uint32_t w[4];
-    if constexpr (FP8) {
-        const v2h a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
-        const v2h c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-        w[0] = __builtin_bit_cast(uint32_t, a);
-        w[1] = __builtin_bit_cast(uint32_t, b);
-        w[2] = __builtin_bit_cast(uint32_t, c);
-        w[3] = __builtin_bit_cast(uint32_t, d);
-    } else {
-        // q + 128 behind the exponent byte of 1024: 1024 + 128 + q, less 1152
-        const v2h bias = {(_Float16)-1152.f, (_Float16)-1152.f};
-        lo ^= 0x80808080u;
-        hi ^= 0x80808080u;
-        const uint32_t u[4] = {__builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u),
-                               __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = __builtin_bit_cast(uint32_t, (v2h)(__builtin_bit_cast(v2h, u[i]) + bias));
-    }
-    const v4u r = {w[0], w[1], w[2], w[3]};
-    return __builtin_bit_cast(v8h, r);
 }
 
 template <int CTRL>
