@@ -143,6 +143,58 @@ int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B, int32_t N
                               void *stream);
 
 /*
+ * Adds up the attention that every token is paid, from the tables of the newest queries (those that lookat_attend_pages takes), for a cache that
+ * is held to a budget:
+ *     weights[b,h,l] = decay * weights[b,h,l] + sum_g softmax_l(scale * s[b, h*group + g, :])        l < min(lengths[b], columns)
+ * with s as in lookat_attend_pages.  The maximum and the sum of a softmax are taken over all of the sequence's tokens.  decay 0 takes no notice of what
+ * weights held.  A token in a page outside the pool, and a query head whose tokens all have a score of -inf, add nothing; a NaN score or one
+ * of +inf makes the weights of its key/value head NaN (that sequence's).  Weights behind a sequence's last token are left as they were.  Every weight
+ * has one writer and its sum one order: results are reproducible bit for bit.
+ *   lut           [B, H*group, m, 256] fp32, 16-byte aligned;  group 1, 2, 4 or 8
+ *   weights       element (b,h,l) at weights[(b*H+h)*weight_stride_bh + l], l < columns <= weight_stride_bh
+ *   max_length    the longest length the host knows of, or 0 for W * page: it sizes the launch alone
+ *   workspace     lookat_pages_weigh_workspace_bytes(pool, B, group, W, max_length) bytes, 16-byte aligned (NULL when 0); calls in flight at once
+ *                 must not share one
+ * The pool's values are not read.
+ */
+size_t lookat_pages_weigh_workspace_bytes(const lookat_page_pool *pool, int32_t B, int32_t group, int32_t W, int64_t max_length);
+
+int lookat_pages_weigh(const lookat_page_pool *pool, int32_t B, int32_t group,
+                       const float *lut,
+                       const int32_t *table, int32_t W, int64_t table_stride,
+                       const int32_t *lengths, int64_t max_length,
+                       float scale, float decay,
+                       float *weights, int32_t columns, int64_t weight_stride_bh,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Keeps k = min(lengths[b], keep[b]) tokens of every sequence b (at least 0, at most W_out * page), each key/value head its own: the last `recent`
+ * tokens (k at most), the first `first` (what is left at most), and of the others the heaviest, among equal weights those of the lowest positions.  NaN
+ * counts as less than any weight, both zeros as equal; tokens from `columns` on weigh 0.  The kept tokens enter the pages of row b of table_out
+ * at positions 0..k-1, in their order, as if lookat_pages_write wrote the values that they stand for into an empty sequence: a page's exponent is
+ * the least that its tokens allow, so a token is rounded only where its exponent grows, by half a step of the new one at most.  What these
+ * pages have behind the last token stays as it was; table, lengths and the books are not changed.  So a user reserves k tokens for an empty slot, calls
+ * this with its row, and frees the old slot: pages shared with other sequences are read, not written.
+ * No page of table_out may be named twice or be one that is read.  A kept token in a page outside the pool leaves its place as it was, and so do
+ * those whose place is in one.
+ *   weights       as in lookat_pages_weigh, read;  keep [B] int32;  first, recent >= 0
+ *   table_out     [B, W_out] int32, rows table_out_stride >= W_out apart
+ *   weights_out   NULL, or element (b,h,j) at weights_out[(b*H+h)*weight_out_stride_bh + j], j < columns_out: the kept tokens' weights, in their
+ *                 new places; must not overlap weights
+ *   workspace     lookat_pages_evict_workspace_bytes(pool, B, W_out) bytes, 16-byte aligned: afterwards the kept positions, [B, H, W_out * page]
+ *                 int32, of which the first k of each head are set; calls in flight at once must not share one
+ */
+size_t lookat_pages_evict_workspace_bytes(const lookat_page_pool *pool, int32_t B, int32_t W_out);
+
+int lookat_pages_evict(const lookat_page_pool *pool, int32_t B,
+                       const int32_t *table, int32_t W, int64_t table_stride, const int32_t *lengths,
+                       const float *weights, int32_t columns, int64_t weight_stride_bh,
+                       const int32_t *keep, int32_t first, int32_t recent,
+                       const int32_t *table_out, int32_t W_out, int64_t table_out_stride,
+                       float *weights_out, int32_t columns_out, int64_t weight_out_stride_bh,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Copies pages src[i] onto pages dst[i] (codes, values, exponents), i < n.  Pairs with an id outside [0, pages) or with
  * src = dst are passed over.  No page may be a destination twice, or both a source and a destination (its content would be
  * unspecified).

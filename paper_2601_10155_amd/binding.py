@@ -121,6 +121,18 @@ def load_library():
         lib.lookat_attend_pages_chunk.argtypes = [pp, i32, i32, i32, vp, ctypes.c_int, i64, i64, i64, vp, vp, i32, i64, vp, vp, i64, f32, i32, vp, sz,
                                                   vp, vp]
         lib.lookat_attend_pages_chunk.restype = ctypes.c_int
+        lib.lookat_pages_weigh_workspace_bytes.argtypes = [pp, i32, i32, i32, i64]
+        lib.lookat_pages_weigh_workspace_bytes.restype = sz
+        lib.lookat_pages_weigh.argtypes = [pp, i32, i32, vp, vp, i32, i64, vp, i64, f32, f32, vp, i32, i64, vp, sz, vp]
+        lib.lookat_pages_weigh.restype = ctypes.c_int
+        lib.lookat_pages_evict_workspace_bytes.argtypes = [pp, i32, i32]
+        lib.lookat_pages_evict_workspace_bytes.restype = sz
+        lib.lookat_pages_evict.argtypes = [pp, i32, vp, i32, i64, vp, vp, i32, i64, vp, i32, i32, vp, i32, i64, vp, i32, i64, vp, sz, vp]
+        lib.lookat_pages_evict.restype = ctypes.c_int
+        lib.lookat_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.lookat_beam_select_workspace_bytes.restype = sz
+        lib.lookat_beam_select.argtypes = [i32, i32, i32, i32, vp, ctypes.c_int, i64, vp, i32, vp, vp, vp, vp, sz, vp]
+        lib.lookat_beam_select.restype = ctypes.c_int
         lib.lookat_pages_copy.argtypes = [pp, i32, vp, vp, vp]
         lib.lookat_pages_copy.restype = ctypes.c_int
         lib.lookat_pages_fork.argtypes = [pp, i32, vp, i32, i64, vp, vp, i32, vp, vp, vp]
@@ -852,6 +864,73 @@ def lookat_attend_pages_chunk(q: torch.Tensor, codebooks: torch.Tensor, pool: Pa
     return out
 
 
+def _weight_rows(t: torch.Tensor, name: str, pool: PagePool, B: int, H: int) -> tuple[int, int, int]:
+    """Columns, stride between heads and address of fp32 weights [B,H,N] whose rows are dense."""
+    if t.dtype != torch.float32 or t.dim() != 3 or tuple(t.shape[:2]) != (B, H) or not t.shape[2]:
+        raise ValueError(f"{name} must be fp32 [B,H,N] of the pool's heads")
+    if t.device != pool.codes.device:
+        raise ValueError(f"{name} must live on the pool's device")
+    return t.shape[2], _bh_stride(t.unsqueeze(2), name), t.data_ptr()
+
+
+def pages_weigh_workspace_bytes(pool: PagePool, B: int, group: int, W: int, max_length: int = 0) -> int:
+    return int(load_library().lookat_pages_weigh_workspace_bytes(ctypes.byref(_pool(pool)), B, group, W, max_length))
+
+
+def lookat_pages_weigh(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, scale: float, weights: torch.Tensor,
+                       decay: float = 1.0, max_length: int = 0, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Adds the attention that the queries of lut [B,H*g,m,256] (as lookat_attend_pages takes it) pay to every token, summed over a key/value
+    head's g query heads, to decay * weights [B,H,N] fp32 (N >= the longest length, or only the first N tokens have one).  In place; returns weights."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    B, W, stride, t_ptr = _table(table, "table", pool)
+    H, m = c_pool.H, c_pool.m
+    if not H:
+        raise ValueError("the pool has no heads")
+    if lut.dim() != 4 or lut.shape[0] != B or not lut.shape[1] or lut.shape[1] % H or tuple(lut.shape[2:]) != (m, 256) or lut.dtype != torch.float32 \
+            or not lut.is_contiguous():
+        raise ValueError("lut must be contiguous fp32 [B,H*g,m,256]")
+    if lut.device != pool.codes.device:
+        raise ValueError("lut must live on the pool's device")
+    l_ptr = _int_array(lengths, "lengths", pool, B)
+    if not B:
+        return weights
+    columns, w_stride, w_ptr = _weight_rows(weights, "weights", pool, B, H)
+    g = lut.shape[1] // H
+    with _OnDevice(pool) as stream:
+        workspace = _scratch(workspace, lib.lookat_pages_weigh_workspace_bytes(ctypes.byref(c_pool), B, g, W, max_length), pool)
+        _check(lib.lookat_pages_weigh(ctypes.byref(c_pool), B, g, lut.data_ptr(), t_ptr, W, stride, l_ptr, int(max_length), float(scale), float(decay),
+                                      w_ptr, columns, w_stride, _ptr(workspace), _bytes(workspace), stream))
+    return weights
+
+
+def pages_evict_workspace_bytes(pool: PagePool, B: int, W_out: int) -> int:
+    return int(load_library().lookat_pages_evict_workspace_bytes(ctypes.byref(_pool(pool)), B, W_out))
+
+
+def lookat_pages_evict(pool: PagePool, table: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor, keep: torch.Tensor,
+                       table_out: torch.Tensor, first: int = 0, recent: int = 0, weights_out: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None) -> None:
+    """min(lengths[b], keep[b]) tokens of every sequence, each head its own - the last `recent`, the first `first`, then the heaviest of weights
+    [B,H,N] fp32 - enter the pages of table_out [B,W_out] int32 at positions 0.., in their order (keep [B] int32; reserve that many for empty slots
+    first, free the old ones afterwards).  weights_out [B,H,M] fp32, if given, gets the kept tokens' weights in their new places."""
+    lib = load_library()
+    c_pool = _pool(pool)
+    B, W, stride, t_ptr = _table(table, "table", pool)
+    rows, W_out, out_stride, o_ptr = _table(table_out, "table_out", pool)
+    if rows != B:
+        raise ValueError("table_out must have a row for every sequence")
+    l_ptr, k_ptr = _int_array(lengths, "lengths", pool, B), _int_array(keep, "keep", pool, B)
+    if not B:
+        return
+    columns, w_stride, w_ptr = _weight_rows(weights, "weights", pool, B, c_pool.H)
+    out = (0, 0, None) if weights_out is None else _weight_rows(weights_out, "weights_out", pool, B, c_pool.H)
+    with _OnDevice(pool) as stream:
+        workspace = _scratch(workspace, lib.lookat_pages_evict_workspace_bytes(ctypes.byref(c_pool), B, W_out), pool)
+        _check(lib.lookat_pages_evict(ctypes.byref(c_pool), B, t_ptr, W, stride, l_ptr, w_ptr, columns, w_stride, k_ptr, int(first), int(recent),
+                                      o_ptr, W_out, out_stride, out[2], out[0], out[1], _ptr(workspace), _bytes(workspace), stream))
+
+
 def lookat_pages_copy(pool: PagePool, src: torch.Tensor, dst: torch.Tensor) -> None:
     """Pages src[i] onto pages dst[i] (int32 [n]; the destinations distinct and none of them a source)."""
     rc = _native().pages_copy(pool, src, dst)
@@ -964,6 +1043,46 @@ def lookat_pages_compact(pool: PagePool, table: torch.Tensor, lengths: torch.Ten
         _check(lib.lookat_pages_compact(ctypes.byref(c_pool), *books, t_ptr, stride, r_ptr, l_ptr, _ptr(workspace), _bytes(workspace),
                                         device_stream))
     return table_out, refs_out, live
+
+
+# ---- beam search (include/lookat_search.h) ---------------------------------------------------------------------
+def beam_select_workspace_bytes(Q: int, beams: int, V: int, n: int) -> int:
+    return int(load_library().lookat_beam_select_workspace_bytes(Q, beams, V, n))
+
+
+def lookat_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, n: int, first_parent: int = 0, scores_out: torch.Tensor | None = None,
+                       parents: torch.Tensor | None = None, tokens: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The n best continuations of each request: logits [Q*beams,V] fp16|fp32 (rows dense), scores [Q*beams] fp32 -> scores [Q,n] fp32 =
+    scores + log_softmax(logits), falling, parents [Q,n] int32 (first_parent + row: the slots that lookat_pages_fork copies) and tokens [Q,n] int32;
+    -inf, -1, -1 where there are fewer.  Beams of score -inf and tokens of logit -inf are not chosen."""
+    lib = load_library()
+    device = _dev(logits, "logits").device
+    if logits.dim() != 2 or beams < 1 or n < 1 or not logits.shape[0] or logits.shape[0] % beams or not logits.shape[1]:
+        raise ValueError("logits must be [Q*beams,V]")
+    tag = _dtype_tag(logits)
+    (R, V), Q = logits.shape, logits.shape[0] // beams
+    if V > 1 and logits.stride(1) != 1 or (R > 1 and logits.stride(0) < V):
+        raise ValueError("logits: rows must be dense and apart")
+    if scores.dtype != torch.float32 or tuple(scores.shape) != (R,) or not scores.is_contiguous():
+        raise ValueError("scores must be contiguous fp32 [Q*beams]")
+    new = lambda t, dtype: torch.empty((Q, n), dtype=dtype, device=device) if t is None else t  # noqa: E731
+    scores_out, parents, tokens = new(scores_out, torch.float32), new(parents, torch.int32), new(tokens, torch.int32)
+    for t, name, dtype in ((scores_out, "scores_out", torch.float32), (parents, "parents", torch.int32), (tokens, "tokens", torch.int32)):
+        if t.dtype != dtype or tuple(t.shape) != (Q, n) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} [Q,n]")
+    if any(t.device != device for t in (scores, scores_out, parents, tokens)):
+        raise ValueError("all tensors must live on the logits' device")
+    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be contiguous and live on the logits' device")
+    with torch.cuda.device(device):
+        need = lib.lookat_beam_select_workspace_bytes(Q, beams, V, n)
+        if need and (workspace is None or _bytes(workspace) < need):
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        _check(lib.lookat_beam_select(Q, beams, V, n, logits.data_ptr(), tag, logits.stride(0) if R > 1 else V, scores.data_ptr(), int(first_parent),
+                                      scores_out.data_ptr(), parents.data_ptr(), tokens.data_ptr(), _ptr(workspace), _bytes(workspace),
+                                      torch._C._cuda_getCurrentRawStream(device.index)))
+    return scores_out, parents, tokens
 
 
 def lookat_probe_stream_read(src: torch.Tensor, sink: torch.Tensor) -> None:

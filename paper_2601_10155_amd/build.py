@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblookat.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 OBJ_DIR = os.path.join(PKG, "_build")
-HEADERS = ("lookat.h", "lookat_pages.h")
+HEADERS = ("lookat.h", "lookat_pages.h", "lookat_search.h")
 
 # -packed-fp32-ops off: keeps the compiler from forming packed fp32 instructions.
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

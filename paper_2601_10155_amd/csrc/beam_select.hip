@@ -1,0 +1,425 @@
+// Beam search's selection: the n best of  scores[r] + logit - log sum exp(logits[r])  over a request's beams and the vocabulary.
+//
+// Two launches.  In the first a wavefront takes 64 E consecutive logits of a row, E to a lane, in registers: their maximum m, their n best in order, and
+// the sum of exp(x - m) over the others.  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots);
+// few logits reach it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n, many equal logits) the n-th best
+// itself is found bit by bit, first its value, then among equal ones its place.
+// In the second launch a workgroup takes a request.  A row's sum is put together in 64 bits, with the listed logits' terms computed in 64 bits: the
+// terms that dominate it carry no fp32 rounding, the others' roundings average out.  Each wavefront then takes the n best from its share of the sorted
+// lists, one by one, and the wavefronts' lists are merged by counting.
+#include "common.h"
+#include "lookat_search.h"
+
+namespace lookat {
+
+struct SelectArgs {
+    const void *logits;
+    const float *scores;
+    float2 *stats;                        // [rows, parts] maximum, sum of the others
+    float *best;                          // [rows, parts, n] logits, falling
+    int32_t *best_tokens;                 // ... and their tokens
+    float *scores_out;
+    int32_t *parents, *tokens;
+    int64_t stride;
+    int32_t rows, V, n, beams, parts, first_parent;
+};
+
+constexpr int kSelectWaves = 4, kSelectThreads = kSelectWaves * kWave;
+constexpr float kLog2eF = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;
+
+typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.f);          // (both zeros one)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ __forceinline__ int ballot_count(bool b) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b)); }
+
+template <typename FT, int E>
+__global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs a)
+{
+    constexpr int PER = 16 / (int)sizeof(FT), LOADS = E / PER;     // a load's logits
+    __shared__ uint64_t lists[kSelectWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t item = (int64_t)blockIdx.x * kSelectWaves + wave;
+    const int row = (int)(item / a.parts), part = (int)(item - (int64_t)row * a.parts);
+    if (row >= a.rows)
+        return;
+    const int first = part * (kWave * E);
+    const int count = a.V - first < kWave * E ? a.V - first : kWave * E;
+    const FT *src = static_cast<const FT *>(a.logits) + row * a.stride + first;
+    // logit j of a lane is number (j / PER) * 64 PER + lane * PER + j % PER of the part
+    float x[E];
+    if (count == kWave * E) {
+        u4_any raw[LOADS];
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+            raw[k] = __builtin_nontemporal_load(reinterpret_cast<const u4_any *>(src + (k * kWave + lane) * PER));
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (PER == 4) {
+                    x[k * 4 + i] = __uint_as_float(raw[k][i]);
+                } else {
+                    const uint32_t w = raw[k][i];
+                    const float2 f = __half22float2(__builtin_bit_cast(__half2, w));
+                    x[k * 8 + 2 * i] = f.x;
+                    x[k * 8 + 2 * i + 1] = f.y;
+                }
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int at = (j / PER) * (kWave * PER) + lane * PER + j % PER;
+            x[j] = at < count ? (float)src[at] : -INFINITY;
+        }
+    }
+    auto number = [&](int j) -> int { return (j / PER) * (kWave * PER) + lane * PER + j % PER; };
+
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < E; ++j)
+        top = fmaxf(top, x[j]);
+    const uint32_t order = ordered(top);
+    uint32_t bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t t = bound | 1u << bit;
+        bound = ballot_count(order >= t) >= a.n ? t : bound;
+    }
+    float border = fmaxf(unordered(bound), kLowest);      // (-inf, and the NaN that no bound stands for, are below)
+    const float m = wave_max(top), base = m == -INFINITY ? 0.f : m;
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        mine += x[j] >= border;
+    auto upto = [&](int v) -> int {
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int y = __shfl_up(v, d);
+            v += lane >= d ? y : 0;
+        }
+        return v;
+    };
+    int before = upto(mine);
+    int found = __builtin_amdgcn_readlane(before, kWave - 1);
+    int most = 0x7fffffff;                // of the logits at the border those up to this number
+    float rest = 0.f;
+    if (found > kWave) {
+        uint32_t nth = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const float t = unordered(nth | 1u << bit);
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                c += ballot_count(x[j] >= t);
+            nth = c >= a.n ? nth | 1u << bit : nth;
+        }
+        border = fmaxf(unordered(nth), kLowest);
+        int above = 0, equal = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            above += ballot_count(x[j] > border);
+            equal += ballot_count(x[j] == border);
+        }
+        const int want = a.n - above;
+        if (equal > want) {
+            // the least number up to which there are enough
+            most = 0;
+            for (int bit = 30; bit >= 0; --bit) {
+                if (1 << bit >= kWave * E)
+                    continue;
+                const int t = most | 1 << bit;
+                int c = 0;
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    c += ballot_count(x[j] == border && number(j) < t);
+                most = c < want ? t : most;
+            }
+            rest = lane == 0 ? (float)(equal - want) * fast_exp2((border - base) * kLog2eF) : 0.f;
+        }
+        mine = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            mine += x[j] > border || (x[j] == border && number(j) <= most);
+        before = upto(mine);
+        found = __builtin_amdgcn_readlane(before, kWave - 1);
+    }
+    before -= mine;
+    if (__builtin_amdgcn_ballot_w64(mine > 0)) {
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (x[j] > border || (x[j] == border && number(j) <= most))
+                lists[wave][before++] = (uint64_t)ordered(x[j]) << 32 | (uint32_t)~number(j);
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float e = fast_exp2((x[j] - base) * kLog2eF);
+        rest += x[j] >= border ? 0.f : e;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint64_t key = lane < found ? lists[wave][lane] : 0;
+    int rank = 0;
+    for (int j = 0; j < found; ++j) {
+        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, j);
+        rank += other > key;
+    }
+    const float logit = unordered((uint32_t)(key >> 32));
+    const bool listed = lane < found && rank < a.n;
+    if (lane < found && !listed)
+        rest += fast_exp2((logit - base) * kLog2eF);
+    float *best = a.best + item * a.n;
+    int32_t *tokens = a.best_tokens + item * a.n;
+    if (listed) {
+        best[rank] = logit;
+        tokens[rank] = first + (int)~(uint32_t)key;
+    }
+    for (int j = found + lane; j < a.n; j += kWave)
+        best[j] = -INFINITY;
+    rest = wave_sum(rest);
+    if (lane == 0)
+        a.stats[item] = make_float2(m, rest);
+}
+
+// A candidate, and the order among them: score, then row, then logit, then token (within a row the score's rounding decides nothing).
+struct Pick {
+    double score;
+    int row, token;
+    float logit;
+};
+__device__ __forceinline__ bool ahead(const Pick &a, const Pick &b)
+{
+    if (a.score != b.score)
+        return a.score > b.score;
+    if (a.row != b.row)
+        return a.row < b.row;
+    return a.logit != b.logit ? a.logit > b.logit : a.token < b.token;
+}
+__device__ __forceinline__ double lane_double(double x, int lane)
+{
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    return __longlong_as_double((long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane)));
+}
+__device__ __forceinline__ double wave_sum_double(double x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2)
+        x += __shfl_xor(x, d);
+    return x;
+}
+
+constexpr int kMostPicks = 64, kMostBeams = 1024;
+
+__global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs a)
+{
+    __shared__ double bases[kMostBeams];
+    __shared__ Pick picks[kSelectWaves * kMostPicks];
+    const int q = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = a.n, parts = a.parts;
+    const int64_t row0 = (int64_t)q * a.beams;
+    for (int r = wave; r < a.beams; r += kSelectWaves) {
+        const float2 *stats = a.stats + (row0 + r) * parts;
+        const float *best = a.best + (row0 + r) * parts * n;
+        float m = -INFINITY;
+        for (int j = lane; j < parts; j += kWave)
+            m = fmaxf(m, stats[j].x);
+        m = wave_max(m);
+        double sum = 0;
+        for (int j = lane; j < parts; j += kWave) {
+            const float2 s = stats[j];
+            // (a part of -inf alone has a sum of zero, or NaN)
+            sum += (double)s.y * (s.x == -INFINITY ? 1.0 : exp((double)s.x - (double)m));
+        }
+        for (int j = lane; j < parts * n; j += kWave) {
+            const float x = best[j];
+            if (x - m > -80.f)            // (what is smaller is not seen behind the largest term)
+                sum += exp((double)x - (double)m);
+        }
+        sum = wave_sum_double(sum);
+        const float score = a.scores[row0 + r];
+        // -inf: no candidates (a sum that is NaN or infinite, a score that is not finite)
+        const bool none = !(fabsf(m) < INFINITY) || !(sum < (double)INFINITY) || !(fabsf(score) < INFINITY);
+        if (lane == 0)
+            bases[r] = none ? -(double)INFINITY : (double)score - ((double)m + log(sum));
+    }
+    __syncthreads();
+
+    const int lists = a.beams * parts, step = kSelectThreads;
+    auto candidate = [&](int list, int j) -> Pick {
+        Pick c;
+        c.row = list / parts;
+        const int64_t at = ((row0 + c.row) * parts + (list - c.row * parts)) * n + j;
+        c.logit = a.best[at];
+        c.token = c.logit == -INFINITY ? -1 : a.best_tokens[at];
+        c.score = bases[c.row] + (double)c.logit;
+        return c;
+    };
+    // the best of this lane's lists behind `last`
+    auto next = [&](bool any, const Pick &last) -> Pick {
+        Pick best;
+        best.score = -(double)INFINITY;
+        best.row = best.token = 0x7fffffff;
+        best.logit = -INFINITY;
+        for (int list = wave * kWave + lane; list < lists; list += step)
+            for (int j = 0; j < n; ++j) {
+                const Pick c = candidate(list, j);
+                if (!(c.score > -(double)INFINITY))
+                    break;
+                if (any && !ahead(last, c))
+                    continue;
+                if (ahead(c, best))
+                    best = c;
+                break;
+            }
+        return best;
+    };
+    Pick mine = next(false, Pick());
+    for (int k = 0; k < n; ++k) {
+        double top = mine.score;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2)
+            top = fmax(top, __shfl_xor(top, d));
+        Pick best;
+        best.score = top;
+        best.row = best.token = -1;
+        best.logit = -INFINITY;
+        int owner = -1;
+        if (top > -(double)INFINITY) {
+            uint64_t tied = __builtin_amdgcn_ballot_w64(mine.score == top);
+            while (tied) {
+                const int l = __builtin_ctzll(tied);
+                tied &= tied - 1;
+                Pick c;
+                c.score = top;
+                c.row = __builtin_amdgcn_readlane(mine.row, l);
+                c.token = __builtin_amdgcn_readlane(mine.token, l);
+                c.logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.logit), l));
+                if (owner < 0 || ahead(c, best)) {
+                    best = c;
+                    owner = l;
+                }
+            }
+        }
+        if (lane == 0)
+            picks[wave * kMostPicks + k] = best;
+        if (lane == owner)
+            mine = next(true, best);
+    }
+    __syncthreads();
+    // a thread per candidate: those ahead of it, and for places without a candidate those in front
+    for (int i = threadIdx.x; i < kSelectWaves * n; i += kSelectThreads) {
+        const Pick c = picks[i / n * kMostPicks + i % n];
+        const bool real = c.score > -(double)INFINITY;
+        int rank = 0;
+        for (int j = 0; j < kSelectWaves * n; ++j) {
+            const Pick o = picks[j / n * kMostPicks + j % n];
+            const bool other = o.score > -(double)INFINITY;
+            rank += real ? other && ahead(o, c) : other || j < i;
+        }
+        if (rank < n) {
+            a.scores_out[(int64_t)q * n + rank] = (float)c.score;
+            a.parents[(int64_t)q * n + rank] = real ? a.first_parent + (int)row0 + c.row : -1;
+            a.tokens[(int64_t)q * n + rank] = c.token;
+        }
+    }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------
+struct SelectCut {
+    int each, parts;
+    size_t stats, best;                   // bytes, each a multiple of 16
+};
+static SelectCut select_cut(int32_t Q, int32_t beams, int32_t V, int32_t n)
+{
+    SelectCut c;
+    const int64_t rows = (int64_t)Q * beams;
+    c.each = rows * V < 1024LL * kWave * 32 ? 8 : 32;
+    const int64_t per = (int64_t)kWave * c.each;
+    c.parts = (int)((V + per - 1) / per);
+    c.stats = ((size_t)rows * c.parts * sizeof(float2) + 15) / 16 * 16;
+    c.best = ((size_t)rows * c.parts * n * 4 + 15) / 16 * 16;
+    return c;
+}
+static int check_select(int32_t Q, int32_t beams, int32_t V, int32_t n)
+{
+    if (Q <= 0 || beams <= 0 || V <= 0 || n <= 0)
+        return fail(LOOKAT_ERR_SHAPE, "Q=%d, beams=%d, V=%d and n=%d must be positive", Q, beams, V, n);
+    if (n > kMostPicks || beams > kMostBeams || (int64_t)Q * beams > 65535 || V > (1 << 24))
+        return fail(LOOKAT_ERR_UNSUPPORTED, "Q=%d, beams=%d, V=%d, n=%d: at most 64 candidates, 1024 beams, 65535 rows and 2^24 tokens", Q, beams, V, n);
+    return LOOKAT_OK;
+}
+
+}  // namespace lookat
+
+extern "C" size_t lookat_beam_select_workspace_bytes(int32_t Q, int32_t beams, int32_t V, int32_t n)
+{
+    using namespace lookat;
+    clear_error();
+    if (check_select(Q, beams, V, n) != LOOKAT_OK)
+        return 0;
+    const SelectCut c = select_cut(Q, beams, V, n);
+    return c.stats + 2 * c.best;
+}
+
+extern "C" int lookat_beam_select(int32_t Q, int32_t beams, int32_t V, int32_t n, const void *logits, lookat_dtype logit_dtype, int64_t logit_stride,
+                                  const float *scores, int32_t first_parent, float *scores_out, int32_t *parents, int32_t *tokens, void *workspace,
+                                  size_t workspace_bytes, void *stream)
+{
+    using namespace lookat;
+    clear_error();
+    if (int rc = check_select(Q, beams, V, n))
+        return rc;
+    if (logit_dtype != LOOKAT_F16 && logit_dtype != LOOKAT_F32)
+        return fail(LOOKAT_ERR_DTYPE, "logit_dtype=%d is neither LOOKAT_F16 nor LOOKAT_F32", (int)logit_dtype);
+    if (logit_stride < V)
+        return fail(LOOKAT_ERR_SHAPE, "logit_stride=%lld smaller than a row of V=%d", (long long)logit_stride, V);
+    if (first_parent < 0 || first_parent > 0x7fffffff - 65535)
+        return fail(LOOKAT_ERR_SHAPE, "first_parent=%d out of range", first_parent);
+    if (!logits || !scores || !scores_out || !parents || !tokens)
+        return fail(LOOKAT_ERR_NULL, "logits, scores, scores_out, parents and tokens must be non-NULL");
+    if (reinterpret_cast<uintptr_t>(logits) & (logit_dtype == LOOKAT_F16 ? 1u : 3u))
+        return fail(LOOKAT_ERR_ALIGN, "logits must be aligned to their type");
+    if ((reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(scores_out) | reinterpret_cast<uintptr_t>(parents) |
+         reinterpret_cast<uintptr_t>(tokens)) & 3u)
+        return fail(LOOKAT_ERR_ALIGN, "scores, scores_out, parents and tokens must be 4-byte aligned");
+    const SelectCut cut = select_cut(Q, beams, V, n);
+    const size_t need = cut.stats + 2 * cut.best;
+    if (!workspace || workspace_bytes < need)
+        return fail(LOOKAT_ERR_WORKSPACE, "workspace of %zu bytes needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+    if (!aligned16(workspace))
+        return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const int64_t rows = (int64_t)Q * beams, groups = (rows * cut.parts + kSelectWaves - 1) / kSelectWaves;
+    if (groups * kSelectThreads > 0xffffffffLL || rows * cut.parts * n > 0x7fffffffLL)
+        return fail(LOOKAT_ERR_UNSUPPORTED, "Q*beams=%lld rows of V=%d tokens exceed one launch", (long long)rows, V);
+    SelectArgs a;
+    a.logits = logits;
+    a.scores = scores;
+    a.stats = static_cast<float2 *>(workspace);
+    a.best = reinterpret_cast<float *>(static_cast<char *>(workspace) + cut.stats);
+    a.best_tokens = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + cut.stats + cut.best);
+    a.scores_out = scores_out;
+    a.parents = parents;
+    a.tokens = tokens;
+    a.stride = logit_stride;
+    a.rows = (int32_t)rows;
+    a.V = V;
+    a.n = n;
+    a.beams = beams;
+    a.parts = cut.parts;
+    a.first_parent = first_parent;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool half = logit_dtype == LOOKAT_F16;
+    const auto f = cut.each == 8 ? (half ? &select_rows_kernel<_Float16, 8> : &select_rows_kernel<float, 8>)
+                                 : (half ? &select_rows_kernel<_Float16, 32> : &select_rows_kernel<float, 32>);
+    hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(kSelectThreads), 0, st, a);
+    if (int rc = check_launch("lookat_beam_select (rows)"))
+        return rc;
+    hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)Q), dim3(kSelectThreads), 0, st, a);
+    return check_launch("lookat_beam_select");
+}
