@@ -29,11 +29,11 @@ struct ChunkArgs {
     float *part, *out;
     int64_t q_b, q_h, q_n, table_stride;  // strides in elements
     int32_t W, N, group, dsub_log2;
-    int32_t tiles, splits, work, per_die; // row tiles of a (sequence, head), ranges, workgroups with something to do, of them per die
+    int32_t tiles, splits, units;         // row tiles of a (sequence, head), ranges, (sequence, head) pairs
+    int32_t whole, left, per_die;         // workgroups of a die for whole rounds of units, of all dies for the others, of one die for the others
     float scale_log2e;
 };
 
-constexpr int kChunkKeys = 64;
 constexpr int kBookTop = 14;              // the largest centroid entry comes between 2^14 and 2^15
 constexpr int kPartPad = 4;               // a partial row: d_k sums, reference, sum, two unused
 
@@ -116,32 +116,71 @@ __device__ __forceinline__ int seen_of(const ChunkSpan &s, int n)
 struct KeyRange {
     int end, t0, t1, ranges;
 };
+template <int KEYS>
 __device__ __forceinline__ KeyRange key_range(const ChunkSpan &s, int last_row, int splits, int split)
 {
     KeyRange r;
     r.end = seen_of(s, last_row);
-    const int tiles = (r.end + kChunkKeys - 1) / kChunkKeys, per = (tiles + splits - 1) / splits;
+    const int tiles = (r.end + KEYS - 1) / KEYS, per = (tiles + splits - 1) / splits;
     r.ranges = per ? (tiles + per - 1) / per : 1;
     r.t0 = split * per;
     r.t1 = tiles - r.t0 < per ? tiles : r.t0 + per;
     return r;
 }
 
-template <int DK, bool SMALL, bool Q32, bool FP8, int NW>
-__global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkArgs a)
+// Which work a workgroup has.  Units (sequence, head) are dealt to the dies in turn, all workgroups of a unit on one die (they read the same keys and
+// values), the last rows first, which see most; what eight dies do not divide is dealt by workgroups.
+struct Place {
+    int unit, tile, split;
+    bool any;
+};
+__device__ __forceinline__ Place place_of(const ChunkArgs &a)
 {
-    constexpr int CH = DK / 8, STEPS = DK / 16, CB = DK / 64, TQ = 32 * NW;
-    constexpr int CPT = CH / NW > 0 ? CH / NW : 1;               // 8-coordinate pieces of a key that a thread fetches
-    constexpr int kPlane = kChunkKeys * DK * 2, kBuffer = 2 * kPlane;
-    static_assert(CH % NW == 0, "whole pieces for every thread");
-    __shared__ __align__(16) char keys_s[2 * kBuffer];
-    __shared__ int ids_s[2][4], exps_s[2][4];
+    const int die = (int)(blockIdx.x % kXcds), nth = (int)(blockIdx.x / kXcds), per_unit = a.tiles * a.splits;
+    int rest = nth % per_unit;
+    Place x;
+    x.unit = nth / per_unit * kXcds + die;
+    x.any = true;
+    if (nth >= a.whole) {
+        // a.whole: workgroups on each die that belong to whole rounds of units
+        const int index = die * a.per_die + nth - a.whole;
+        x.any = nth - a.whole < a.per_die && index < a.left;
+        x.unit = a.units - a.left / per_unit + index / per_unit;
+        rest = index % per_unit;
+    }
+    x.tile = a.tiles - 1 - rest / a.splits;
+    x.split = rest % a.splits;
+    return x;
+}
+
+// What the first fp16 term of each of a pair of weights left, as a pair: (w0 - h.x, w1 - h.y), each rounded once.
+__device__ __forceinline__ uint32_t left_of(float w0, float w1, uint32_t h)
+{
+    uint32_t r;
+    asm("v_fma_mixlo_f16 %0, %1, 1.0, -%2 op_sel_hi:[0,0,1]" : "=v"(r) : "v"(w0), "v"(h));
+    asm("v_fma_mixhi_f16 %0, %1, 1.0, -%2 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "+v"(r) : "v"(w1), "v"(h));
+    return r;
+}
+
+// Wavefronts to a SIMD that the registers have to allow.
+__host__ __device__ constexpr int chunk_waves(int d_k, bool q32, int keys) { return d_k == 64 && keys == 32 ? 3 : 2; }
+
+template <int DK, bool SMALL, bool Q32, bool FP8, int NW, int KEYS>
+__global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_kernel(PoolArgs p, ChunkArgs a)
+{
+    constexpr int threads = NW * kWave, CH = DK / 8, STEPS = DK / 16, CB = DK / 32, TQ = 32 * NW;
+    constexpr int TPK = threads / KEYS, CPT = CH / TPK, KB = KEYS / 32, GROUPS = KEYS / 16;                                 // 8-coordinate pieces of a key that a thread fetches
+    constexpr int kPlane = KEYS * DK * 2, kBuffer = 2 * kPlane, kValues = KEYS * DK * 2;
+    constexpr int kItems = KEYS / 8 * DK / 2, VPT = (kItems + threads - 1) / threads;    // two coordinates of eight tokens: 16 stored bytes
+    static_assert(CH % TPK == 0, "whole pieces for every thread");
+    __shared__ __align__(16) char keys_s[2 * kBuffer];           // [buffer][term][key][coordinate]
+    __shared__ __align__(16) char values_s[2 * kValues];         // [buffer][octet][coordinate][token]
+    __shared__ int ids_s[4][GROUPS], exps_s[4][GROUPS];                    // of 16 tokens, by tile modulo 4
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
-    const int index = (int)(blockIdx.x % kXcds) * a.per_die + (int)(blockIdx.x / kXcds);
-    if ((int)(blockIdx.x / kXcds) >= a.per_die || index >= a.work)
+    const Place at_work = place_of(a);
+    if (!at_work.any)
         return;
-    const int per_unit = a.tiles * a.splits, unit = index / per_unit, rest = index - unit * per_unit;
-    const int tile = a.tiles - 1 - rest / a.splits, split = rest % a.splits;
+    const int unit = at_work.unit, tile = at_work.tile, split = at_work.split;
     const int b = unit / p.H, h = unit - b * p.H;
     const ChunkSpan span = chunk_span(a, b, p.page_log2);
     const int r0 = tile * TQ, n_first = r0 / a.group;
@@ -149,7 +188,7 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
         return;
     int n_last = (r0 + TQ - 1) / a.group;
     n_last = n_last < span.count ? n_last : span.count - 1;
-    const KeyRange range = key_range(span, n_last, a.splits, split);
+    const KeyRange range = key_range<KEYS>(span, n_last, a.splits, split);
     if (split >= range.ranges)
         return;
     const int32_t *row = a.table + b * a.table_stride;
@@ -163,10 +202,10 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
     const int n_at = n < a.N ? n : a.N - 1;
 
     // ---- the keys of a tile ----
-    const int kk = tid / NW, sub = tid % NW;
+    const int kk = tid / TPK, sub = tid % TPK;
     const int krow = (kk & ~12) | (kk & 4) << 1 | (kk & 8) >> 1;
     auto load_id = [&](int t) -> int {
-        const int key = t * kChunkKeys + kk;
+        const int key = t * KEYS + kk;
         int id = -1;
         if (key < range.end)
             id = row[key >> p.page_log2];
@@ -176,12 +215,12 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
     uint32_t codes[CODES];
     int exponent;
     auto load_codes = [&](int t, int id) {
-        const int key = t * kChunkKeys + kk;
+        const int key = t * KEYS + kk;
         const int64_t place = (int64_t)(id < 0 ? 0 : id) * p.H + h;
         const uint8_t *c = p.codes + ((place << p.page_log2) + (key & page_mask)) * p.m;
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
-            const int chunk = sub + j * NW;
+            const int chunk = sub + j * TPK;
             if constexpr (SMALL) {
                 codes[2 * j] = c[2 * chunk];
                 codes[2 * j + 1] = c[2 * chunk + 1];
@@ -196,7 +235,7 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
     auto load_centroids = [&]() {
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
-            const int chunk = sub + j * NW;
+            const int chunk = sub + j * TPK;
             if constexpr (SMALL) {
                 // four coordinates to a centroid: its terms are 16 bytes
 #pragma unroll
@@ -210,11 +249,11 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
             }
         }
     };
-    auto put = [&](int t, int id, int e) {
+    auto put_keys = [&](int t, int id, int e) {
         char *to = keys_s + (t & 1) * kBuffer + krow * (DK * 2);
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
-            const int chunk = sub + j * NW, at = (chunk ^ (krow & (CH - 1))) << 4;
+            const int chunk = sub + j * TPK, at = (chunk ^ (krow & (CH - 1))) << 4;
             v4u hi = piece[j][0], lo = piece[j][1];
             if constexpr (SMALL) {
                 hi = (v4u){piece[j][0].x, piece[j][0].y, piece[j][1].x, piece[j][1].y};
@@ -226,11 +265,47 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
             *reinterpret_cast<v4u *>(to + kPlane + at) = lo;
         }
         if ((kk & 15) == 0 && sub == 0) {
-            ids_s[t & 1][kk >> 4] = id;
-            exps_s[t & 1][kk >> 4] = id < 0 ? 0 : e;
+            ids_s[t & 3][kk >> 4] = id;
+            exps_s[t & 3][kk >> 4] = id < 0 ? 0 : e;
         }
     };
-    int id1 = load_id(range.t0), id2 = load_id(range.t0 + 1), id3 = load_id(range.t0 + 2);
+    // ---- the values of a tile ----
+    v4u stored[VPT];
+    auto load_values = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int item = tid + j * threads;
+            if (kItems % threads == 0 || item < kItems) {
+                const int octet = item / (DK / 2), pair = item % (DK / 2), id = ids_s[t & 3][octet >> 1];
+                const int64_t at = ((int64_t)(id < 0 ? 0 : id) * p.H + h) << p.page_log2;
+                stored[j] = *reinterpret_cast<const v4u *>(p.values + (at + ((t * KEYS + 8 * octet) & page_mask)) * DK + pair * 16);
+            }
+        }
+    };
+    auto put_values = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int item = tid + j * threads;
+            if (kItems % threads == 0 || item < kItems) {
+                if constexpr (FP8) {
+                    // bytes without a token behind them may be NaN: zeros in their place
+                    if ((t + 1) * KEYS > range.end) {
+                        const int m = range.end - t * KEYS - 8 * (item / (DK / 2));
+                        const uint32_t lo = m >= 4 ? ~0u : m <= 0 ? 0u : (1u << (8 * m)) - 1;
+                        const uint32_t hi = m >= 8 ? ~0u : m <= 4 ? 0u : (1u << (8 * (m - 4))) - 1;
+                        stored[j].x &= lo, stored[j].y &= hi;
+                        stored[j].z &= lo, stored[j].w &= hi;
+                    }
+                    if (ids_s[t & 3][item / (DK / 2) >> 1] < 0)
+                        stored[j] = (v4u){0, 0, 0, 0};
+                }
+                v8h *to = reinterpret_cast<v8h *>(values_s + (t & 1) * kValues) + 2 * item;
+                to[0] = widen<FP8>(stored[j].x, stored[j].y);
+                to[1] = widen<FP8>(stored[j].z, stored[j].w);
+            }
+        }
+    };
+    int id0 = load_id(range.t0), id1 = load_id(range.t0 + 1), id2 = load_id(range.t0 + 2), id3 = load_id(range.t0 + 3);
 
     // ---- the rows as operand: coordinates 16 s + 8 half .. + 7 of row `col` ----
     v8h qh[STEPS], ql[Q32 ? STEPS : 1];
@@ -267,100 +342,95 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
                 ql[s][e] = (_Float16)(w - (float)qh[s][e]);
             }
     }
-    const float to_log2 = a.scale_log2e * unscale;
+    // A negative scale turns the rows around, and a scale of zero becomes fp32's least, so that a score of -inf stays one.
+    if (a.scale_log2e < 0.f) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            qh[s] = -qh[s];
+            if constexpr (Q32)
+                ql[s] = -ql[s];
+        }
+    }
+    const float to_log2 = fmaxf(fabsf(a.scale_log2e * unscale), 1.17549435e-38f);
 
-    load_codes(range.t0, id1);
+    v16f acc[CB], s[KB], s_next[KB];
+    auto score = [&](int t, v16f (&to)[KB]) {
+        const char *from = keys_s + (t & 1) * kBuffer;
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                to[k][i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                const char *at = from + (32 * k + col) * (DK * 2) + (((2 * st + half) ^ (col & (CH - 1))) << 4);
+                const v8h hi = *reinterpret_cast<const v8h *>(at), lo = *reinterpret_cast<const v8h *>(at + kPlane);
+                to[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, qh[st], to[k], 0, 0, 0);
+                to[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, qh[st], to[k], 0, 0, 0);
+                if constexpr (Q32)
+                    to[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, ql[st], to[k], 0, 0, 0);
+            }
+    };
+
+    // Two tiles of keys and one of values are staged, the scores of the first are there before the loop.
+    load_codes(range.t0, id0);
     load_centroids();
     const int exponent0 = exponent;
-    load_codes(range.t0 + 1, id2);
-    put(range.t0, id1, exponent0);
+    load_codes(range.t0 + 1, id1);
+    put_keys(range.t0, id0, exponent0);
+    load_centroids();
+    const int exponent1 = exponent;
+    load_codes(range.t0 + 2, id2);
+    put_keys(range.t0 + 1, id1, exponent1);
     __syncthreads();
-
-    v16f acc[CB][2];
+    load_values(range.t0);
+    score(range.t0, s);
+    put_values(range.t0);
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            acc[c][0][i] = acc[c][1][i] = 0.f;
+            acc[c][i] = 0.f;
     float ref = kNoReference, z = 0.f;    // the reference less kRefLift
+    __syncthreads();
 
     for (int t = range.t0; t < range.t1; ++t) {
-        const int slot = t & 1;
-        int ids[4], exps[4];
+        const int slot = t & 3;
+        int ids[GROUPS], exps[GROUPS], all = 0;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < GROUPS; ++g) {
             ids[g] = __builtin_amdgcn_readfirstlane(ids_s[slot][g]);
             exps[g] = __builtin_amdgcn_readfirstlane(exps_s[slot][g]);
+            all |= ids[g];
         }
-        // values of this tile, centroids of the next, codes of the one behind it, page ids of the third
-        v4u v[4][CB];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int64_t at = ((int64_t)(ids[g] < 0 ? 0 : ids[g]) * p.H + h) << p.page_log2;
-            const uint8_t *src = p.values + (at + ((t * kChunkKeys + 16 * g) & page_mask)) * DK + half * (8 * DK) + col * 16;
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-                v[g][c] = *reinterpret_cast<const v4u *>(src + c * 512);
-        }
-        const int e1 = exponent;
+        // values of the next tile, centroids of the one behind it, codes of the third, page ids of the fourth
+        load_values(t + 1);
+        const int e2 = exponent;
         load_centroids();
-        load_codes(t + 2, id3);
-        const int id4 = load_id(t + 3);
+        load_codes(t + 3, id3);
+        const int id4 = load_id(t + 4);
 
-        // scores
-        v16f s[2];
+        // score i of block k belongs to token 32 k + 16 (i / 8) + 8 half + i % 8
+        if (all < 0 || (t + 1) * KEYS > seen_by_all) {
+            const int limit = seen - t * KEYS - 8 * half;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[k][i] = 0.f;
-        const char *from = keys_s + slot * kBuffer;
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const char *at = from + (32 * k + col) * (DK * 2) + (((2 * st + half) ^ (col & (CH - 1))) << 4);
-                const v8h hi = *reinterpret_cast<const v8h *>(at), lo = *reinterpret_cast<const v8h *>(at + kPlane);
-                s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, qh[st], s[k], 0, 0, 0);
-                s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, qh[st], s[k], 0, 0, 0);
-                if constexpr (Q32)
-                    s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, ql[st], s[k], 0, 0, 0);
-            }
-        // logits: score i of block k belongs to token 32 k + 16 (i / 8) + 8 half + i % 8
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[k][i] = fmaf(s[k][i], to_log2, (float)exps[2 * k + i / 8]);
-        const bool absent = (ids[0] | ids[1] | ids[2] | ids[3]) < 0;
-        if (absent || (t + 1) * kChunkKeys > seen_by_all) {
-            const int limit = seen - t * kChunkKeys - 8 * half;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     s[k][i] = 32 * k + 16 * (i / 8) + i % 8 < (ids[2 * k + i / 8] < 0 ? -64 : limit) ? s[k][i] : -INFINITY;
-            if constexpr (FP8) {
-                // bytes without a token behind them may be NaN: zeros in their place
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int m = ids[g] < 0 ? 0 : range.end - t * kChunkKeys - 16 * g - 8 * half;
-                    const uint32_t lo = m >= 4 ? ~0u : m <= 0 ? 0u : (1u << (8 * m)) - 1;
-                    const uint32_t hi = m >= 8 ? ~0u : m <= 4 ? 0u : (1u << (8 * (m - 4))) - 1;
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) {
-                        v[g][c].x &= lo, v[g][c].y &= hi;
-                        v[g][c].z &= lo, v[g][c].w &= hi;
-                    }
-                }
-            }
         }
+        // the largest logit (log2 units, exponent added; to_log2 is above zero)
+        float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int g = 0; g < GROUPS; ++g) {
+            float m = s[g / 2][8 * (g % 2)];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                top = fmaxf(top, s[k][i]);
+            for (int i = 1; i < 8; ++i)
+                m = fmaxf(m, s[g / 2][8 * (g % 2) + i]);
+            top = fmaxf(top, fmaf(m, to_log2, (float)exps[g]));
+        }
         if (__builtin_amdgcn_ballot_w64(top - ref > kRefLift + kRefLag)) {
             float u, w;
             lanes_xor32(top, u, w);
@@ -370,34 +440,41 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
 #pragma unroll
             for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    acc[c][0][i] *= fix;
-                    acc[c][1][i] *= fix;
-                }
+                for (int i = 0; i < 16; ++i)
+                    acc[c][i] *= fix;
         }
-        // weights and the weighted sum, 16 tokens at a time
+        // the next tile's scores, this one's weights and its weighted sum, 16 tokens at a time
+        score(t + 1, s_next);
+        const v8h *from = reinterpret_cast<const v8h *>(values_s + (t & 1) * kValues) + half * DK + col;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            float w[8], sum = 0.f;
-            v8h hi, lo;
+        for (int g = 0; g < GROUPS; ++g) {
+            float sum = 0.f;
+            v4u hi, lo;
+            const float shift = (float)exps[g] - ref;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = fast_exp2(s[g / 2][8 * (g % 2) + i] - ref);
-                sum += w[i];
-                hi[i] = (_Float16)w[i];
-                lo[i] = (_Float16)(w[i] - (float)hi[i]);
+            for (int i = 0; i < 4; ++i) {
+                const float w0 = fast_exp2(fmaf(s[g / 2][8 * (g % 2) + 2 * i], to_log2, shift));
+                const float w1 = fast_exp2(fmaf(s[g / 2][8 * (g % 2) + 2 * i + 1], to_log2, shift));
+                sum += w0;
+                sum += w1;
+                // (cut, not rounded: the second term takes up what is left all the same)
+                hi[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w0, w1));
+                lo[i] = left_of(w0, w1, hi[i]);
             }
             z = fmaf(sum, power_of_two(-exps[g]), z);
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
-                const v8h a0 = widen<FP8>(v[g][c].x, v[g][c].y), a1 = widen<FP8>(v[g][c].z, v[g][c].w);
-                acc[c][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a0, hi, acc[c][0], 0, 0, 0);
-                acc[c][1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a1, hi, acc[c][1], 0, 0, 0);
-                acc[c][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a0, lo, acc[c][0], 0, 0, 0);
-                acc[c][1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a1, lo, acc[c][1], 0, 0, 0);
+                const v8h x = from[2 * g * DK + 32 * c];
+                acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(v8h, hi), acc[c], 0, 0, 0);
+                acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, __builtin_bit_cast(v8h, lo), acc[c], 0, 0, 0);
             }
         }
-        put(t + 1, id2, e1);
+        // (these buffers were last read before the barrier that ended the tile before)
+        put_keys(t + 2, id2, e2);
+        put_values(t + 1);
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+            s[k] = s_next[k];
         id2 = id3;
         id3 = id4;
         __syncthreads();
@@ -418,18 +495,345 @@ __global__ __launch_bounds__(NW *kWave, 2) void chunk_kernel(PoolArgs p, ChunkAr
         if (half == 0)
             *reinterpret_cast<float2 *>(to + DK) = make_float2(ref, z);
     }
-    // register i of a result is coordinate 64 c + 2 ((i % 4) + 8 (i / 4) + 4 half) of acc[c][0], the next one of acc[c][1]
+    // register i of acc[c] is coordinate 32 c + i % 4 + 8 (i / 4) + 4 half
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const v4f o = {acc[c][0][i] * f, acc[c][1][i] * f, acc[c][0][i + 1] * f, acc[c][1][i + 1] * f};
-            *reinterpret_cast<v4f *>(to + 64 * c + 16 * (i / 4) + 8 * half + 2 * (i % 4)) = o;
+        for (int i = 0; i < 16; i += 4) {
+            const v4f o = {acc[c][i] * f, acc[c][i + 1] * f, acc[c][i + 2] * f, acc[c][i + 3] * f};
+            *reinterpret_cast<v4f *>(to + 32 * c + 2 * i + 4 * half) = o;
         }
 }
 
+// Few rows (drafted tokens, the ends of prompts): 16 RB rows of a (sequence, head) to a workgroup, whose wavefronts take tiles of 32 tokens in turn, each
+// for itself: centroids go straight from the books to the operand's registers, values as in attention of one token, and the wavefronts'
+// results are merged in LDS.  v_mfma_f32_16x16x32_f16: keys are dealt to the two blocks of 16 such that a lane's eight scores belong to one octet.
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kFewKeys = 32;
+__host__ __device__ constexpr size_t few_lds_bytes(int d_k) { return (size_t)kFewWaves * 16 * (d_k + 4) * 4 + kFewWaves * 16 * 8; }
+
+template <int DK, bool SMALL, bool Q32, bool FP8, int RB>
+__global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, ChunkArgs a)
+{
+    constexpr int STEPS = DK / 32, CB = DK / 32, TQ = 16 * RB, ROW = DK + 4;
+    extern __shared__ __align__(16) char few_s[];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, quad = lane >> 4, col = lane & 15;
+    const Place at = place_of(a);
+    if (!at.any)
+        return;
+    const int b = at.unit / p.H, h = at.unit - b * p.H, tile = at.tile, split = at.split;
+    const ChunkSpan span = chunk_span(a, b, p.page_log2);
+    const int r0 = tile * TQ, n_first = r0 / a.group;
+    if (n_first >= span.count)
+        return;
+    int n_last = (r0 + TQ - 1) / a.group;
+    n_last = n_last < span.count ? n_last : span.count - 1;
+    const KeyRange range = key_range<kFewKeys>(span, n_last, a.splits, split);
+    if (split >= range.ranges)
+        return;
+    const int32_t *row = a.table + b * a.table_stride;
+    const int page_mask = (1 << p.page_log2) - 1;
+    const int seen_by_all = seen_of(span, n_first);
+
+    // a page id of the octet `o` of tile t
+    auto load_id = [&](int t, int o) -> int {
+        const int key = t * kFewKeys + 8 * o;
+        int id = -1;
+        if (key < range.end)
+            id = row[key >> p.page_log2];
+        return (uint32_t)id < (uint32_t)p.pages ? id : -1;
+    };
+    // keys: row `col` of block k is token 8 (col / 4) + 4 k + col % 4
+    const int my_octet = col >> 2, my_key = 8 * my_octet + (col & 3);
+    constexpr int CODES = SMALL ? 2 : 1;
+    uint32_t codes[2][STEPS][CODES];
+    auto load_codes = [&](int t, int id) {
+        const int64_t place = (int64_t)(id < 0 ? 0 : id) * p.H + h;
+        const uint8_t *c = p.codes + ((place << p.page_log2) + ((t * kFewKeys + my_key) & page_mask)) * p.m;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if constexpr (SMALL) {
+                    codes[k][s][0] = c[4 * k * p.m + 2 * (4 * s + quad)];
+                    codes[k][s][1] = c[4 * k * p.m + 2 * (4 * s + quad) + 1];
+                } else {
+                    codes[k][s][0] = c[4 * k * p.m + ((8 * (4 * s + quad)) >> a.dsub_log2)];
+                }
+    };
+    v4u piece[2][STEPS][2];
+    const char *books = a.books + (int64_t)h * kCentroids * DK * 4;
+    auto load_centroids = [&]() {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const int chunk = 4 * s + quad;
+                if constexpr (SMALL) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        piece[k][s][e] = *reinterpret_cast<const v4u *>(books + (((2 * chunk + e) * kCentroids + (int)codes[k][s][e]) << 4));
+                } else {
+                    const int i = (chunk * 8) >> a.dsub_log2, within = (chunk * 8) & ((1 << a.dsub_log2) - 1);
+                    const char *from = books + (((i * kCentroids + (int)codes[k][s][0]) << a.dsub_log2) * 2 + within) * 2;
+                    piece[k][s][0] = *reinterpret_cast<const v4u *>(from);
+                    piece[k][s][1] = *reinterpret_cast<const v4u *>(from + (2 << a.dsub_log2));
+                }
+            }
+    };
+
+    int t = range.t0 + wave;
+    int id_k = load_id(t, my_octet), id_k1 = load_id(t + kFewWaves, my_octet), id_k2 = load_id(t + 2 * kFewWaves, my_octet);
+    int id_v = load_id(t, quad), id_v1 = load_id(t + kFewWaves, quad);
+
+    // the rows as operand: coordinates 32 s + 8 quad .. + 7 of row `col` of every block
+    v8h qh[RB][STEPS], ql[Q32 ? RB : 1][STEPS];
+    float to_log2[RB];
+    int seen[RB];
+    const float unscale = a.unscale[h];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        const int r = r0 + 16 * j + col, n = r / a.group, hq = h * a.group + r - n * a.group;
+        const int n_at = n < a.N ? n : a.N - 1;
+        seen[j] = n < span.count ? seen_of(span, n) : range.end;
+        const int64_t q_at = b * a.q_b + hq * a.q_h + n_at * a.q_n + 8 * quad;
+        to_log2[j] = a.scale_log2e * unscale;
+        if constexpr (!Q32) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                qh[j][s] = *reinterpret_cast<const v8h *>(static_cast<const _Float16 *>(a.q) + q_at + 32 * s);
+        } else {
+            v4f x[STEPS][2];
+            float top = 0.f;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    x[s][k] = *reinterpret_cast<const v4f *>(static_cast<const float *>(a.q) + q_at + 32 * s + 4 * k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        top = fmaxf(top, fabsf(x[s][k][e]));
+                }
+            float u, v;
+            lanes_xor16(top, u, v);
+            lanes_xor32(fmaxf(u, v), u, v);
+            const int lift = lift_of(__float_as_uint(fmaxf(u, v)));
+            const float f = power_of_two(lift);
+            to_log2[j] = a.scale_log2e * (unscale * power_of_two(-lift));
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = x[s][e / 4][e % 4] * f;
+                    qh[j][s][e] = (_Float16)w;
+                    ql[j][s][e] = (_Float16)(w - (float)qh[j][s][e]);
+                }
+        }
+        // A negative scale turns the rows around, and a scale of zero becomes fp32's least, so that a score of -inf stays one.
+        if (a.scale_log2e < 0.f) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                qh[j][s] = -qh[j][s];
+                if constexpr (Q32)
+                    ql[j][s] = -ql[j][s];
+            }
+        }
+        to_log2[j] = fmaxf(fabsf(to_log2[j]), 1.17549435e-38f);
+    }
+
+    v4f acc[RB][CB][2];
+    float ref[RB], z[RB];                 // the reference less kRefLift
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        ref[j] = kNoReference;
+        z[j] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+            acc[j][c][0] = acc[j][c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
+    }
+    if (t < range.t1) {
+        load_codes(t, id_k);
+        load_centroids();
+        load_codes(t + kFewWaves, id_k1);
+    }
+    while (t < range.t1) {
+        // values of this tile
+        const int64_t place = (int64_t)(id_v < 0 ? 0 : id_v) * p.H + h;
+        const uint8_t *src = p.values + ((place << p.page_log2) + ((t * kFewKeys + 8 * quad) & page_mask)) * DK + col * 16;
+        v4u v[CB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+            v[c] = *reinterpret_cast<const v4u *>(src + c * 256);
+        const int stored_e = p.exponents[place];
+        const float e = id_v < 0 ? 0.f : (float)stored_e;
+        // scores: element 4 k + i belongs to token 8 quad + 4 k + i
+        const bool edge = (t + 1) * kFewKeys > seen_by_all || __builtin_amdgcn_ballot_w64(id_k < 0 || id_v < 0);
+        if (edge) {
+            // no token: zeros, whatever the centroids hold
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (id_k < 0 || t * kFewKeys + my_key + 4 * k >= range.end)
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s)
+                        piece[k][s][0] = piece[k][s][1] = (v4u){0, 0, 0, 0};
+        }
+        v4f s[RB][2];
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+            s[j][0] = s[j][1] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v4u hi = piece[k][st][0], lo = piece[k][st][1];
+                if constexpr (SMALL) {
+                    hi = (v4u){piece[k][st][0].x, piece[k][st][0].y, piece[k][st][1].x, piece[k][st][1].y};
+                    lo = (v4u){piece[k][st][0].z, piece[k][st][0].w, piece[k][st][1].z, piece[k][st][1].w};
+                }
+#pragma unroll
+                for (int j = 0; j < RB; ++j) {
+                    s[j][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, hi), qh[j][st], s[j][k], 0, 0, 0);
+                    s[j][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, lo), qh[j][st], s[j][k], 0, 0, 0);
+                    if constexpr (Q32)
+                        s[j][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, hi), ql[j][st], s[j][k], 0, 0, 0);
+                }
+            }
+        // centroids of the next tile, codes of the one behind it, page ids of the third
+        const int id_kn = load_id(t + 3 * kFewWaves, my_octet), id_vn = load_id(t + 2 * kFewWaves, quad);
+        if (t + kFewWaves < range.t1) {
+            load_centroids();
+            load_codes(t + 2 * kFewWaves, id_k2);
+        }
+        if (edge) {
+            const int have = id_v < 0 ? 0 : range.end - t * kFewKeys - 8 * quad;
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                const int limit = id_v < 0 ? 0 : seen[j] - t * kFewKeys - 8 * quad;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s[j][i / 4][i % 4] = i < limit ? s[j][i / 4][i % 4] : -INFINITY;
+            }
+            if constexpr (FP8) {
+                // bytes without a token behind them may be NaN: zeros in their place
+                const uint32_t lo = have >= 4 ? ~0u : have <= 0 ? 0u : (1u << (8 * have)) - 1;
+                const uint32_t hi = have >= 8 ? ~0u : have <= 4 ? 0u : (1u << (8 * (have - 4))) - 1;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    v[c].x &= lo, v[c].y &= hi;
+                    v[c].z &= lo, v[c].w &= hi;
+                }
+            }
+        }
+        const float unexp = power_of_two(-(int)e);
+        v4u hi[RB], lo[RB];
+#pragma unroll
+        for (int j = 0; j < RB; ++j) {
+            float m = s[j][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                m = fmaxf(m, s[j][i / 4][i % 4]);
+            const float top = fmaf(m, to_log2[j], e);
+            if (__builtin_amdgcn_ballot_w64(top - ref[j] > kRefLift + kRefLag)) {
+                float u, w;
+                lanes_xor16(top, u, w);
+                lanes_xor32(fmaxf(u, w), u, w);
+                const float to = fmaxf(ref[j], fmaxf(u, w) - kRefLift), fix = fast_exp2(ref[j] - to);
+                ref[j] = to;
+                z[j] *= fix;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    acc[j][c][0] *= fix;
+                    acc[j][c][1] *= fix;
+                }
+            }
+            const float shift = e - ref[j];
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w0 = fast_exp2(fmaf(s[j][i / 2][2 * (i % 2)], to_log2[j], shift));
+                const float w1 = fast_exp2(fmaf(s[j][i / 2][2 * (i % 2) + 1], to_log2[j], shift));
+                sum += w0;
+                sum += w1;
+                hi[j][i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w0, w1));
+                lo[j][i] = left_of(w0, w1, hi[j][i]);
+            }
+            z[j] = fmaf(sum, unexp, z[j]);
+        }
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            const v8h x0 = widen<FP8>(v[c].x, v[c].y), x1 = widen<FP8>(v[c].z, v[c].w);
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                acc[j][c][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x0, __builtin_bit_cast(v8h, hi[j]), acc[j][c][0], 0, 0, 0);
+                acc[j][c][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, __builtin_bit_cast(v8h, hi[j]), acc[j][c][1], 0, 0, 0);
+                acc[j][c][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x0, __builtin_bit_cast(v8h, lo[j]), acc[j][c][0], 0, 0, 0);
+                acc[j][c][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, __builtin_bit_cast(v8h, lo[j]), acc[j][c][1], 0, 0, 0);
+            }
+        }
+        t += kFewWaves;
+        id_k = id_k1;
+        id_k1 = id_k2;
+        id_k2 = id_kn;
+        id_v = id_v1;
+        id_v1 = id_vn;
+    }
+
+    // The wavefronts' results, 16 rows at a time: references and sums first, so that every wavefront brings its own to the common reference.
+    float *results = reinterpret_cast<float *>(few_s);
+    float2 *stats = reinterpret_cast<float2 *>(few_s + (size_t)kFewWaves * 16 * ROW * 4);
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        float u, w;
+        lanes_xor16(z[j], u, w);
+        lanes_xor32(u + w, u, w);
+        if (quad == 0)
+            stats[wave * 16 + col] = make_float2(ref[j], u + w);
+        __syncthreads();
+        float top = kNoReference;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k)
+            top = fmaxf(top, stats[k * 16 + col].x);
+        const float f = fast_exp2(ref[j] - top);
+        // register i of acc[c][x] is coordinate 32 c + 2 (4 quad + i) + x
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2)
+                *reinterpret_cast<v4f *>(results + (wave * 16 + col) * ROW + 32 * c + 8 * quad + 2 * i) =
+                    (v4f){acc[j][c][0][i] * f, acc[j][c][1][i] * f, acc[j][c][0][i + 1] * f, acc[j][c][1][i + 1] * f};
+        __syncthreads();
+        for (int x = tid; x < 16 * (DK / 4); x += kFewThreads) {
+            const int k = x / (DK / 4), d = x % (DK / 4) * 4;
+            const int r = r0 + 16 * j + k, n = r / a.group, hq = h * a.group + r - n * a.group;
+            if (n >= span.count)
+                continue;
+            float best = kNoReference, sum = 0.f;
+#pragma unroll
+            for (int y = 0; y < kFewWaves; ++y)
+                best = fmaxf(best, stats[y * 16 + k].x);
+            v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int y = 0; y < kFewWaves; ++y) {
+                const float2 st = stats[y * 16 + k];
+                sum = fmaf(fast_exp2(st.x - best), st.y, sum);
+                o += *reinterpret_cast<const v4f *>(results + (y * 16 + k) * ROW + d);
+            }
+            if (range.ranges == 1) {
+                const float g = sum == 0.f ? 0.f : 1.f / sum;        // (nothing to sum: zeros; a sum that is NaN stays one)
+                *reinterpret_cast<v4f *>(a.out + ((int64_t)(b * p.H * a.group + hq) * a.N + n) * DK + d) = o * g;
+            } else {
+                float *to = a.part + ((((int64_t)at.unit * a.tiles + tile) * a.splits + split) * TQ + 16 * j + k) * (DK + kPartPad);
+                *reinterpret_cast<v4f *>(to + d) = o;
+                if (d == 0)
+                    *reinterpret_cast<float2 *>(to + DK) = make_float2(best, sum);
+            }
+        }
+        if (j + 1 < RB)
+            __syncthreads();
+    }
+}
+
 // Merges the ranges of one row: a thread per coordinate.
-__global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, int TQ)
+__global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, int TQ, int keys)
 {
     const int n = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, d = threadIdx.x;
     const ChunkSpan span = chunk_span(a, b, page_log2);
@@ -438,7 +842,7 @@ __global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, i
     const int h = hq / a.group, r = n * a.group + hq - h * a.group, tile = r / TQ;
     int n_last = (tile * TQ + TQ - 1) / a.group;
     n_last = n_last < span.count ? n_last : span.count - 1;
-    const int ranges = key_range(span, n_last, a.splits, 0).ranges;
+    const int ranges = (keys == 32 ? key_range<32>(span, n_last, a.splits, 0) : key_range<64>(span, n_last, a.splits, 0)).ranges;
     if (ranges == 1)
         return;
     const int stride = d_k + kPartPad;
@@ -455,7 +859,8 @@ __global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, i
 
 // ---- host -------------------------------------------------------------------------------------------------------
 struct ChunkCut {
-    int waves, tiles, splits;
+    int few, waves, keys, rows;           // row blocks of the kernel for few rows or 0, wavefronts of a workgroup, tokens and rows of a tile
+    int tiles, splits;
     int64_t work;
     size_t books, unscale, part;          // bytes, each a multiple of 16
 };
@@ -463,13 +868,15 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
 {
     ChunkCut c;
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
-    c.waves = rows <= 128 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
-    const int TQ = 32 * c.waves;
-    c.tiles = (int)((rows + TQ - 1) / TQ);
+    c.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+    c.waves = c.few ? kFewWaves : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
+    c.keys = c.waves == 8 && !c.few ? 64 : 32;
+    c.rows = c.few ? 16 * c.few : 32 * c.waves;
+    c.tiles = (int)((rows + c.rows - 1) / c.rows);
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
     c.splits = num_splits;
     if (!num_splits) {
-        const int64_t target = 256 * 8 / c.waves, most = (longest + 255) / 256;
+        const int64_t target = 256 * 8 / c.waves, most = (longest + 511) / 512;
         int64_t s = (target + units * c.tiles / 2) / (units * c.tiles);
         s = s < most ? s : most;
         c.splits = (int)(s < 1 ? 1 : s);
@@ -477,7 +884,7 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
     c.work = units * c.tiles * c.splits;
     c.books = (size_t)p->H * kCentroids * p->d_k * 4;
     c.unscale = ((size_t)p->H * 4 + 15) / 16 * 16;
-    c.part = c.splits > 1 ? (size_t)c.work * TQ * (p->d_k + kPartPad) * 4 : 0;
+    c.part = c.splits > 1 ? (size_t)c.work * c.rows * (p->d_k + kPartPad) * 4 : 0;
     return c;
 }
 
@@ -502,12 +909,36 @@ static int check_chunk(const lookat_page_pool *pool, int32_t B, int32_t N, int32
     return LOOKAT_OK;
 }
 
-template <int DK, bool SMALL, int NW>
-static void launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, hipStream_t st)
+template <int DK, bool SMALL, int NW, int KEYS>
+static int launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
-    const auto f = q32 ? (fp8 ? &chunk_kernel<DK, SMALL, true, true, NW> : &chunk_kernel<DK, SMALL, true, false, NW>)
-                       : (fp8 ? &chunk_kernel<DK, SMALL, false, true, NW> : &chunk_kernel<DK, SMALL, false, false, NW>);
-    hipLaunchKernelGGL(f, dim3((unsigned)(a.per_die * kXcds)), dim3(NW * kWave), 0, st, p, a);
+    const auto f = q32 ? (fp8 ? &chunk_kernel<DK, SMALL, true, true, NW, KEYS> : &chunk_kernel<DK, SMALL, true, false, NW, KEYS>)
+                       : (fp8 ? &chunk_kernel<DK, SMALL, false, true, NW, KEYS> : &chunk_kernel<DK, SMALL, false, false, NW, KEYS>);
+    hipLaunchKernelGGL(f, dim3(groups), dim3(NW * kWave), 0, st, p, a);
+    return check_launch("lookat_attend_pages_chunk");
+}
+template <int DK, bool SMALL, int RB>
+static int launch_few(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
+{
+    const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, RB> : &chunk_few_kernel<DK, SMALL, true, false, RB>)
+                       : (fp8 ? &chunk_few_kernel<DK, SMALL, false, true, RB> : &chunk_few_kernel<DK, SMALL, false, false, RB>);
+    constexpr size_t lds = few_lds_bytes(DK);
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess)
+            return fail(LOOKAT_ERR_HIP, "lookat_attend_pages_chunk: %s", hipGetErrorString(e));
+    }
+    hipLaunchKernelGGL(f, dim3(groups), dim3(kFewThreads), lds, st, p, a);
+    return check_launch("lookat_attend_pages_chunk");
+}
+template <int DK, bool SMALL>
+static int launch_rows(const ChunkCut &c, const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
+{
+    switch (c.few) {
+    case 1: return launch_few<DK, SMALL, 1>(p, a, q32, fp8, groups, st);
+    case 2: return launch_few<DK, SMALL, 2>(p, a, q32, fp8, groups, st);
+    default: return c.waves == 8 ? launch_chunk<DK, SMALL, 8, 64>(p, a, q32, fp8, groups, st) : launch_chunk<DK, SMALL, 4, 32>(p, a, q32, fp8, groups, st);
+    }
 }
 
 }  // namespace lookat
@@ -552,7 +983,9 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
         return fail(LOOKAT_ERR_WORKSPACE, "workspace of %zu bytes needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
     if (!aligned16(workspace))
         return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
-    if (cut.work > 0x7fffffff || !fits_launch((cut.work + kXcds - 1) / kXcds * kXcds, cut.waves * kWave))
+    const int64_t all_units = (int64_t)B * pool->H, per_unit = (int64_t)cut.tiles * cut.splits, whole = all_units / kXcds * per_unit;
+    const int64_t left = all_units % kXcds * per_unit, per_die = (left + kXcds - 1) / kXcds, groups = (whole + per_die) * kXcds;
+    if (!fits_launch(groups, cut.waves * kWave))
         return fail(LOOKAT_ERR_UNSUPPORTED, "B*H*rows*num_splits: %lld workgroups exceed one launch", (long long)cut.work);
     if (cut.splits > 1 && !fits_launch((int64_t)N * pool->H * group * B, pool->d_k))
         return fail(LOOKAT_ERR_UNSUPPORTED, "N=%d rows of %d heads in %d sequences exceed one launch when cut into ranges", N, pool->H * group, B);
@@ -579,25 +1012,24 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
     a.dsub_log2 = dsub_log2;
     a.tiles = cut.tiles;
     a.splits = cut.splits;
-    a.work = (int32_t)cut.work;
-    a.per_die = (int32_t)((cut.work + kXcds - 1) / kXcds);
+    a.units = (int32_t)all_units;
+    a.whole = (int32_t)whole;
+    a.left = (int32_t)left;
+    a.per_die = (int32_t)per_die;
     a.scale_log2e = scale * kLog2e;
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(chunk_books_kernel, dim3(kBookParts, p.H), dim3(kBookThreads), 0, st, codebooks, books, unscale, p.d_k, dsub_log2);
     if (int rc = check_launch("lookat_attend_pages_chunk (codebooks)"))
         return rc;
     const bool q32 = q_dtype == LOOKAT_F32, fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
-    if (p.d_k == 128)
-        cut.waves == 8 ? launch_chunk<128, false, 8>(p, a, q32, fp8, st) : launch_chunk<128, false, 4>(p, a, q32, fp8, st);
-    else if (dsub == 4)
-        cut.waves == 8 ? launch_chunk<64, true, 8>(p, a, q32, fp8, st) : launch_chunk<64, true, 4>(p, a, q32, fp8, st);
-    else
-        cut.waves == 8 ? launch_chunk<64, false, 8>(p, a, q32, fp8, st) : launch_chunk<64, false, 4>(p, a, q32, fp8, st);
-    if (int rc = check_launch("lookat_attend_pages_chunk"))
+    const int rc = p.d_k == 128 ? launch_rows<128, false>(cut, p, a, q32, fp8, (unsigned)groups, st)
+                   : dsub == 4  ? launch_rows<64, true>(cut, p, a, q32, fp8, (unsigned)groups, st)
+                                : launch_rows<64, false>(cut, p, a, q32, fp8, (unsigned)groups, st);
+    if (rc != LOOKAT_OK)
         return rc;
     if (cut.splits == 1)
         return LOOKAT_OK;
     hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)N, (unsigned)(p.H * group), (unsigned)B), dim3(p.d_k), 0, st, a, p.H, p.d_k, p.page_log2,
-                       32 * cut.waves);
+                       cut.rows, cut.keys);
     return check_launch("lookat_attend_pages_chunk (merge)");
 }
