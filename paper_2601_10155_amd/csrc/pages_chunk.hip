@@ -128,28 +128,39 @@ __device__ __forceinline__ KeyRange key_range(const ChunkSpan &s, int last_row, 
     return r;
 }
 
-// Which work a workgroup has.  Units (sequence, head) are dealt to the dies in turn, all workgroups of a unit on one die (they read the same keys and
-// values), the last rows first, which see most; what eight dies do not divide is dealt by workgroups.
+// Which work a workgroup has.  Units (sequence, head) are dealt to the dies in turn, all workgroups of a unit on one die (they read the same keys,
+// values and centroids); the units that eight dies do not divide are dealt by workgroups.  The last rows come first: they see most.  A die's
+// workgroups go round its 32 compute units, and every second round turns back, so that no compute unit gets the longest of each (prompts of 400 to
+// 1000 rows, all workgroups in flight at once: unit by unit 60.7 us, so 57.9.
 struct Place {
     int unit, tile, split;
     bool any;
 };
 __device__ __forceinline__ Place place_of(const ChunkArgs &a)
 {
-    const int die = (int)(blockIdx.x % kXcds), nth = (int)(blockIdx.x / kXcds), per_unit = a.tiles * a.splits;
-    int rest = nth % per_unit;
+    constexpr int kRound = 32;
+    const int die = (int)(blockIdx.x % kXcds), per_unit = a.tiles * a.splits;
+    int nth = (int)(blockIdx.x / kXcds);
+    const bool whole = nth < a.whole;
+    const int most = whole ? a.whole : a.whole + a.per_die, start = nth - (nth - (whole ? 0 : a.whole)) % kRound;
+    const int size = most - start < kRound ? most - start : kRound;
+    if ((start / kRound) & 1)
+        nth = start + size - 1 - (nth - start);
     Place x;
-    x.unit = nth / per_unit * kXcds + die;
-    x.any = true;
-    if (nth >= a.whole) {
-        // a.whole: workgroups on each die that belong to whole rounds of units
-        const int index = die * a.per_die + nth - a.whole;
-        x.any = nth - a.whole < a.per_die && index < a.left;
-        x.unit = a.units - a.left / per_unit + index / per_unit;
-        rest = index % per_unit;
+    int level;
+    if (whole) {
+        const int units = a.whole / per_unit;
+        level = nth / units;
+        x.unit = (nth - level * units) * kXcds + die;
+        x.any = true;
+    } else {
+        const int index = (nth - a.whole) * kXcds + die, units = a.left / per_unit;
+        x.any = index < a.left;
+        level = units ? index / units : 0;
+        x.unit = a.units - units + index - level * units;
     }
-    x.tile = a.tiles - 1 - rest / a.splits;
-    x.split = rest % a.splits;
+    x.tile = a.tiles - 1 - level / a.splits;
+    x.split = level % a.splits;
     return x;
 }
 
@@ -163,7 +174,7 @@ __device__ __forceinline__ uint32_t left_of(float w0, float w1, uint32_t h)
 }
 
 // Wavefronts to a SIMD that the registers have to allow.
-__host__ __device__ constexpr int chunk_waves(int d_k, bool q32, int keys) { return d_k == 64 && keys == 32 ? 3 : 2; }
+__host__ __device__ constexpr int chunk_waves(int d_k, bool q32, int keys) { return 2; }
 
 template <int DK, bool SMALL, bool Q32, bool FP8, int NW, int KEYS>
 __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_kernel(PoolArgs p, ChunkArgs a)
@@ -193,6 +204,10 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
         return;
     const int32_t *row = a.table + b * a.table_stride;
     const int page_mask = (1 << p.page_log2) - 1;
+    // bytes from page to page (below 2^27), and this head's part of page 0
+    const uint32_t code_step = (uint32_t)(p.H * p.m) << p.page_log2, value_step = (uint32_t)(p.H * DK) << p.page_log2;
+    const uint8_t *head_codes = p.codes + ((uint32_t)(h * p.m) << p.page_log2), *head_values = p.values + ((uint32_t)(h * DK) << p.page_log2);
+    const int8_t *head_exponents = p.exponents + h;
 
     // this lane's row
     const int r = r0 + wave * 32 + col, n = r / a.group, hq = h * a.group + r - n * a.group;
@@ -202,22 +217,22 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
     const int n_at = n < a.N ? n : a.N - 1;
 
     // ---- the keys of a tile ----
-    const int kk = tid / TPK, sub = tid % TPK;
+    const int kk = tid / TPK, sub = tid % TPK, last_key = range.end > 0 ? range.end - 1 : 0;
     const int krow = (kk & ~12) | (kk & 4) << 1 | (kk & 8) >> 1;
+    // (What is loaded for a later tile is looked at only there: nothing waits for it in this one.)
     auto load_id = [&](int t) -> int {
         const int key = t * KEYS + kk;
-        int id = -1;
-        if (key < range.end)
-            id = row[key >> p.page_log2];
-        return (uint32_t)id < (uint32_t)p.pages ? id : -1;
+        return row[(key < range.end ? key : last_key) >> p.page_log2];
     };
+    // the page of this thread's 16 tokens, which lie in one, or -1: none of them is there
+    auto page_of = [&](int t, int id) -> int { return t * KEYS + (kk & ~15) < range.end && (uint32_t)id < (uint32_t)p.pages ? id : -1; };
     constexpr int CODES = SMALL ? 2 * CPT : CPT;
     uint32_t codes[CODES];
     int exponent;
-    auto load_codes = [&](int t, int id) {
-        const int key = t * KEYS + kk;
-        const int64_t place = (int64_t)(id < 0 ? 0 : id) * p.H + h;
-        const uint8_t *c = p.codes + ((place << p.page_log2) + (key & page_mask)) * p.m;
+    auto load_codes = [&](int t, int raw_id) {
+        const int id = page_of(t, raw_id);
+        const uint32_t page = id < 0 ? 0 : id;
+        const uint8_t *c = head_codes + (uint64_t)page * code_step + (uint32_t)(((t * KEYS + kk) & page_mask) * p.m);
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
             const int chunk = sub + j * TPK;
@@ -228,7 +243,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
                 codes[j] = c[(chunk * 8) >> a.dsub_log2];
             }
         }
-        exponent = p.exponents[place];
+        exponent = head_exponents[(uint64_t)page * (uint32_t)p.H];
     };
     v4u piece[CPT][2];
     const char *books = a.books + (int64_t)h * kCentroids * DK * 4;
@@ -249,7 +264,8 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             }
         }
     };
-    auto put_keys = [&](int t, int id, int e) {
+    auto put_keys = [&](int t, int raw_id, int e) {
+        const int id = page_of(t, raw_id);
         char *to = keys_s + (t & 1) * kBuffer + krow * (DK * 2);
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
@@ -259,7 +275,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
                 hi = (v4u){piece[j][0].x, piece[j][0].y, piece[j][1].x, piece[j][1].y};
                 lo = (v4u){piece[j][0].z, piece[j][0].w, piece[j][1].z, piece[j][1].w};
             }
-            if (id < 0)                   // no token: zeros, whatever the centroids hold
+            if (id < 0 || t * KEYS + kk >= range.end)     // no token: zeros, whatever the centroids hold
                 hi = lo = (v4u){0, 0, 0, 0};
             *reinterpret_cast<v4u *>(to + at) = hi;
             *reinterpret_cast<v4u *>(to + kPlane + at) = lo;
@@ -277,8 +293,8 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             const int item = tid + j * threads;
             if (kItems % threads == 0 || item < kItems) {
                 const int octet = item / (DK / 2), pair = item % (DK / 2), id = ids_s[t & 3][octet >> 1];
-                const int64_t at = ((int64_t)(id < 0 ? 0 : id) * p.H + h) << p.page_log2;
-                stored[j] = *reinterpret_cast<const v4u *>(p.values + (at + ((t * KEYS + 8 * octet) & page_mask)) * DK + pair * 16);
+                stored[j] = *reinterpret_cast<const v4u *>(head_values + (uint64_t)(uint32_t)(id < 0 ? 0 : id) * value_step +
+                                                           (uint32_t)(((t * KEYS + 8 * octet) & page_mask) * DK + pair * 16));
             }
         }
     };
@@ -407,7 +423,8 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
         }
         // values of the next tile, centroids of the one behind it, codes of the third, page ids of the fourth
         load_values(t + 1);
-        const int e2 = exponent;
+        int e2 = exponent;
+        asm volatile("" : "+v"(e2));      // (else its load is moved into the branch that stores it, and waited for there)
         load_centroids();
         load_codes(t + 3, id3);
         const int id4 = load_id(t + 4);
@@ -532,23 +549,27 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
         return;
     const int32_t *row = a.table + b * a.table_stride;
     const int page_mask = (1 << p.page_log2) - 1;
+    // bytes from page to page (below 2^27), and this head's part of page 0
+    const uint32_t code_step = (uint32_t)(p.H * p.m) << p.page_log2, value_step = (uint32_t)(p.H * DK) << p.page_log2;
+    const uint8_t *head_codes = p.codes + ((uint32_t)(h * p.m) << p.page_log2), *head_values = p.values + ((uint32_t)(h * DK) << p.page_log2);
+    const int8_t *head_exponents = p.exponents + h;
     const int seen_by_all = seen_of(span, n_first);
 
     // a page id of the octet `o` of tile t
+    // (as it stands in the table: looked at by page_of, where it is used)
+    const int last_key = range.end > 0 ? range.end - 1 : 0;
     auto load_id = [&](int t, int o) -> int {
         const int key = t * kFewKeys + 8 * o;
-        int id = -1;
-        if (key < range.end)
-            id = row[key >> p.page_log2];
-        return (uint32_t)id < (uint32_t)p.pages ? id : -1;
+        return row[(key < range.end ? key : last_key) >> p.page_log2];
     };
+    auto page_of = [&](int t, int o, int id) -> int { return t * kFewKeys + 8 * o < range.end && (uint32_t)id < (uint32_t)p.pages ? id : -1; };
     // keys: row `col` of block k is token 8 (col / 4) + 4 k + col % 4
     const int my_octet = col >> 2, my_key = 8 * my_octet + (col & 3);
     constexpr int CODES = SMALL ? 2 : 1;
     uint32_t codes[2][STEPS][CODES];
-    auto load_codes = [&](int t, int id) {
-        const int64_t place = (int64_t)(id < 0 ? 0 : id) * p.H + h;
-        const uint8_t *c = p.codes + ((place << p.page_log2) + ((t * kFewKeys + my_key) & page_mask)) * p.m;
+    auto load_codes = [&](int t, int raw_id) {
+        const int id = page_of(t, my_octet, raw_id);
+        const uint8_t *c = head_codes + (uint64_t)(uint32_t)(id < 0 ? 0 : id) * code_step + (uint32_t)(((t * kFewKeys + my_key) & page_mask) * p.m);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -582,8 +603,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
     };
 
     int t = range.t0 + wave;
-    int id_k = load_id(t, my_octet), id_k1 = load_id(t + kFewWaves, my_octet), id_k2 = load_id(t + 2 * kFewWaves, my_octet);
-    int id_v = load_id(t, quad), id_v1 = load_id(t + kFewWaves, quad);
+    int id_k0 = load_id(t, my_octet), id_k1 = load_id(t + kFewWaves, my_octet), id_k2 = load_id(t + 2 * kFewWaves, my_octet);
+    int id_v0 = load_id(t, quad), id_v1 = load_id(t + kFewWaves, quad);
 
     // the rows as operand: coordinates 32 s + 8 quad .. + 7 of row `col` of every block
     v8h qh[RB][STEPS], ql[Q32 ? RB : 1][STEPS];
@@ -651,19 +672,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
             acc[j][c][0] = acc[j][c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
     }
     if (t < range.t1) {
-        load_codes(t, id_k);
+        load_codes(t, id_k0);
         load_centroids();
         load_codes(t + kFewWaves, id_k1);
     }
     while (t < range.t1) {
         // values of this tile
-        const int64_t place = (int64_t)(id_v < 0 ? 0 : id_v) * p.H + h;
-        const uint8_t *src = p.values + ((place << p.page_log2) + ((t * kFewKeys + 8 * quad) & page_mask)) * DK + col * 16;
+        const int id_v = page_of(t, quad, id_v0), id_k = page_of(t, my_octet, id_k0);
+        const uint32_t page = id_v < 0 ? 0 : id_v;
+        const uint8_t *src = head_values + (uint64_t)page * value_step + (uint32_t)(((t * kFewKeys + 8 * quad) & page_mask) * DK + col * 16);
         v4u v[CB];
 #pragma unroll
         for (int c = 0; c < CB; ++c)
             v[c] = *reinterpret_cast<const v4u *>(src + c * 256);
-        const int stored_e = p.exponents[place];
+        const int stored_e = head_exponents[(uint64_t)page * (uint32_t)p.H];
         const float e = id_v < 0 ? 0.f : (float)stored_e;
         // scores: element 4 k + i belongs to token 8 quad + 4 k + i
         const bool edge = (t + 1) * kFewKeys > seen_by_all || __builtin_amdgcn_ballot_w64(id_k < 0 || id_v < 0);
@@ -770,10 +792,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
             }
         }
         t += kFewWaves;
-        id_k = id_k1;
+        id_k0 = id_k1;
         id_k1 = id_k2;
         id_k2 = id_kn;
-        id_v = id_v1;
+        id_v0 = id_v1;
         id_v1 = id_vn;
     }
 
@@ -859,7 +881,7 @@ __global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, i
 
 // ---- host -------------------------------------------------------------------------------------------------------
 struct ChunkCut {
-    int few, waves, keys, rows;           // row blocks of the kernel for few rows or 0, wavefronts of a workgroup, tokens and rows of a tile
+    int few, waves, rows;                 // row blocks of the kernel for few rows or 0, wavefronts of a workgroup, rows of a tile
     int tiles, splits;
     int64_t work;
     size_t books, unscale, part;          // bytes, each a multiple of 16
@@ -870,7 +892,6 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
     c.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
     c.waves = c.few ? kFewWaves : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
-    c.keys = c.waves == 8 && !c.few ? 64 : 32;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
@@ -909,11 +930,15 @@ static int check_chunk(const lookat_page_pool *pool, int32_t B, int32_t N, int32
     return LOOKAT_OK;
 }
 
-template <int DK, bool SMALL, int NW, int KEYS>
+// Tokens of a tile: 64 for 256 rows of fp16, 32 where fp32 rows take the registers or the workgroup is small.
+constexpr int chunk_keys(int waves, bool q32) { return waves == 8 && !q32 ? 64 : 32; }
+
+template <int DK, bool SMALL, int NW>
 static int launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
-    const auto f = q32 ? (fp8 ? &chunk_kernel<DK, SMALL, true, true, NW, KEYS> : &chunk_kernel<DK, SMALL, true, false, NW, KEYS>)
-                       : (fp8 ? &chunk_kernel<DK, SMALL, false, true, NW, KEYS> : &chunk_kernel<DK, SMALL, false, false, NW, KEYS>);
+    constexpr int K32 = chunk_keys(NW, true), K16 = chunk_keys(NW, false);
+    const auto f = q32 ? (fp8 ? &chunk_kernel<DK, SMALL, true, true, NW, K32> : &chunk_kernel<DK, SMALL, true, false, NW, K32>)
+                       : (fp8 ? &chunk_kernel<DK, SMALL, false, true, NW, K16> : &chunk_kernel<DK, SMALL, false, false, NW, K16>);
     hipLaunchKernelGGL(f, dim3(groups), dim3(NW * kWave), 0, st, p, a);
     return check_launch("lookat_attend_pages_chunk");
 }
@@ -937,7 +962,11 @@ static int launch_rows(const ChunkCut &c, const PoolArgs &p, const ChunkArgs &a,
     switch (c.few) {
     case 1: return launch_few<DK, SMALL, 1>(p, a, q32, fp8, groups, st);
     case 2: return launch_few<DK, SMALL, 2>(p, a, q32, fp8, groups, st);
-    default: return c.waves == 8 ? launch_chunk<DK, SMALL, 8, 64>(p, a, q32, fp8, groups, st) : launch_chunk<DK, SMALL, 4, 32>(p, a, q32, fp8, groups, st);
+    default:
+        if constexpr (DK == 128)
+            if (c.waves == 8)
+                return launch_chunk<DK, SMALL, 8>(p, a, q32, fp8, groups, st);
+        return launch_chunk<DK, SMALL, 4>(p, a, q32, fp8, groups, st);
     }
 }
 
@@ -1030,6 +1059,6 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
     if (cut.splits == 1)
         return LOOKAT_OK;
     hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)N, (unsigned)(p.H * group), (unsigned)B), dim3(p.d_k), 0, st, a, p.H, p.d_k, p.page_log2,
-                       cut.rows, cut.keys);
+                       cut.rows, cut.few ? kFewKeys : chunk_keys(cut.waves, q32));
     return check_launch("lookat_attend_pages_chunk (merge)");
 }
