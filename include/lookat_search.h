@@ -18,7 +18,7 @@ extern "C" {
  *     scores[r] + logits[r,v] - log sum_u exp(logits[r,u])
  * Candidates of a request are ordered by that, falling, equal ones by (row, token), rising; the first n are written.  Rows are ordered as their
  * logits are whatever the rounding of the sum (candidates are compared in 64 bits, with the row's sum to fp32's precision; the score that is written is
- * rounded to fp32 once).  A logit of -inf is a token that cannot be chosen, a score of -inf a beam that has none (one that ended; all but the first
+ * rounded to fp32 once, below its range to its lowest number).  A logit of -inf is a token that cannot be chosen, a score of -inf a beam that has none (one that ended; all but the first
  * of a request that begins).  A row that has a NaN or +inf among its logits, or whose score is NaN or +inf, gives no candidate either.  Where a
  * request has fewer than n candidates the rest is -inf, -1, -1.
  *   logits        fp16 or fp32, element (r,v) at logits[r*logit_stride + v], logit_stride >= V; any alignment of its type

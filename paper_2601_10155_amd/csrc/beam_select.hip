@@ -1,21 +1,28 @@
 // Beam search's selection: the n best of  scores[r] + logit - log sum exp(logits[r])  over a request's beams and the vocabulary.
 //
 // Two launches.  In the first a wavefront takes 64 E consecutive logits of a row, E to a lane, in registers: their maximum m, their n best in order, and
-// the sum of exp(x - m) over the others.  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots);
-// few logits reach it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n, many equal logits) the n-th best
-// itself is found bit by bit, first its value, then among equal ones its place.
-// In the second launch a workgroup takes a request.  A row's sum is put together in 64 bits, with the listed logits' terms computed in 64 bits: the
-// terms that dominate it carry no fp32 rounding, the others' roundings average out.  Each wavefront then takes the n best from its share of the sorted
-// lists, one by one, and the wavefronts' lists are merged by counting.
+// the sum of exp(x - m).  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots); few logits reach
+// it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n, many equal logits) the n-th best itself is found
+// bit by bit, first its value, then among equal ones its place.  Listed logits near m enter the sum in 64 bits, so that the terms that
+// dominate a row's sum carry no fp32 rounding; the others' roundings average out.
+// In the second launch a workgroup takes a request.  A lower bound on the n-th best score, found as above from a few entries of every sorted list,
+// leaves few candidates, whose places are counted.  Where more than kMostFound reach the bound (many equal scores) each wavefront takes the n best of its
+// share of the lists one by one, and those are merged by counting.
+#include <type_traits>
+
 #include "common.h"
 #include "lookat_search.h"
 
 namespace lookat {
 
+struct PartSum {
+    double sum;                           // of exp(x - top) over a part's logits
+    float top, unused;
+};
 struct SelectArgs {
     const void *logits;
     const float *scores;
-    float2 *stats;                        // [rows, parts] maximum, sum of the others
+    PartSum *stats;                       // [rows, parts]
     float *best;                          // [rows, parts, n] logits, falling
     int32_t *best_tokens;                 // ... and their tokens
     float *scores_out;
@@ -27,6 +34,7 @@ struct SelectArgs {
 constexpr int kSelectWaves = 4, kSelectThreads = kSelectWaves * kWave;
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
+constexpr float kNear = 3.f;              // listed logits that are nearer to their part's maximum enter its sum in 64 bits
 
 typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
 
@@ -37,6 +45,14 @@ __device__ __forceinline__ uint32_t ordered(float x)
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 __device__ __forceinline__ int ballot_count(bool b) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b)); }
+
+__device__ __forceinline__ double wave_sum_double(double x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2)
+        x += __shfl_xor(x, d);
+    return x;
+}
 
 template <typename FT, int E>
 __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs a)
@@ -93,22 +109,33 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     }
     float border = fmaxf(unordered(bound), kLowest);      // (-inf, and the NaN that no bound stands for, are below)
     const float m = wave_max(top), base = m == -INFINITY ? 0.f : m;
-    int mine = 0;
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-        mine += x[j] >= border;
-    auto upto = [&](int v) -> int {
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-            const int y = __shfl_up(v, d);
-            v += lane >= d ? y : 0;
-        }
-        return v;
-    };
-    int before = upto(mine);
-    int found = __builtin_amdgcn_readlane(before, kWave - 1);
-    int most = 0x7fffffff;                // of the logits at the border those up to this number
+    // One sweep lists the logits that reach the border (up to number `most` of those at it) and adds up the others.  Few reach it: the list's part is
+    // branched over.  (The difference first: rows that differ by a constant then have the same sum, and their ties stay ties.)
+    const uint64_t below = (1ull << lane) - 1;
+    int found = 0;
     float rest = 0.f;
+    auto sweep = [&](auto all, float at_least, int most) {
+        found = 0;
+        rest = 0.f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const bool reaches = x[j] >= at_least;
+            bool list = reaches;
+            if constexpr (!decltype(all)::value)
+                list = reaches && (x[j] > at_least || number(j) <= most);
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(list);
+            if (mask) {
+                const int place = found + __builtin_popcountll(mask & below);
+                if (list && place < kWave)
+                    lists[wave][place] = (uint64_t)ordered(x[j]) << 32 | (uint32_t)~number(j);
+                found += __builtin_popcountll(mask);
+            }
+            const float e = fast_exp2((x[j] - base) * kLog2eF);
+            rest += reaches ? 0.f : e;
+        }
+    };
+    sweep(std::true_type(), border, 0);
+    float ties = 0.f;                     // logits at the border that are not listed
     if (found > kWave) {
         uint32_t nth = 0;
         for (int bit = 31; bit >= 0; --bit) {
@@ -127,8 +154,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
             equal += ballot_count(x[j] == border);
         }
         const int want = a.n - above;
+        int most = 0x7fffffff;            // of the logits at the border those up to this number
         if (equal > want) {
-            // the least number up to which there are enough
             most = 0;
             for (int bit = 30; bit >= 0; --bit) {
                 if (1 << bit >= kWave * E)
@@ -140,26 +167,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
                     c += ballot_count(x[j] == border && number(j) < t);
                 most = c < want ? t : most;
             }
-            rest = lane == 0 ? (float)(equal - want) * fast_exp2((border - base) * kLog2eF) : 0.f;
+            ties = (float)(equal - want);
         }
-        mine = 0;
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            mine += x[j] > border || (x[j] == border && number(j) <= most);
-        before = upto(mine);
-        found = __builtin_amdgcn_readlane(before, kWave - 1);
-    }
-    before -= mine;
-    if (__builtin_amdgcn_ballot_w64(mine > 0)) {
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            if (x[j] > border || (x[j] == border && number(j) <= most))
-                lists[wave][before++] = (uint64_t)ordered(x[j]) << 32 | (uint32_t)~number(j);
-    }
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const float e = fast_exp2((x[j] - base) * kLog2eF);
-        rest += x[j] >= border ? 0.f : e;
+        sweep(std::false_type(), border, most);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -172,8 +182,15 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     }
     const float logit = unordered((uint32_t)(key >> 32));
     const bool listed = lane < found && rank < a.n;
-    if (lane < found && !listed)
+    // listed logits near the maximum in 64 bits, the others of them as the rest
+    double sum = 0;
+    if (lane < found && !(listed && logit > m - kNear))
         rest += fast_exp2((logit - base) * kLog2eF);
+    else if (lane < found)
+        sum = exp((double)logit - (double)base);
+    if (ties > 0.f && lane == 0)
+        rest += ties * fast_exp2((border - base) * kLog2eF);
+    sum = wave_sum_double(sum + (double)rest);
     float *best = a.best + item * a.n;
     int32_t *tokens = a.best_tokens + item * a.n;
     if (listed) {
@@ -182,9 +199,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     }
     for (int j = found + lane; j < a.n; j += kWave)
         best[j] = -INFINITY;
-    rest = wave_sum(rest);
     if (lane == 0)
-        a.stats[item] = make_float2(m, rest);
+        a.stats[item] = PartSum{sum, m, 0.f};
 }
 
 // A candidate, and the order among them: score, then row, then logit, then token (within a row the score's rounding decides nothing).
@@ -201,45 +217,30 @@ __device__ __forceinline__ bool ahead(const Pick &a, const Pick &b)
         return a.row < b.row;
     return a.logit != b.logit ? a.logit > b.logit : a.token < b.token;
 }
-__device__ __forceinline__ double lane_double(double x, int lane)
-{
-    const uint64_t u = (uint64_t)__double_as_longlong(x);
-    return __longlong_as_double((long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 |
-                                            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane)));
-}
-__device__ __forceinline__ double wave_sum_double(double x)
-{
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2)
-        x += __shfl_xor(x, d);
-    return x;
-}
+// A score as fp32; those below its range, which are candidates all the same, as its lowest number.
+__device__ __forceinline__ float rounded(double score) { return score > -(double)INFINITY ? fmaxf((float)score, kLowest) : -INFINITY; }
 
-constexpr int kMostPicks = 64, kMostBeams = 1024;
+constexpr int kMostPicks = 64, kMostBeams = 1024, kMostFound = 1024, kBatch = 4;
 
 __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs a)
 {
     __shared__ double bases[kMostBeams];
-    __shared__ Pick picks[kSelectWaves * kMostPicks];
+    __shared__ Pick picks[kMostFound];
+    __shared__ uint32_t tops[kSelectThreads];
+    __shared__ int found_s;
     const int q = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = a.n, parts = a.parts;
     const int64_t row0 = (int64_t)q * a.beams;
     for (int r = wave; r < a.beams; r += kSelectWaves) {
-        const float2 *stats = a.stats + (row0 + r) * parts;
-        const float *best = a.best + (row0 + r) * parts * n;
+        const PartSum *stats = a.stats + (row0 + r) * parts;
         float m = -INFINITY;
         for (int j = lane; j < parts; j += kWave)
-            m = fmaxf(m, stats[j].x);
+            m = fmaxf(m, stats[j].top);
         m = wave_max(m);
         double sum = 0;
         for (int j = lane; j < parts; j += kWave) {
-            const float2 s = stats[j];
+            const PartSum s = stats[j];
             // (a part of -inf alone has a sum of zero, or NaN)
-            sum += (double)s.y * (s.x == -INFINITY ? 1.0 : exp((double)s.x - (double)m));
-        }
-        for (int j = lane; j < parts * n; j += kWave) {
-            const float x = best[j];
-            if (x - m > -80.f)            // (what is smaller is not seen behind the largest term)
-                sum += exp((double)x - (double)m);
+            sum += s.sum * (s.top == -INFINITY ? 1.0 : exp((double)s.top - (double)m));
         }
         sum = wave_sum_double(sum);
         const float score = a.scores[row0 + r];
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
         c.row = list / parts;
         const int64_t at = ((row0 + c.row) * parts + (list - c.row * parts)) * n + j;
         c.logit = a.best[at];
-        c.token = c.logit == -INFINITY ? -1 : a.best_tokens[at];
+        c.token = a.best_tokens[at];      // (not looked at where the logit is -inf)
         c.score = bases[c.row] + (double)c.logit;
         return c;
     };
@@ -279,54 +280,116 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
             }
         return best;
     };
-    Pick mine = next(false, Pick());
-    for (int k = 0; k < n; ++k) {
-        double top = mine.score;
+    // the wavefronts' n best of their lists, into picks
+    auto one_by_one = [&]() {
+        Pick mine = next(false, Pick());
+        for (int k = 0; k < n; ++k) {
+            double top = mine.score;
 #pragma unroll
-        for (int d = 1; d < kWave; d *= 2)
-            top = fmax(top, __shfl_xor(top, d));
-        Pick best;
-        best.score = top;
-        best.row = best.token = -1;
-        best.logit = -INFINITY;
-        int owner = -1;
-        if (top > -(double)INFINITY) {
-            uint64_t tied = __builtin_amdgcn_ballot_w64(mine.score == top);
-            while (tied) {
-                const int l = __builtin_ctzll(tied);
-                tied &= tied - 1;
-                Pick c;
-                c.score = top;
-                c.row = __builtin_amdgcn_readlane(mine.row, l);
-                c.token = __builtin_amdgcn_readlane(mine.token, l);
-                c.logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.logit), l));
-                if (owner < 0 || ahead(c, best)) {
-                    best = c;
-                    owner = l;
+            for (int d = 1; d < kWave; d *= 2)
+                top = fmax(top, __shfl_xor(top, d));
+            Pick best;
+            best.score = top;
+            best.row = best.token = -1;
+            best.logit = -INFINITY;
+            int owner = -1;
+            if (top > -(double)INFINITY) {
+                uint64_t tied = __builtin_amdgcn_ballot_w64(mine.score == top);
+                while (tied) {
+                    const int l = __builtin_ctzll(tied);
+                    tied &= tied - 1;
+                    Pick c;
+                    c.score = top;
+                    c.row = __builtin_amdgcn_readlane(mine.row, l);
+                    c.token = __builtin_amdgcn_readlane(mine.token, l);
+                    c.logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.logit), l));
+                    if (owner < 0 || ahead(c, best)) {
+                        best = c;
+                        owner = l;
+                    }
+                }
+            }
+            if (lane == 0)
+                picks[wave * n + k] = best;
+            if (lane == owner)
+                mine = next(true, best);
+        }
+    };
+    // A bound that n candidates reach, from the first `deep` entries of every list (rounded to fp32, which keeps their order).
+    const int deep = lists >= kSelectThreads ? 1 : (kSelectThreads + lists - 1) / lists < n ? (kSelectThreads + lists - 1) / lists : n;
+    float top = -INFINITY;
+    for (int item = threadIdx.x; item < lists * deep; item += step) {
+        const int list = item / deep;
+        top = fmaxf(top, rounded(bases[list / parts] + (double)a.best[(row0 * parts + list) * n + item - list * deep]));
+    }
+    tops[threadIdx.x] = ordered(top);
+    if (threadIdx.x == 0)
+        found_s = 0;
+    __syncthreads();
+    uint32_t order[kSelectWaves], bound = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w)
+        order[w] = tops[w * kWave + lane];
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t t = bound | 1u << bit;
+        int c = 0;
+#pragma unroll
+        for (int w = 0; w < kSelectWaves; ++w)
+            c += ballot_count(order[w] >= t);
+        bound = c >= n ? t : bound;
+    }
+    const float border = fmaxf(unordered(bound), kLowest);
+    for (int list = threadIdx.x; list < lists; list += step) {
+        bool more = true;
+        for (int j0 = 0; j0 < n && more; j0 += kBatch) {
+            Pick c[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                c[i] = candidate(list, j0 + i < n ? j0 + i : n - 1);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                more = more && j0 + i < n && rounded(c[i].score) >= border;
+                if (more) {
+                    const int at = atomicAdd(&found_s, 1);
+                    if (at < kMostFound)
+                        picks[at] = c[i];
                 }
             }
         }
-        if (lane == 0)
-            picks[wave * kMostPicks + k] = best;
-        if (lane == owner)
-            mine = next(true, best);
     }
     __syncthreads();
-    // a thread per candidate: those ahead of it, and for places without a candidate those in front
-    for (int i = threadIdx.x; i < kSelectWaves * n; i += kSelectThreads) {
-        const Pick c = picks[i / n * kMostPicks + i % n];
-        const bool real = c.score > -(double)INFINITY;
+    int found = found_s;
+    const bool listed = found > kMostFound;
+    if (listed) {
+        __syncthreads();
+        found = kSelectWaves * n;
+        one_by_one();
+        __syncthreads();
+    }
+    __syncthreads();
+    // a thread per candidate: its place is the number of those ahead of it
+    for (int i = threadIdx.x; i < found; i += kSelectThreads) {
+        const Pick c = picks[i];
+        if (!(c.score > -(double)INFINITY))
+            continue;
         int rank = 0;
-        for (int j = 0; j < kSelectWaves * n; ++j) {
-            const Pick o = picks[j / n * kMostPicks + j % n];
-            const bool other = o.score > -(double)INFINITY;
-            rank += real ? other && ahead(o, c) : other || j < i;
-        }
+        for (int j = 0; j < found; ++j)
+            rank += ahead(picks[j], c);
         if (rank < n) {
-            a.scores_out[(int64_t)q * n + rank] = (float)c.score;
-            a.parents[(int64_t)q * n + rank] = real ? a.first_parent + (int)row0 + c.row : -1;
+            a.scores_out[(int64_t)q * n + rank] = rounded(c.score);
+            a.parents[(int64_t)q * n + rank] = a.first_parent + (int)row0 + c.row;
             a.tokens[(int64_t)q * n + rank] = c.token;
         }
+    }
+    // and what has no candidate
+    int real = found;
+    if (listed)
+        for (int j = 0; j < found; ++j)
+            real -= !(picks[j].score > -(double)INFINITY);
+    for (int j = real + threadIdx.x; j < n; j += kSelectThreads) {
+        a.scores_out[(int64_t)q * n + j] = -INFINITY;
+        a.parents[(int64_t)q * n + j] = a.tokens[(int64_t)q * n + j] = -1;
     }
 }
 
@@ -339,10 +402,12 @@ static SelectCut select_cut(int32_t Q, int32_t beams, int32_t V, int32_t n)
 {
     SelectCut c;
     const int64_t rows = (int64_t)Q * beams;
-    c.each = rows * V < 1024LL * kWave * 32 ? 8 : 32;
+    // Logits of a lane: 32, or 16 where there would be few wavefronts.  us of the launch, 8 / 16 / 32 / 64: 4 x 50257 fp32 4.7 / 5.0 / 6.0 / - (and 10.0
+    // / 8.3 / 7.9 / - of the merge), 128 x 32001 fp16 9.5 / 7.7 / 9.0 / -, 512 x 131072 fp32 (a call) 133 / 80.9 / 63.5 / 79.8.
+    c.each = rows * V < (16LL << 20) ? 16 : 32;
     const int64_t per = (int64_t)kWave * c.each;
     c.parts = (int)((V + per - 1) / per);
-    c.stats = ((size_t)rows * c.parts * sizeof(float2) + 15) / 16 * 16;
+    c.stats = ((size_t)rows * c.parts * sizeof(PartSum) + 15) / 16 * 16;
     c.best = ((size_t)rows * c.parts * n * 4 + 15) / 16 * 16;
     return c;
 }
@@ -400,7 +465,7 @@ extern "C" int lookat_beam_select(int32_t Q, int32_t beams, int32_t V, int32_t n
     SelectArgs a;
     a.logits = logits;
     a.scores = scores;
-    a.stats = static_cast<float2 *>(workspace);
+    a.stats = static_cast<PartSum *>(workspace);
     a.best = reinterpret_cast<float *>(static_cast<char *>(workspace) + cut.stats);
     a.best_tokens = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + cut.stats + cut.best);
     a.scores_out = scores_out;
@@ -415,8 +480,8 @@ extern "C" int lookat_beam_select(int32_t Q, int32_t beams, int32_t V, int32_t n
     a.first_parent = first_parent;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool half = logit_dtype == LOOKAT_F16;
-    const auto f = cut.each == 8 ? (half ? &select_rows_kernel<_Float16, 8> : &select_rows_kernel<float, 8>)
-                                 : (half ? &select_rows_kernel<_Float16, 32> : &select_rows_kernel<float, 32>);
+    const auto f = cut.each == 16 ? (half ? &select_rows_kernel<_Float16, 16> : &select_rows_kernel<float, 16>)
+                                  : (half ? &select_rows_kernel<_Float16, 32> : &select_rows_kernel<float, 32>);
     hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(kSelectThreads), 0, st, a);
     if (int rc = check_launch("lookat_beam_select (rows)"))
         return rc;
