@@ -41,6 +41,7 @@ class _PythonOnly:
         return None
     encode_keys = build_lut = attend_decode = decode_step = decode_step_split = decode_step_gqa = score_prefill = _leave
     pages_write = attend_pages = pages_copy = pages_fork = pages_free = pages_reserve = pages_compact = _leave
+    attend_pages_chunk = pages_weigh = pages_evict = beam_select = _leave
 
 
 class _Shape(ctypes.Structure):
@@ -171,6 +172,9 @@ def load_library():
             native.bind_pages(*(ctypes.cast(getattr(lib, "lookat_" + name), vp).value for name in (
                 "pages_write", "attend_pages", "attend_pages_workspace_bytes", "pages_copy", "pages_fork", "pages_free", "pages_reserve",
                 "pages_reserve_workspace_bytes", "pages_compact", "pages_compact_workspace_bytes")))
+            native.bind_serving(*(ctypes.cast(getattr(lib, "lookat_" + name), vp).value for name in (
+                "attend_pages_chunk", "attend_pages_chunk_workspace_bytes", "pages_weigh", "pages_weigh_workspace_bytes", "pages_evict",
+                "pages_evict_workspace_bytes", "beam_select", "beam_select_workspace_bytes")))
         except (ImportError, AttributeError, TypeError) as e:
             # (not built, or for another torch: the same library calls are made, 2 to 6 us later each)
             warnings.warn(f"the native marshalling is not available ({e}); run `python -m paper_2601_10155_amd.build`", RuntimeWarning)
@@ -824,6 +828,13 @@ def lookat_attend_pages_chunk(q: torch.Tensor, codebooks: torch.Tensor, pool: Pa
     [H,m,256,d_k/m] fp32, table [B,W] int32, lengths [B] int32 INCLUDING the chunk's tokens, which the pages hold already, counts [B] int32 (None: N)
     -> out [B,H*g,N,d_k] fp32: row n of sequence b, at position lengths[b] - counts[b] + n, attends over the tokens up to its own.  Rows from
     counts[b] on are left as they were (zeros if out is not given).  max_length: as in lookat_attend_pages."""
+    rc = _native().attend_pages_chunk(q, codebooks, pool, table, lengths, scale, counts, max_length, num_splits, workspace, out)
+    if rc is not None:
+        if out is None and rc.__class__ is not int:
+            return rc                # the output, allocated there
+        if rc:
+            _check(rc)
+        return out
     lib = load_library()
     c_pool = _pool(pool)
     B, W, stride, t_ptr = _table(table, "table", pool)
@@ -881,6 +892,11 @@ def lookat_pages_weigh(lut: torch.Tensor, pool: PagePool, table: torch.Tensor, l
                        decay: float = 1.0, max_length: int = 0, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Adds the attention that the queries of lut [B,H*g,m,256] (as lookat_attend_pages takes it) pay to every token, summed over a key/value
     head's g query heads, to decay * weights [B,H,N] fp32 (N >= the longest length, or only the first N tokens have one).  In place; returns weights."""
+    rc = _native().pages_weigh(lut, pool, table, lengths, scale, weights, decay, max_length, workspace)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return weights
     lib = load_library()
     c_pool = _pool(pool)
     B, W, stride, t_ptr = _table(table, "table", pool)
@@ -914,6 +930,11 @@ def lookat_pages_evict(pool: PagePool, table: torch.Tensor, lengths: torch.Tenso
     """min(lengths[b], keep[b]) tokens of every sequence, each head its own - the last `recent`, the first `first`, then the heaviest of weights
     [B,H,N] fp32 - enter the pages of table_out [B,W_out] int32 at positions 0.., in their order (keep [B] int32; reserve that many for empty slots
     first, free the old ones afterwards).  weights_out [B,H,M] fp32, if given, gets the kept tokens' weights in their new places."""
+    rc = _native().pages_evict(pool, table, lengths, weights, keep, table_out, first, recent, weights_out, workspace)
+    if rc is not None:
+        if rc:
+            _check(rc)
+        return
     lib = load_library()
     c_pool = _pool(pool)
     B, W, stride, t_ptr = _table(table, "table", pool)
@@ -1056,6 +1077,12 @@ def lookat_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, n
     """The n best continuations of each request: logits [Q*beams,V] fp16|fp32 (rows dense), scores [Q*beams] fp32 -> scores [Q,n] fp32 =
     scores + log_softmax(logits), falling, parents [Q,n] int32 (first_parent + row: the slots that lookat_pages_fork copies) and tokens [Q,n] int32;
     -inf, -1, -1 where there are fewer.  Beams of score -inf and tokens of logit -inf are not chosen."""
+    if scores_out is None and parents is None and tokens is None:
+        rc = _native().beam_select(logits, scores, beams, n, first_parent, workspace)
+        if rc.__class__ is tuple:
+            return rc
+        if rc:
+            _check(rc)
     lib = load_library()
     device = _dev(logits, "logits").device
     if logits.dim() != 2 or beams < 1 or n < 1 or not logits.shape[0] or logits.shape[0] % beams or not logits.shape[1]:

@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "lookat_pages.h"
+#include "lookat_search.h"
 
 namespace {
 
@@ -45,6 +46,18 @@ struct PageEntries {
     decltype(&lookat_pages_compact_workspace_bytes) compact_workspace_bytes;
 };
 PageEntries pages = {};
+// those of chunks, of a cache held to a budget and of beam search, in the order in which bind_serving() takes their addresses
+struct ServingEntries {
+    decltype(&lookat_attend_pages_chunk) chunk;
+    decltype(&lookat_attend_pages_chunk_workspace_bytes) chunk_workspace_bytes;
+    decltype(&lookat_pages_weigh) weigh;
+    decltype(&lookat_pages_weigh_workspace_bytes) weigh_workspace_bytes;
+    decltype(&lookat_pages_evict) evict;
+    decltype(&lookat_pages_evict_workspace_bytes) evict_workspace_bytes;
+    decltype(&lookat_beam_select) select;
+    decltype(&lookat_beam_select_workspace_bytes) select_workspace_bytes;
+};
+ServingEntries serving = {};
 PyObject *stream_of_device = nullptr;   // torch's "current raw stream of device i"
 
 // A tensor whose memory can be handed to the library as it is (no subclass, no wrapper of a transform), or nullptr.
@@ -598,6 +611,161 @@ PyObject *pages_compact(PyObject *const *args, Py_ssize_t n)
     return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(table)), THPVariable_Wrap(std::move(refs)), THPVariable_Wrap(std::move(live)));
 }
 
+// q, codebooks, pool, table, lengths, scale, counts | None, max_length, num_splits, workspace | None, out | None
+PyObject *attend_pages_chunk(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    Table t;
+    float scale;
+    int64_t longest, splits;
+    if (n != 11 || !pool_of(args[2], p) || !table_of(args[3], p, t) || !number(args[5], scale) || !integer(args[7], 0, INT64_MAX, longest) ||
+        !integer(args[8], 0, 0x7fffffff, splits))
+        GIVE_UP;
+    const at::Tensor *q = plain(args[0]), *cb = dense(args[1], at::kFloat), *out = args[10] == Py_None ? nullptr : dense(args[10], at::kFloat);
+    const int32_t *lengths = ints(args[4], p, t.rows), *counts = args[6] == Py_None ? nullptr : ints(args[6], p, t.rows);
+    if (!q || !cb || q->dim() != 4 || cb->dim() != 4 || !beside(p, *q) || !beside(p, *cb) || !lengths || (args[6] != Py_None && !counts))
+        GIVE_UP;
+    const bool f16 = q->scalar_type() == at::kHalf;
+    const int64_t Hq = q->size(1), N = q->size(2), H = p.c.H, unit = f16 ? 8 : 4;
+    if ((!f16 && q->scalar_type() != at::kFloat) || q->size(0) != t.rows || Hq % H || q->size(3) != p.c.d_k || q->stride(3) != 1 ||
+        std::max(Hq, N) > 0x7fffffff || (reinterpret_cast<uintptr_t>(q->data_ptr()) & 15) || cb->size(0) != H || cb->size(1) != p.c.m ||
+        cb->size(2) != 256 || cb->size(3) != p.c.d_k / p.c.m)
+        GIVE_UP;
+    int64_t stride[3];
+    for (int i = 0; i < 3; ++i) {
+        stride[i] = q->size(i) > 1 ? q->stride(i) : 0;
+        if (stride[i] % unit)
+            GIVE_UP;
+    }
+    if (args[10] != Py_None && (!out || out->dim() != 4 || out->size(0) != t.rows || out->size(1) != Hq || out->size(2) != N || out->size(3) != p.c.d_k ||
+                                !beside(p, *out)))
+        GIVE_UP;
+    at::Tensor own, made;
+    void *ws, *stream;
+    size_t bytes;
+    const int32_t group = (int32_t)(Hq / H);
+    if (!scratch_of(args[9], serving.chunk_workspace_bytes(&p.c, t.rows, (int32_t)N, group, t.W, longest, (int32_t)splits), p, own, ws, bytes) ||
+        !current_stream(*q, stream))
+        GIVE_UP;
+    if (!out)
+        made = counts ? at::zeros({t.rows, Hq, N, p.c.d_k}, cb->options()) : at::empty({t.rows, Hq, N, p.c.d_k}, cb->options());
+    float *op = static_cast<float *>((out ? *out : made).data_ptr());
+    CALL(rc, serving.chunk(&p.c, t.rows, (int32_t)N, group, q->data_ptr(), f16 ? LOOKAT_F16 : LOOKAT_F32, stride[0], stride[1], stride[2],
+                           static_cast<const float *>(cb->data_ptr()), t.ptr, t.W, t.stride, lengths, counts, longest, scale, (int32_t)splits, ws,
+                           bytes, op, stream));
+    return rc == LOOKAT_OK && made.defined() ? THPVariable_Wrap(std::move(made)) : status(rc);
+}
+
+// Weights [B,H,N] fp32 whose rows are dense.
+struct Weights {
+    float *ptr;
+    int32_t columns;
+    int64_t stride;
+};
+bool weights_of(PyObject *o, const Pool &p, int64_t B, Weights &w)
+{
+    const at::Tensor *t = plain(o, at::kFloat);
+    if (!t || t->dim() != 3 || t->size(0) != B || t->size(1) != p.c.H || t->size(2) > 0x7fffffff || t->stride(2) != 1 || !beside(p, *t))
+        return false;
+    w.stride = p.c.H > 1 ? t->stride(1) : std::max(t->stride(0), t->size(2));
+    w.columns = (int32_t)t->size(2);
+    w.ptr = static_cast<float *>(t->data_ptr());
+    return B == 1 || t->stride(0) == p.c.H * w.stride;
+}
+
+// lut, pool, table, lengths, scale, weights, decay, max_length, workspace | None
+PyObject *pages_weigh(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    Table t;
+    Weights w;
+    float scale, decay;
+    int64_t longest;
+    if (n != 9 || !pool_of(args[1], p) || !table_of(args[2], p, t) || !number(args[4], scale) || !weights_of(args[5], p, t.rows, w) ||
+        !number(args[6], decay) || !integer(args[7], 0, INT64_MAX, longest))
+        GIVE_UP;
+    const at::Tensor *lut = dense(args[0], at::kFloat);
+    const int32_t *lengths = ints(args[3], p, t.rows);
+    if (!lut || lut->dim() != 4 || lut->size(0) != t.rows || lut->size(1) % p.c.H || lut->size(1) > 0x7fffffff || lut->size(2) != p.c.m ||
+        lut->size(3) != 256 || !beside(p, *lut) || !lengths)
+        GIVE_UP;
+    const int32_t group = (int32_t)(lut->size(1) / p.c.H);
+    at::Tensor own;
+    void *ws, *stream;
+    size_t bytes;
+    if (!scratch_of(args[8], serving.weigh_workspace_bytes(&p.c, t.rows, group, t.W, longest), p, own, ws, bytes) || !current_stream(*lut, stream))
+        GIVE_UP;
+    CALL(rc, serving.weigh(&p.c, t.rows, group, static_cast<const float *>(lut->data_ptr()), t.ptr, t.W, t.stride, lengths, longest, scale, decay, w.ptr,
+                           w.columns, w.stride, ws, bytes, stream));
+    return status(rc);
+}
+
+// pool, table, lengths, weights, keep, table_out, first, recent, weights_out | None, workspace | None
+PyObject *pages_evict(PyObject *const *args, Py_ssize_t n)
+{
+    Pool p;
+    Table t, to;
+    Weights w, wo = {nullptr, 0, 0};
+    int64_t first, recent;
+    if (n != 10 || !pool_of(args[0], p) || !table_of(args[1], p, t) || !weights_of(args[3], p, t.rows, w) || !table_of(args[5], p, to) ||
+        to.rows != t.rows || !integer(args[6], 0, 0x7fffffff, first) || !integer(args[7], 0, 0x7fffffff, recent) ||
+        (args[8] != Py_None && !weights_of(args[8], p, t.rows, wo)))
+        GIVE_UP;
+    const int32_t *lengths = ints(args[2], p, t.rows), *keep = ints(args[4], p, t.rows);
+    at::Tensor own;
+    void *ws, *stream;
+    size_t bytes;
+    if (!lengths || !keep || !scratch_of(args[9], serving.evict_workspace_bytes(&p.c, t.rows, to.W), p, own, ws, bytes) ||
+        !current_stream(*p.codes, stream))
+        GIVE_UP;
+    CALL(rc, serving.evict(&p.c, t.rows, t.ptr, t.W, t.stride, lengths, w.ptr, w.columns, w.stride, keep, (int32_t)first, (int32_t)recent, to.ptr, to.W,
+                           to.stride, wo.ptr, wo.columns, wo.stride, ws, bytes, stream));
+    return status(rc);
+}
+
+// logits, scores, beams, n, first_parent, workspace | None  ->  (scores, parents, tokens), all made here; given outputs are left to the Python
+// function, and so are tensors on another device than the current one
+PyObject *beam_select(PyObject *const *args, Py_ssize_t count)
+{
+    int64_t beams, n, first;
+    if (count != 6 || !integer(args[2], 1, 0x7fffffff, beams) || !integer(args[3], 1, 0x7fffffff, n) || !integer(args[4], 0, 0x7fffffff, first))
+        GIVE_UP;
+    const at::Tensor *x = plain(args[0]), *scores = dense(args[1], at::kFloat);
+    if (!x || !scores || x->dim() != 2 || scores->dim() != 1 || scores->device() != x->device() ||
+        c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != x->device())
+        GIVE_UP;
+    const bool f16 = x->scalar_type() == at::kHalf;
+    const int64_t R = x->size(0), V = x->size(1);
+    if ((!f16 && x->scalar_type() != at::kFloat) || R % beams || scores->size(0) != R || (V > 1 && x->stride(1) != 1) || (R > 1 && x->stride(0) < V) ||
+        std::max(R, V) > 0x7fffffff)
+        GIVE_UP;
+    const int32_t Q = (int32_t)(R / beams);
+    const size_t need = serving.select_workspace_bytes(Q, (int32_t)beams, (int32_t)V, (int32_t)n);
+    at::Tensor own;
+    void *ws = nullptr, *stream;
+    size_t bytes = need;
+    if (args[5] != Py_None) {
+        const at::Tensor *w = plain(args[5]);
+        if (!w || !w->is_contiguous() || w->device() != x->device())
+            GIVE_UP;
+        ws = w->data_ptr();
+        bytes = (size_t)w->numel() * w->element_size();
+    } else if (need) {
+        own = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+        ws = own.data_ptr();
+    }
+    if (!need || bytes < need || !current_stream(*x, stream))
+        GIVE_UP;
+    at::Tensor best = at::empty({Q, n}, scores->options()), parents = at::empty({Q, n}, scores->options().dtype(at::kInt));
+    at::Tensor tokens = at::empty({Q, n}, parents.options());
+    CALL(rc, serving.select(Q, (int32_t)beams, (int32_t)V, (int32_t)n, x->data_ptr(), f16 ? LOOKAT_F16 : LOOKAT_F32, R > 1 ? x->stride(0) : V,
+                            static_cast<const float *>(scores->data_ptr()), (int32_t)first, static_cast<float *>(best.data_ptr()),
+                            static_cast<int32_t *>(parents.data_ptr()), static_cast<int32_t *>(tokens.data_ptr()), ws, bytes, stream));
+    if (rc != LOOKAT_OK)
+        return status(rc);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(best)), THPVariable_Wrap(std::move(parents)), THPVariable_Wrap(std::move(tokens)));
+}
+
 // No C++ exception crosses into the interpreter: whatever torch throws while a tensor is looked at, the Python function
 // will meet as well, and raise.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
@@ -616,6 +784,18 @@ template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyObject *guarded_pages(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (!entry.score_prefill || !pages.compact_workspace_bytes)
+        GIVE_UP;
+    try {
+        return F(args, n);
+    } catch (...) {
+        GIVE_UP;
+    }
+}
+// The same for those of ServingEntries.
+template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
+PyObject *guarded_serving(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!entry.score_prefill || !serving.select_workspace_bytes)
         GIVE_UP;
     try {
         return F(args, n);
@@ -669,6 +849,28 @@ PyObject *bind_pages(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// bind_serving(addresses of the entry points in the order of ServingEntries)
+PyObject *bind_serving(PyObject *, PyObject *args)
+{
+    unsigned long long a[8];
+    if (!PyArg_ParseTuple(args, "KKKKKKKK", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7))
+        return nullptr;
+    serving.chunk = reinterpret_cast<decltype(serving.chunk)>(a[0]);
+    serving.chunk_workspace_bytes = reinterpret_cast<decltype(serving.chunk_workspace_bytes)>(a[1]);
+    serving.weigh = reinterpret_cast<decltype(serving.weigh)>(a[2]);
+    serving.weigh_workspace_bytes = reinterpret_cast<decltype(serving.weigh_workspace_bytes)>(a[3]);
+    serving.evict = reinterpret_cast<decltype(serving.evict)>(a[4]);
+    serving.evict_workspace_bytes = reinterpret_cast<decltype(serving.evict_workspace_bytes)>(a[5]);
+    serving.select = reinterpret_cast<decltype(serving.select)>(a[6]);
+    serving.select_workspace_bytes = reinterpret_cast<decltype(serving.select_workspace_bytes)>(a[7]);
+    Py_RETURN_NONE;
+}
+
+template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
+PyMethodDef serving_method(const char *name)
+{
+    return PyMethodDef{name, (PyCFunction)(void (*)(void))guarded_serving<F>, METH_FASTCALL, nullptr};
+}
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyMethodDef page_method(const char *name)
 {
@@ -684,7 +886,9 @@ PyMethodDef methods[] = {method<step0>("decode_step"),   method<step1>("decode_s
                          method<prefill>("score_prefill"), page_method<pages_write>("pages_write"), page_method<attend_pages>("attend_pages"),
                          page_method<pages_copy>("pages_copy"), page_method<pages_fork>("pages_fork"), page_method<pages_free>("pages_free"),
                          page_method<pages_reserve>("pages_reserve"), page_method<pages_compact>("pages_compact"),
-                         {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         serving_method<attend_pages_chunk>("attend_pages_chunk"), serving_method<pages_weigh>("pages_weigh"),
+                         serving_method<pages_evict>("pages_evict"), serving_method<beam_select>("beam_select"),
+                         {"bind_serving", bind_serving, METH_VARARGS, nullptr}, {"bind_pages", bind_pages, METH_VARARGS, nullptr}, {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
