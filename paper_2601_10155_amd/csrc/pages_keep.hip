@@ -214,214 +214,425 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / kWave, kPickBins = 2048;
+__device__ __forceinline__ int ballot_count(bool b) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b)); }
 
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / kWave, kPickBins = 2048, kPickCopies = 4;
+
+// KEYS: the weights of up to so many tokens a thread stay in registers; 0: they are read again in every pass.  Token i * 1024 + tid is the thread's i-th.
+template <int KEYS>
 __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, int H, int page_log2)
 {
-    __shared__ uint32_t bins[kPickBins];
+    __shared__ uint32_t bins[kPickBins * kPickCopies];    // (a bin's copies side by side: many tokens have the same weight, zero among them)
     __shared__ uint32_t sums[kPickWaves];
     __shared__ uint32_t found[2];
-    __shared__ int2 counts[kPickWaves];
+    constexpr bool HELD = KEYS > 0;
+    constexpr int kPickKeys = HELD ? KEYS : 1, kEach = (kPickKeys * kPickWaves + kWave - 1) / kWave;
+    __shared__ uint32_t counts[2][kPickKeys * kPickWaves];
     const int unit = blockIdx.x, b = unit / H, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int n = clamp_length(a.lengths[b], a.W, page_log2), k = kept_of(a, b, n, page_log2);
     if (k == 0)
         return;
-    const int recent = a.recent < k ? a.recent : k, first = a.first < k - recent ? a.first : k - recent;
-    const int last = n - recent;          // tokens [first, last) compete for the places that are left
-    int left = k - recent - first;
+    // The k greatest of n: tokens that are kept whatever they weigh count above all weights.  What is behind the last token counts as the least, and
+    // is never reached: among equal ones the lowest positions go first, and k <= n.
+    const int recent = a.recent < k ? a.recent : k, first = a.first < k - recent ? a.first : k - recent, last = n - recent;
+    int left = k;
     const float *weights = a.weights + (int64_t)unit * a.weight_stride;
-    auto order_at = [&](int at) -> uint32_t { return order_of(at < a.columns ? weights[at] : 0.f); };
-    uint32_t border = 0;                  // digits found so far
-    const bool all = left >= last - first;
-    if (!all && left > 0) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-            for (int j = tid; j < kPickBins; j += kPickThreads)
-                bins[j] = 0;
-            __syncthreads();
-            for (int at = first + tid; at < last; at += kPickThreads) {
-                const uint32_t u = order_at(at);
-                if (pass == 0 || (u >> (shift + width)) == border)
-                    atomicAdd(&bins[(u >> shift) & ((1u << width) - 1)], 1u);
+    auto weight_at = [&](int at) -> float { return at < n && at < a.columns ? weights[at] : 0.f; };
+    auto order_at = [&](int at, float w) -> uint32_t { return at >= n ? 0 : at < first || at >= last ? 0xffffffffu : order_of(w); };
+    float held_w[kPickKeys];
+    uint32_t held[kPickKeys];
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < kPickKeys; ++i)
+            held_w[i] = i * kPickThreads < n ? weight_at(i * kPickThreads + tid) : 0.f;
+#pragma unroll
+        for (int i = 0; i < kPickKeys; ++i)
+            held[i] = order_at(i * kPickThreads + tid, held_w[i]);
+    }
+    // f(token, its order, its weight, index) for every token of this thread
+    auto each = [&](auto f) {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < kPickKeys; ++i)
+                if (i * kPickThreads < n)
+                    f(i * kPickThreads + tid, held[i], held_w[i], i);
+        } else {
+            for (int64_t at = tid, i = 0; at - tid < n; at += kPickThreads, ++i) {
+                const float w = weight_at((int)at);
+                f((int)at, order_at((int)at, w), w, (int)i);
             }
-            __syncthreads();
-            // the bin in which the tokens above make `left`: bins from the top, two to a thread
-            const int j1 = kPickBins - 1 - 2 * tid, j0 = j1 - 1;
-            const uint32_t c1 = bins[j1], c0 = bins[j0];
-            uint32_t upto = c1 + c0;
+        }
+    };
+    uint32_t border = 0;                  // digits found so far
+    for (int j = tid; j < kPickBins * kPickCopies; j += kPickThreads)
+        bins[j] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        constexpr int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
+        const int shift = shifts[pass], width = widths[pass];
+        each([&](int, uint32_t u, float, int) {
+            if (pass == 0 || (u >> (shift + width)) == border)
+                atomicAdd(&bins[((u >> shift) & ((1u << width) - 1)) * kPickCopies + (lane & (kPickCopies - 1))], 1u);
+        });
+        __syncthreads();
+        // the bin in which the tokens above make `left`: bins from the top, two to a thread, cleared for the next pass
+        const int j1 = kPickBins - 1 - 2 * tid, j0 = j1 - 1;
+        u32x4 *mine = reinterpret_cast<u32x4 *>(bins) + j0;
+        const u32x4 x0 = mine[0], x1 = mine[1];
+        mine[0] = mine[1] = (u32x4){0, 0, 0, 0};
+        const uint32_t c1 = x1.x + x1.y + x1.z + x1.w, c0 = x0.x + x0.y + x0.z + x0.w;
+        uint32_t upto = c1 + c0;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const uint32_t x = __shfl_up(upto, d);
+            upto += lane >= d ? x : 0;
+        }
+        if (lane == kWave - 1)
+            sums[wave] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kPickWaves; ++w)
+            upto += w < wave ? sums[w] : 0;
+        const uint32_t above1 = upto - c1 - c0, above0 = upto - c0, want = (uint32_t)left;
+        if (above1 < want && above1 + c1 >= want) {
+            found[0] = (uint32_t)j1;
+            found[1] = above1;
+        } else if (above0 < want && above0 + c0 >= want) {
+            found[0] = (uint32_t)j0;
+            found[1] = above0;
+        }
+        __syncthreads();
+        border = border << width | found[0];
+        left -= (int)found[1];
+    }
+    // Now all tokens above `border` are kept (sure), and of those at it (ties) the `left` lowest.
+    int32_t *places = a.places + (int64_t)unit * ((int64_t)a.W_out << page_log2);
+    float *weights_out = a.weights_out ? a.weights_out + (int64_t)unit * a.weight_out_stride : nullptr;
+    const uint64_t below = (1ull << lane) - 1;
+    // A place is the number of kept tokens before one: `above` and `equal` of those before these 64.
+    auto store = [&](int at, uint32_t u, float w, int above, int equal) {
+        const bool sure = u > border, tie = u == border;
+        const uint64_t sures = __builtin_amdgcn_ballot_w64(sure), tied = __builtin_amdgcn_ballot_w64(tie);
+        const int ties = equal + __builtin_popcountll(tied & below);
+        if (sure || (tie && ties < left)) {
+            const int place = above + __builtin_popcountll(sures & below) + (ties < left ? ties : left);
+            places[place] = at;
+            if (weights_out && place < a.columns_out)
+                weights_out[place] = w;
+        }
+    };
+    if constexpr (HELD) {
+        // counts of every 64 tokens, then their sums, then the places
+        each([&](int, uint32_t u, float, int i) {
+            const int sures = ballot_count(u > border), ties = ballot_count(u == border);
+            if (lane == 0) {
+                counts[0][i * kPickWaves + wave] = sures;
+                counts[1][i * kPickWaves + wave] = ties;
+            }
+        });
+        __syncthreads();
+        // (two wavefronts, one for each kind, up to eight counts a lane; those of tokens that are not there are left out)
+        if (wave < 2) {
+            const int used = (n + kPickThreads - 1) / kPickThreads * kPickWaves;
+            uint32_t c[kEach], total = 0;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                c[j] = lane * kEach + j < used ? counts[wave][lane * kEach + j] : 0;
+                total += c[j];
+            }
+            uint32_t upto = total;
 #pragma unroll
             for (int d = 1; d < kWave; d *= 2) {
                 const uint32_t x = __shfl_up(upto, d);
                 upto += lane >= d ? x : 0;
             }
-            if (lane == kWave - 1)
-                sums[wave] = upto;
-            __syncthreads();
-            for (int w = 0; w < wave; ++w)
-                upto += sums[w];
-            const uint32_t above1 = upto - c1 - c0, above0 = upto - c0, want = (uint32_t)left;
-            if (above1 < want && above1 + c1 >= want) {
-                found[0] = (uint32_t)j1;
-                found[1] = above1;
-            } else if (above0 < want && above0 + c0 >= want) {
-                found[0] = (uint32_t)j0;
-                found[1] = above0;
+            upto -= total;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                if (lane * kEach + j < used)
+                    counts[wave][lane * kEach + j] = upto;
+                upto += c[j];
+            }
+        }
+        __syncthreads();
+        each([&](int at, uint32_t u, float w, int i) { store(at, u, w, (int)counts[0][i * kPickWaves + wave], (int)counts[1][i * kPickWaves + wave]); });
+    } else {
+        // 1024 tokens at a time
+        int above_all = 0, equal_all = 0;
+        each([&](int at, uint32_t u, float w, int) {
+            const int sures = ballot_count(u > border), ties = ballot_count(u == border);
+            __syncthreads();              // (the last counts were read)
+            if (lane == 0) {
+                counts[0][wave] = sures;
+                counts[1][wave] = ties;
             }
             __syncthreads();
-            border = border << width | found[0];
-            left -= (int)found[1];
-            __syncthreads();
-        }
-    }
-    // now `left` of the tokens of weight `border` are kept, the lowest, and all above it
-    const int each = ((n + kPickWaves - 1) / kPickWaves + kWave - 1) / kWave * kWave;
-    const int from = wave * each < n ? wave * each : n, to = from + each < n ? from + each : n;
-    // 2: kept, 1: kept if there is room, 0: not
-    auto state_of = [&](int at) -> int {
-        if (at >= to)
-            return 0;
-        if (at < first || at >= last || all)
-            return 2;
-        if (left <= 0 && border == 0)
-            return 0;                     // (no place is left for the middle)
-        const uint32_t u = order_at(at);
-        return u > border ? 2 : u == border ? 1 : 0;
-    };
-    int above = 0, equal = 0;
-    for (int t = from; t < to; t += kWave) {
-        const int s = state_of(t + lane);
-        above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(s == 2));
-        equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(s == 1));
-    }
-    if (lane == 0)
-        counts[wave] = make_int2(above, equal);
-    __syncthreads();
-    int before = 0, ties = 0;
-    for (int w = 0; w < wave; ++w) {
-        before += counts[w].x;
-        ties += counts[w].y;
-    }
-    before += ties < left ? ties : left;
-    int32_t *places = a.places + (int64_t)unit * ((int64_t)a.W_out << page_log2);
-    float *weights_out = a.weights_out ? a.weights_out + (int64_t)unit * a.weight_out_stride : nullptr;
-    const uint64_t below = (1ull << lane) - 1;
-    for (int t = from; t < to; t += kWave) {
-        const int at = t + lane, s = state_of(at);
-        const uint64_t tie = __builtin_amdgcn_ballot_w64(s == 1);
-        const bool kept = s == 2 || (s == 1 && ties + __builtin_popcountll(tie & below) < left);
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(kept);
-        const int place = before + __builtin_popcountll(mask & below);
-        if (kept) {
-            places[place] = at;
-            if (weights_out && place < a.columns_out)
-                weights_out[place] = at < a.columns ? weights[at] : 0.f;
-        }
-        before += __builtin_popcountll(mask);
-        ties += __builtin_popcountll(tie);
+            int above = above_all, equal = equal_all;
+#pragma unroll
+            for (int x = 0; x < kPickWaves; ++x) {
+                above += x < wave ? counts[0][x] : 0;
+                equal += x < wave ? counts[1][x] : 0;
+                above_all += counts[0][x];
+                equal_all += counts[1][x];
+            }
+            store(at, u, w, above, equal);
+        });
     }
 }
 
-constexpr int kMoveThreads = 256;
-// grid: (new page of the sequence, head, sequence)
-template <int DK, bool FP8>
+// Moving.  A token is one byte in eight of what a page holds for its octet and coordinate, so octets are read whole, a lane per coordinate, 512
+// consecutive bytes a wavefront, and a new octet is put together from the octets that its tokens come from (mostly two or three) by byte permutes
+// whose selectors are the same for all lanes.  A wavefront takes 64 new tokens (128 where a page has as many), a lane each while it is found out where
+// they are; no wavefront waits for another.  The bytes stay in registers until the largest value, and with it the exponent, is known; where all
+// tokens of an octet had that exponent they are stored as they are.
+constexpr int kMoveWaves = 4, kMoveThreads = kMoveWaves * kWave;
+constexpr int kMoveAhead = 3;             // octets requested at once for a new one
+constexpr int kMoveBatch = 2;             // new octets (64 coordinates of them) whose octets are requested together
+constexpr int kMixed = 127;               // no exponent: the tokens of an octet have several
+
+struct MoveSource {
+    int64_t at;                           // an octet's first byte in the values
+    uint32_t lo, hi;                      // where its bytes go in the new octet: selectors of v_perm_b32, 12 for none
+};
+typedef short v2s __attribute__((ext_vector_type(2)));
+
+// The largest |stored| of eight bytes as a number of fp32; e4m3's NaN counts above all.
+template <bool FP8>
+__device__ __forceinline__ float largest(uint32_t lo, uint32_t hi)
+{
+    if constexpr (FP8) {
+        // (without their signs the bytes are ordered as the numbers)
+        const v2s a = __builtin_bit_cast(v2s, lo & 0x007f007fu), b = __builtin_bit_cast(v2s, lo >> 8 & 0x007f007fu);
+        const v2s c = __builtin_bit_cast(v2s, hi & 0x007f007fu), d = __builtin_bit_cast(v2s, hi >> 8 & 0x007f007fu);
+        const v2s m = __builtin_elementwise_max(__builtin_elementwise_max(a, b), __builtin_elementwise_max(c, d));
+        const int top = m.x > m.y ? m.x : m.y;
+        return top == 0x7f ? INFINITY : __builtin_amdgcn_cvt_f32_fp8(top, 0);
+    } else {
+        const v2s l = __builtin_bit_cast(v2s, lo), h = __builtin_bit_cast(v2s, hi);
+        const v2s a = (l << 8) >> 8, b = l >> 8, c = (h << 8) >> 8, d = h >> 8;
+        const v2s most = __builtin_elementwise_max(__builtin_elementwise_max(a, b), __builtin_elementwise_max(c, d));
+        const v2s least = __builtin_elementwise_min(__builtin_elementwise_min(a, b), __builtin_elementwise_min(c, d));
+        const int x = most.x > most.y ? most.x : most.y, y = least.x < least.y ? least.x : least.y;
+        return (float)(x > -y ? x : -y);
+    }
+}
+
+// Four stored numbers, none of them NaN, times a power of two after which none is above the largest.
+template <bool FP8>
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f)
+{
+    if constexpr (FP8) {
+        const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, f, true);
+        const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a.x, a.y, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x, b.y, r, true);
+    } else {
+        float x[4];
+        unpack4<FP8>(w, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] *= f;
+        return pack4<FP8>(x[0], x[1], x[2], x[3]);
+    }
+}
+
+// grid: (new pages of the sequence in fours of wavefronts, head, sequence)
+template <int DK, bool FP8, int PAGE>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PoolArgs p, EvictArgs a)
 {
-    __shared__ int64_t source[128];       // a token's first byte in the values, or -1
-    __shared__ int exps[128];
-    __shared__ float tops[kMoveThreads / kWave];
-    const int b = blockIdx.z, h = blockIdx.y, slot = blockIdx.x, tid = threadIdx.x;
-    const int n = clamp_length(a.lengths[b], a.W, p.page_log2), k = kept_of(a, b, n, p.page_log2);
-    const int page = 1 << p.page_log2, j0 = slot << p.page_log2;
+    constexpr int TOKENS = PAGE > kWave ? PAGE : kWave;
+    constexpr int EACH = TOKENS / kWave, PAGES = TOKENS / PAGE, OCTETS = TOKENS / 8, CB = DK / kWave;
+    constexpr int PIECES = PAGE / 8 * CB, BATCHES = PIECES / kMoveBatch;     // of a page
+    constexpr int page_log2 = PAGE == 16 ? 4 : PAGE == 32 ? 5 : PAGE == 64 ? 6 : 7;
+    __shared__ MoveSource sources_s[kMoveWaves][TOKENS];
+    __shared__ __align__(16) float scales_s[kMoveWaves][TOKENS];      // 2^exponent
+    __shared__ int octet_e_s[kMoveWaves][OCTETS], octet_n_s[kMoveWaves][OCTETS];
+    __shared__ uint32_t octet_has_s[kMoveWaves][OCTETS];  // a bit for every token
+    const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    MoveSource *sources = sources_s[wave];
+    float *scales = scales_s[wave];
+    int *octet_e = octet_e_s[wave], *octet_n = octet_n_s[wave];
+    uint32_t *octet_has = octet_has_s[wave];
+    const int n = clamp_length(a.lengths[b], a.W, page_log2), k = kept_of(a, b, n, page_log2);
+    const int slot0 = (int)(blockIdx.x * kMoveWaves + wave) * PAGES, j0 = slot0 * PAGE;
     if (j0 >= k)
         return;
-    const int to_id = a.table_out[b * a.out_stride + slot];
-    if ((uint32_t)to_id >= (uint32_t)p.pages)
-        return;
-    const int tokens = k - j0 < page ? k - j0 : page;
-    const int64_t to = (int64_t)to_id * p.H + h;
-    const int32_t *places = a.places + ((int64_t)b * p.H + h) * ((int64_t)a.W_out << p.page_log2) + j0;
-    if (tid < page) {
-        int64_t at = -1;
-        int e = 0;
-        if (tid < tokens) {
-            const int pos = places[tid], id = a.table[b * a.table_stride + (pos >> p.page_log2)], t = pos & (page - 1);
-            if ((uint32_t)id < (uint32_t)p.pages) {
-                const int64_t from = (int64_t)id * p.H + h;
-                e = p.exponents[from];
-                e = e < kLowExponent ? kLowExponent : e > kHighExponent ? kHighExponent : e;
-                at = (from << p.page_log2) * DK + (int64_t)(t & ~7) * DK + (t & 7);
-                copy_code(p.codes + (to << p.page_log2) * p.m + (int64_t)tid * p.m, p.codes + ((from << p.page_log2) + t) * p.m, p.m, 0);
-            }
-        }
-        source[tid] = at;
-        exps[tid] = e;
-    }
-    __syncthreads();
-    const int items = (page / 8) * DK, rounds = (items + kMoveThreads - 1) / kMoveThreads;    // an item: eight tokens of a coordinate
-    constexpr int most = 128 / 8 * DK / kMoveThreads;
-    uint32_t lo[most], hi[most];
-    float top = -1.f;                     // (below zero: no token at all)
+    const int32_t *places = a.places + ((int64_t)b * p.H + h) * ((int64_t)a.W_out << page_log2);
+    const int32_t *row = a.table + b * a.table_stride, *row_out = a.table_out + b * a.out_stride;
+    int pos[EACH], id[EACH], to_id[EACH], exponent[EACH];
 #pragma unroll
-    for (int r = 0; r < most; ++r) {
-        lo[r] = hi[r] = 0;
-        if (r >= rounds)
-            continue;
-        const int item = tid + r * kMoveThreads, octet = item / DK, d = item % DK;
-        if (item >= items)
-            continue;
+    for (int g = 0; g < EACH; ++g) {
+        const int j = j0 + g * kWave + lane;
+        pos[g] = j < k ? places[j] : -1;
+        to_id[g] = j < k ? row_out[j >> page_log2] : -1;
+    }
+#pragma unroll
+    for (int g = 0; g < EACH; ++g) {
+        id[g] = pos[g] >= 0 ? row[pos[g] >> page_log2] : -1;
+        if ((uint32_t)id[g] >= (uint32_t)p.pages || (uint32_t)to_id[g] >= (uint32_t)p.pages)
+            id[g] = -1;
+    }
+    const int first = lane & ~7, me = lane & 7;
+#pragma unroll
+    for (int g = 0; g < EACH; ++g) {
+        const int t = pos[g] & (PAGE - 1), token = g * kWave + lane;
+        const int64_t from = (int64_t)(id[g] < 0 ? 0 : id[g]) * p.H + h;
+        const int64_t at = id[g] < 0 ? -1 : ((from << page_log2) + (t & ~7)) * DK;
+        exponent[g] = p.exponents[from];
+        // the octets that this octet's eight tokens come from, one entry for each, written by its first token
+        const uint32_t has = (uint32_t)(__builtin_amdgcn_ballot_w64(at >= 0) >> first) & 0xff;
+        uint32_t sel[2] = {0, 0};
+        bool leads = at >= 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int64_t at = source[octet * 8 + i];
-            if (at >= 0) {
-                const uint32_t x = p.values[at + d * 8];
-                if (i < 4)
-                    lo[r] |= x << (8 * i);
-                else
-                    hi[r] |= x << (8 * (i - 4));
-            }
+            const int64_t other = __shfl(at, first + i);
+            const int other_t = __shfl(t, first + i);
+            sel[i / 4] |= (uint32_t)(other == at ? other_t & 7 : 12) << (8 * (i % 4));
+            leads = leads && !(i < me && other == at);
         }
-        float x[8];
-        unpack4<FP8>(lo[r], *reinterpret_cast<float(*)[4]>(x));
-        unpack4<FP8>(hi[r], *reinterpret_cast<float(*)[4]>(x + 4));
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            top = source[octet * 8 + i] >= 0 ? fmaxf(top, fabsf(x[i]) * two_to(exps[octet * 8 + i])) : top;
+        const uint32_t heads = (uint32_t)(__builtin_amdgcn_ballot_w64(leads) >> first) & 0xff;
+        // (the entries behind them name bytes that are there and take none: every new octet requests as many, without a branch, so that what is
+        // waited for is counted)
+        const int used = __builtin_popcount(heads);
+        MoveSource s = {0, 0x0c0c0c0cu, 0x0c0c0c0cu};
+        if (me >= used)
+            sources[token] = s;
+        if (leads) {
+            s.at = at;
+            s.lo = sel[0];
+            s.hi = sel[1];
+            sources[(token & ~7) + __builtin_popcount(heads & ((1u << me) - 1))] = s;
+        }
+        if (me == 0) {
+            octet_n[token / 8] = used;
+            octet_has[token / 8] = has;
+        }
     }
-    top = wave_max(top);
-    if ((tid & (kWave - 1)) == 0)
-        tops[tid / kWave] = top;
-    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    uint8_t *values = p.values;
+    uint64_t ahead[2][kMoveBatch][kMoveAhead];
+    auto request = [&](int octet0, int batch) {
 #pragma unroll
-    for (int w = 0; w < kMoveThreads / kWave; ++w)
-        top = fmaxf(top, tops[w]);
-    if (top < 0.f)
-        return;
-    const int e = exponent_of<FP8>(top);
-    uint8_t *values = p.values + (to << p.page_log2) * DK;
+        for (int r = 0; r < kMoveBatch; ++r) {
+            const int piece = batch * kMoveBatch + r, octet = octet0 + piece / CB, d = piece % CB * kWave + lane;
 #pragma unroll
-    for (int r = 0; r < most; ++r) {
-        const int item = tid + r * kMoveThreads, octet = item / DK;
-        if (r >= rounds || item >= items)
-            continue;
-        float x[8];
-        unpack4<FP8>(lo[r], *reinterpret_cast<float(*)[4]>(x));
-        unpack4<FP8>(hi[r], *reinterpret_cast<float(*)[4]>(x + 4));
-        uint64_t mask = 0;
+            for (int i = 0; i < kMoveAhead; ++i)
+                ahead[batch & 1][r][i] = *reinterpret_cast<const uint64_t *>(values + sources[octet * 8 + i].at + d * 8);
+        }
+    };
+    request(0, 0);
+    // (while the octets are on their way: the tokens' exponents and codes)
+#pragma unroll
+    for (int g = 0; g < EACH; ++g) {
+        const int e = exponent[g] < kLowExponent ? kLowExponent : exponent[g] > kHighExponent ? kHighExponent : exponent[g], token = g * kWave + lane;
+        const uint32_t has = (uint32_t)(__builtin_amdgcn_ballot_w64(id[g] >= 0) >> first) & 0xff;
+        scales[token] = two_to(e);
+        bool same = true;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] *= two_to(exps[octet * 8 + i] - e);
-            mask |= source[octet * 8 + i] >= 0 ? 0xffull << (8 * i) : 0;
+            const int other_e = __shfl(e, first + i);     // (by all lanes)
+            same = same && (!(has >> i & 1) || other_e == e);
         }
-        if (!mask)
-            continue;
-        uint64_t w = (uint64_t)pack4<FP8>(x[4], x[5], x[6], x[7]) << 32 | pack4<FP8>(x[0], x[1], x[2], x[3]);
-        uint64_t *dst = reinterpret_cast<uint64_t *>(values) + item;
-        if (mask != ~0ull)                // (what lies behind the last token stays)
-            w = (w & mask) | (*dst & ~mask);
-        *dst = w;
+        if (has ? me == __builtin_ctz(has) : me == 0)
+            octet_e[token / 8] = same ? e : kMixed;
+        if (id[g] >= 0) {
+            const int64_t from = ((int64_t)id[g] * p.H + h) << page_log2, to = ((int64_t)to_id[g] * p.H + h) << page_log2;
+            copy_code(p.codes + (to + (token & (PAGE - 1))) * p.m, p.codes + (from + (pos[g] & (PAGE - 1))) * p.m, p.m, 0);
+        }
     }
-    if (tid == 0)
-        p.exponents[to] = (int8_t)e;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+#pragma unroll 1
+    for (int x = 0; x < PAGES; ++x) {
+        const int octet0 = x * (PAGE / 8);
+        uint32_t lo[PIECES], hi[PIECES];
+        float most = -1.f;                // (below zero: no token at all)
+        uint32_t odd = 0;                 // pieces that have to be looked at token by token: several exponents, NaN
+        if (x > 0)
+            request(octet0, 0);
+#pragma unroll
+        for (int batch = 0; batch < BATCHES; ++batch) {
+            if (batch + 1 < BATCHES)
+                request(octet0, batch + 1);
+#pragma unroll
+            for (int r = 0; r < kMoveBatch; ++r) {
+                const int piece = batch * kMoveBatch + r, octet = octet0 + piece / CB, d = piece % CB * kWave + lane;
+                lo[piece] = hi[piece] = 0;
+                const int count = __builtin_amdgcn_readfirstlane(octet_n[octet]);
+                auto take = [&](const MoveSource &s, uint64_t y) {
+                    lo[piece] |= __builtin_amdgcn_perm((uint32_t)(y >> 32), (uint32_t)y, s.lo);
+                    hi[piece] |= __builtin_amdgcn_perm((uint32_t)(y >> 32), (uint32_t)y, s.hi);
+                };
+#pragma unroll
+                for (int i = 0; i < kMoveAhead; ++i)
+                    take(sources[octet * 8 + i], ahead[batch & 1][r][i]);
+#pragma unroll 1
+                for (int i = kMoveAhead; i < count; ++i) {
+                    const MoveSource s = sources[octet * 8 + i];
+                    take(s, *reinterpret_cast<const uint64_t *>(values + s.at + d * 8));
+                }
+                if (!count)
+                    continue;
+                const int e = __builtin_amdgcn_readfirstlane(octet_e[octet]);
+                const float y = largest<FP8>(lo[piece], hi[piece]);
+                if (e != kMixed && !__builtin_amdgcn_ballot_w64(y == INFINITY)) {
+                    most = fmaxf(most, y * two_to(e));
+                    continue;
+                }
+                odd |= 1u << piece;
+                float z[8];
+                unpack4<FP8>(lo[piece], *reinterpret_cast<float(*)[4]>(z));
+                unpack4<FP8>(hi[piece], *reinterpret_cast<float(*)[4]>(z + 4));
+                most = fmaxf(most, 0.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)       // (a token that is not there has zeros)
+                    most = fmaxf(most, fabsf(z[i]) * scales[octet * 8 + i]);
+            }
+        }
+        most = wave_max(most);
+        if (most < 0.f)
+            continue;
+        const int e = exponent_of<FP8>(most);
+        // (the page's first token has its new id if any has; behind the sequence's last page nothing is there)
+        const int64_t to = (int64_t)row_out[slot0 + x] * p.H + h;
+        uint64_t *out = reinterpret_cast<uint64_t *>(values + (to << page_log2) * DK);
+#pragma unroll
+        for (int piece = 0; piece < PIECES; ++piece) {
+            const int octet = octet0 + piece / CB, d = piece % CB * kWave + lane;
+            const uint32_t has = __builtin_amdgcn_readfirstlane(octet_has[octet]);
+            if (!has)
+                continue;
+            uint64_t w = (uint64_t)hi[piece] << 32 | lo[piece];
+            const int was = __builtin_amdgcn_readfirstlane(octet_e[octet]);
+            if (odd >> piece & 1) {
+                float y[8];
+                unpack4<FP8>(lo[piece], *reinterpret_cast<float(*)[4]>(y));
+                unpack4<FP8>(hi[piece], *reinterpret_cast<float(*)[4]>(y + 4));
+                const float f = two_to(-e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[i] *= scales[octet * 8 + i] * f;
+                w = (uint64_t)pack4<FP8>(y[4], y[5], y[6], y[7]) << 32 | pack4<FP8>(y[0], y[1], y[2], y[3]);
+            } else if (was != e) {
+                w = (uint64_t)rescale4<FP8>(hi[piece], two_to(was - e)) << 32 | rescale4<FP8>(lo[piece], two_to(was - e));
+            }
+            uint64_t *dst = out + (piece / CB) * DK + d;
+            if (has != 0xff) {            // (what lies behind the last token stays)
+                uint64_t mask = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    mask |= has >> i & 1 ? 0xffull << (8 * i) : 0;
+                w = (w & mask) | (*dst & ~mask);
+            }
+            __builtin_nontemporal_store(w, dst);
+        }
+        if (lane == 0)
+            p.exponents[to] = (int8_t)e;
+    }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
@@ -505,6 +716,12 @@ static int check_evict(const lookat_page_pool *pool, int32_t B, int32_t W, int32
     if (B > 65535 || (int64_t)W * pool->page > (1 << 30) || (int64_t)W_out * pool->page > (1 << 30))
         return fail(LOOKAT_ERR_UNSUPPORTED, "B=%d, W=%d, W_out=%d pages of %d tokens: at most 65535 sequences of 2^30 tokens", B, W, W_out, pool->page);
     return LOOKAT_OK;
+}
+template <int PAGE>
+static auto move_kernel(int d_k, bool fp8)
+{
+    return d_k == 64 ? (fp8 ? &evict_move_kernel<64, true, PAGE> : &evict_move_kernel<64, false, PAGE>)
+                     : (fp8 ? &evict_move_kernel<128, true, PAGE> : &evict_move_kernel<128, false, PAGE>);
 }
 static size_t evict_bytes(const lookat_page_pool *p, int32_t B, int32_t W_out) { return (size_t)B * p->H * W_out * p->page * 4; }
 
@@ -613,7 +830,8 @@ extern "C" int lookat_pages_evict(const lookat_page_pool *pool, int32_t B, const
     if (!aligned16(workspace))
         return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
     const int64_t units = (int64_t)B * pool->H;
-    if (!fits_launch(units, kPickThreads) || !fits_launch(W_out, kMoveThreads))
+    const int per_group = (pool->page < kWave ? kWave / pool->page : 1) * kMoveWaves, groups = (W_out + per_group - 1) / per_group;
+    if (!fits_launch(units, kPickThreads) || !fits_launch(groups, kMoveThreads))
         return fail(LOOKAT_ERR_UNSUPPORTED, "B*H=%lld heads or W_out=%d pages exceed one launch", (long long)units, W_out);
     const PoolArgs p = pool_args(pool);
     EvictArgs a;
@@ -635,12 +853,20 @@ extern "C" int lookat_pages_evict(const lookat_page_pool *pool, int32_t B, const
     a.first = first;
     a.recent = recent;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(evict_pick_kernel, dim3((unsigned)units), dim3(kPickThreads), 0, st, a, p.H, p.page_log2);
+    // (by the room of a row; a variant for few tokens is short code: {PICK})
+    const int64_t each = ((int64_t)W * pool->page + kPickThreads - 1) / kPickThreads;
+    const auto pick = each <= 2    ? &evict_pick_kernel<2>
+                      : each <= 8  ? &evict_pick_kernel<8>
+                      : each <= 32 ? &evict_pick_kernel<32>
+                                   : &evict_pick_kernel<0>;
+    hipLaunchKernelGGL(pick, dim3((unsigned)units), dim3(kPickThreads), 0, st, a, p.H, p.page_log2);
     if (int rc = check_launch("lookat_pages_evict (choice)"))
         return rc;
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
-    const auto f = p.d_k == 64 ? (fp8 ? &evict_move_kernel<64, true> : &evict_move_kernel<64, false>)
-                               : (fp8 ? &evict_move_kernel<128, true> : &evict_move_kernel<128, false>);
-    hipLaunchKernelGGL(f, dim3((unsigned)W_out, (unsigned)p.H, (unsigned)B), dim3(kMoveThreads), 0, st, p, a);
+    const auto f = pool->page == 16   ? move_kernel<16>(p.d_k, fp8)
+                   : pool->page == 32 ? move_kernel<32>(p.d_k, fp8)
+                   : pool->page == 64 ? move_kernel<64>(p.d_k, fp8)
+                                      : move_kernel<128>(p.d_k, fp8);
+    hipLaunchKernelGGL(f, dim3((unsigned)groups, (unsigned)p.H, (unsigned)B), dim3(kMoveThreads), 0, st, p, a);
     return check_launch("lookat_pages_evict");
 }

@@ -175,9 +175,10 @@ def spread_weights(rng, *shape):
 
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 @pytest.mark.parametrize("d_k,m,page", [(64, 4, 16), (64, 2, 64), (128, 8, 32), (128, 16, 128), (64, 16, 128)])
-@pytest.mark.parametrize("first,recent", [(0, 0), (4, 30), (1000, 7), (3, 1000)])
-def test_evict(lk, d_k, m, page, kind, first, recent):  # noqa: F811
-    """Lengths of zero and one, all kept, none, one, pages that end inside the kept tokens, ties, places for fewer than asked."""
+@pytest.mark.parametrize("first,recent,room", [(0, 0, 0), (4, 30, 0), (1000, 7, 0), (3, 1000, 0), (4, 30, 1 << 14)])
+def test_evict(lk, d_k, m, page, kind, first, recent, room):  # noqa: F811
+    """Lengths of zero and one, all kept, none, one, pages that end inside the kept tokens, ties, places for fewer than asked, rows with room for many
+    more tokens (which the launch goes by)."""
     rng = np.random.default_rng(page + first)
     H, B = 2, 9
     lengths = [200, 1, 0, page, 129, 200, 64, 200, 77]
@@ -189,6 +190,9 @@ def test_evict(lk, d_k, m, page, kind, first, recent):  # noqa: F811
     ids = rng.permutation(P).astype(np.int32)
     table = ids[:B * W].reshape(B, W)
     table_out = ids[B * W: B * (W + W_out)].reshape(B, W_out)
+    if room:
+        W_out = room // page
+        table_out = np.concatenate([table_out, np.full((B, W_out - table_out.shape[1]), -1, np.int32)], 1)
     weights = spread_weights(rng, B, H, 200)
     weights[0, 0, 20:40] = -weights[0, 0, 20:40]
     out = np.full((B, H, 90), -5.0, np.float32)
