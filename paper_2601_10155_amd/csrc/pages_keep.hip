@@ -20,15 +20,15 @@ struct WeighArgs {
     float scale_log2e, decay;
 };
 
-constexpr int kWeighThreads = 1024, kWeighWaves = kWeighThreads / kWave, kWeighScores = 32;
+constexpr int kWeighThreads = 1024, kWeighWaves = kWeighThreads / kWave, kWeighScores = 32, kWeighFew = 4;
 __host__ __device__ constexpr int weigh_tokens(int G) { return kWeighThreads * (kWeighScores / G); }     // of a range, at most
 
 enum WeighPhase { kWeighAll, kWeighStats, kWeighAdd };
 
-template <int M, int G, int PHASE>
+template <int M, int G, int PHASE, int T>
 __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighArgs a)
 {
-    constexpr int GP = G < 4 ? G : 4, PLANES = G / GP, T = kWeighScores / G;
+    constexpr int GP = G < 4 ? G : 4, PLANES = G / GP;
     typedef float vg __attribute__((ext_vector_type(GP)));
     extern __shared__ __align__(16) float tables[];       // [plane][i][c][head of the plane]
     __shared__ float red[2][G][kWeighWaves];
@@ -43,12 +43,66 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         return;
     const int32_t *row = a.table + b * a.table_stride;
     const int page_mask = (1 << p.page_log2) - 1;
+    const uint32_t code_step = (uint32_t)(p.H * M) << p.page_log2;
+    const uint8_t *head_codes = p.codes + ((uint32_t)(h * M) << p.page_log2);
 
+    // The first tokens' pages and codes are requested ahead of the tables, the old weights behind them: they are needed last.  Then one group of
+    // tokens is requested while the one before it is looked up.
+    constexpr int WORDS = (M + 3) / 4, most = WORDS == 4 || G == 8 ? 2 : 4, U = T < most ? T : most;
+    static_assert(T % U == 0, "whole groups");
+    uint32_t codes[2][U][WORDS];
+    bool there[2][U];
+    auto request = [&](int t0) {
+        int id[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int key = k0 + (t0 + u) * kWeighThreads + tid;
+            id[u] = row[(key < k1 ? key : k1 - 1) >> p.page_log2];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int key = k0 + (t0 + u) * kWeighThreads + tid;
+            there[t0 / U & 1][u] = key < k1 && (uint32_t)id[u] < (uint32_t)p.pages;
+            const uint8_t *c = head_codes + (uint64_t)(uint32_t)(there[t0 / U & 1][u] ? id[u] : 0) * code_step + (uint32_t)(key & page_mask) * M;
+            if constexpr (M == 2) {
+                codes[t0 / U & 1][u][0] = *reinterpret_cast<const uint16_t *>(c);
+            } else if constexpr (M == 4) {
+                codes[t0 / U & 1][u][0] = *reinterpret_cast<const uint32_t *>(c);
+            } else if constexpr (M == 8) {
+                const v2u x = *reinterpret_cast<const v2u *>(c);
+                codes[t0 / U & 1][u][0] = x.x, codes[t0 / U & 1][u][1] = x.y;
+            } else {
+                const v4u x = *reinterpret_cast<const v4u *>(c);
+                codes[t0 / U & 1][u][0] = x.x, codes[t0 / U & 1][u][1] = x.y, codes[t0 / U & 1][u][2] = x.z, codes[t0 / U & 1][u][3] = x.w;
+            }
+        }
+    };
+    request(0);
     {
-        const float *lut = a.lut + (int64_t)unit * G * M * kCentroids;
-        for (int j = tid; j < G * M * kCentroids; j += kWeighThreads) {
-            const int g = j / (M * kCentroids), entry = j % (M * kCentroids);
-            tables[(g / GP * M * kCentroids + entry) * GP + g % GP] = lut[j] * a.scale_log2e;
+        const v4f *lut = reinterpret_cast<const v4f *>(a.lut + (int64_t)unit * G * M * kCentroids);
+        for (int j = tid; j < PLANES * M * (kCentroids / 4); j += kWeighThreads) {
+            const int plane = j / (M * (kCentroids / 4)), entry = j % (M * (kCentroids / 4));
+            v4f x[GP];
+#pragma unroll
+            for (int g = 0; g < GP; ++g)
+                x[g] = lut[(plane * GP + g) * (M * (kCentroids / 4)) + entry];
+#pragma unroll
+            for (int k = 0; k < GP; ++k) {                // ordered entry, head
+                v4f y;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    y[w] = x[(4 * k + w) % GP][(4 * k + w) / GP] * a.scale_log2e;
+                reinterpret_cast<v4f *>(tables)[j * GP + k] = y;
+            }
+        }
+    }
+    float *weights = a.weights + (int64_t)unit * a.weight_stride;
+    float old[T];
+    if constexpr (PHASE != kWeighStats) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int key = k0 + t * kWeighThreads + tid;
+            old[t] = a.decay != 0.f && key < k1 && key < a.columns ? weights[key] : 0.f;
         }
     }
     __syncthreads();
@@ -58,42 +112,39 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
     for (int g = 0; g < G; ++g)
         top[g] = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
+    for (int t0 = 0; t0 < T; t0 += U) {
+        if (k0 + t0 * kWeighThreads >= k1) {
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-            y[t][g] = -INFINITY;
-        const int key = k0 + t * kWeighThreads + tid;
-        if (k0 + t * kWeighThreads < k1 && key < k1) {
-            const int id = row[key >> p.page_log2];
-            if ((uint32_t)id < (uint32_t)p.pages) {
-                const uint8_t *c = p.codes + ((((int64_t)id * p.H + h) << p.page_log2) + (key & page_mask)) * M;
-                uint32_t codes[(M + 3) / 4];
-                if constexpr (M == 2) {
-                    codes[0] = *reinterpret_cast<const uint16_t *>(c);
-                } else if constexpr (M == 4) {
-                    codes[0] = *reinterpret_cast<const uint32_t *>(c);
-                } else if constexpr (M == 8) {
-                    const v2u x = *reinterpret_cast<const v2u *>(c);
-                    codes[0] = x.x, codes[1] = x.y;
-                } else {
-                    const v4u x = *reinterpret_cast<const v4u *>(c);
-                    codes[0] = x.x, codes[1] = x.y, codes[2] = x.z, codes[3] = x.w;
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    y[t0 + u][g] = -INFINITY;
+            continue;
+        }
+        if (t0 + U < T && k0 + (t0 + U) * kWeighThreads < k1)
+            request(t0 + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int q = 0; q < PLANES; ++q) {
+                vg s = {};
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    if (G * M >= 16 && i % (16 / GP) == 0)
+                        __builtin_amdgcn_sched_barrier(0);        // (look-ups in flight at once: 16 registers of them)
+                    s += reinterpret_cast<const vg *>(tables)[(q * M + i) * kCentroids + ((codes[t0 / U & 1][u][i / 4] >> (8 * (i % 4))) & 0xffu)];
                 }
 #pragma unroll
-                for (int q = 0; q < PLANES; ++q) {
-                    vg s = {};
-#pragma unroll
-                    for (int i = 0; i < M; ++i)
-                        s += reinterpret_cast<const vg *>(tables)[(q * M + i) * kCentroids + ((codes[i / 4] >> (8 * (i % 4))) & 0xffu)];
-#pragma unroll
-                    for (int g = 0; g < GP; ++g)
-                        y[t][q * GP + g] = s[g];
+                for (int g = 0; g < GP; ++g) {
+                    const float x = GP == 1 ? (float)s[0] : (float)s[g];
+                    y[t0 + u][q * GP + g] = there[t0 / U & 1][u] ? x : -INFINITY;
+                    if constexpr (PHASE == kWeighAdd)
+                        asm volatile("" : "+v"(y[t0 + u][q * GP + g]));   // (summed up here: not all terms kept until the maximum is known)
+                    else
+                        top[q * GP + g] = fmaxf(top[q * GP + g], y[t0 + u][q * GP + g]);
                 }
             }
         }
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-            top[g] = fmaxf(top[g], y[t][g]);
     }
 
     // (a maximum of -inf counts as 0: differences are -inf then, and weights nothing)
@@ -129,11 +180,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWeighWaves; ++w)
-                s += red[1][g][w];
-            sum[g] = s;
+            sum[g] = wave_sum(lane < kWeighWaves ? red[1][g][lane] : 0.f);
         }
         if constexpr (PHASE == kWeighStats) {
             if (tid < G) {
@@ -154,10 +201,12 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float m = -INFINITY, s = 0.f;
+#pragma unroll 1
             for (int r = lane; r < ranges; r += kWave)
                 m = fmaxf(m, stats[r * G + g].x);
             m = wave_max(m);
             m = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
             for (int r = lane; r < ranges; r += kWave)
                 s = fmaf(stats[r * G + g].y, fast_exp2(stats[r * G + g].x - m), s);
             top[g] = m;
@@ -173,7 +222,6 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
 #pragma unroll
     for (int g = 0; g < G; ++g)
         sum[g] = sum[g] == 0.f ? 0.f : 1.f / sum[g];
-    float *weights = a.weights + (int64_t)unit * a.weight_stride;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
         const int key = k0 + t * kWeighThreads + tid;
@@ -182,7 +230,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
 #pragma unroll
             for (int g = 1; g < G; ++g)
                 w = fmaf(y[t][g], sum[g], w);
-            weights[key] = a.decay == 0.f ? w : fmaf(a.decay, weights[key], w);
+            weights[key] = a.decay == 0.f ? w : fmaf(a.decay, old[t], w);
         }
     }
 }
@@ -674,11 +722,11 @@ static int check_weigh(const lookat_page_pool *pool, int32_t B, int32_t group, i
     return LOOKAT_OK;
 }
 
-template <int M, int G, int PHASE>
+template <int M, int G, int PHASE, int T>
 static int launch_weigh_phase(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
 {
     constexpr size_t lds = (size_t)G * M * kCentroids * 4;
-    const auto f = &weigh_kernel<M, G, PHASE>;
+    const auto f = &weigh_kernel<M, G, PHASE, T>;
     if (lds > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
@@ -687,14 +735,21 @@ static int launch_weigh_phase(const PoolArgs &p, const WeighArgs &a, int64_t gro
     hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(kWeighThreads), lds, st, p, a);
     return check_launch("lookat_pages_weigh");
 }
+template <int M, int G, int T>
+static int launch_weigh_phases(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
+{
+    if (a.splits == 1)
+        return launch_weigh_phase<M, G, kWeighAll, T>(p, a, groups, st);
+    if (int rc = launch_weigh_phase<M, G, kWeighStats, T>(p, a, groups, st))
+        return rc;
+    return launch_weigh_phase<M, G, kWeighAdd, T>(p, a, groups, st);
+}
+// Few scores a thread where that is enough: short code ({WSHORT}).
 template <int M, int G>
 static int launch_weigh(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
 {
-    if (a.splits == 1)
-        return launch_weigh_phase<M, G, kWeighAll>(p, a, groups, st);
-    if (int rc = launch_weigh_phase<M, G, kWeighStats>(p, a, groups, st))
-        return rc;
-    return launch_weigh_phase<M, G, kWeighAdd>(p, a, groups, st);
+    constexpr int few = kWeighFew / G > 0 ? kWeighFew / G : 1;
+    return a.chunk <= few * kWeighThreads ? launch_weigh_phases<M, G, few>(p, a, groups, st) : launch_weigh_phases<M, G, kWeighScores / G>(p, a, groups, st);
 }
 template <int M>
 static int launch_weigh_g(int G, const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
