@@ -229,7 +229,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
     constexpr int CODES = SMALL ? 2 * CPT : CPT;
     uint32_t codes[CODES];
     int exponent;
-    auto load_codes = [&](int t, int raw_id) {
+    auto load_codes = [&](int t, int raw_id, uint32_t (&codes)[CODES], int &exponent) {
         const int id = page_of(t, raw_id);
         const uint32_t page = id < 0 ? 0 : id;
         const uint8_t *c = head_codes + (uint64_t)page * code_step + (uint32_t)(((t * KEYS + kk) & page_mask) * p.m);
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
     };
     v4u piece[CPT][2];
     const char *books = a.books + (int64_t)h * kCentroids * DK * 4;
-    auto load_centroids = [&]() {
+    auto load_centroids = [&](const uint32_t (&codes)[CODES], v4u (&piece)[CPT][2]) {
 #pragma unroll
         for (int j = 0; j < CPT; ++j) {
             const int chunk = sub + j * TPK;
@@ -264,7 +264,13 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             }
         }
     };
-    auto put_keys = [&](int t, int raw_id, int e) {
+    auto put_page = [&](int t, int id, int e) {
+        if ((kk & 15) == 0 && sub == 0) {
+            ids_s[t & 3][kk >> 4] = id;
+            exps_s[t & 3][kk >> 4] = id < 0 ? 0 : e;
+        }
+    };
+    auto put_keys = [&](int t, int raw_id, int e, const v4u (&piece)[CPT][2]) {
         const int id = page_of(t, raw_id);
         char *to = keys_s + (t & 1) * kBuffer + krow * (DK * 2);
 #pragma unroll
@@ -280,10 +286,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             *reinterpret_cast<v4u *>(to + at) = hi;
             *reinterpret_cast<v4u *>(to + kPlane + at) = lo;
         }
-        if ((kk & 15) == 0 && sub == 0) {
-            ids_s[t & 3][kk >> 4] = id;
-            exps_s[t & 3][kk >> 4] = id < 0 ? 0 : e;
-        }
+        put_page(t, id, e);
     };
     // ---- the values of a tile ----
     v4u stored[VPT];
@@ -390,20 +393,26 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             }
     };
 
-    // Two tiles of keys and one of values are staged, the scores of the first are there before the loop.
-    load_codes(range.t0, id0);
-    load_centroids();
-    const int exponent0 = exponent;
-    load_codes(range.t0 + 1, id1);
-    put_keys(range.t0, id0, exponent0);
-    load_centroids();
-    const int exponent1 = exponent;
-    load_codes(range.t0 + 2, id2);
-    put_keys(range.t0 + 1, id1, exponent1);
+    // Two tiles of keys and one of values are staged, the scores of the first are there before the loop.  (What can be requested together is: page
+    // ids, then the codes of three tiles and the values, then the centroids of two.)
+    put_page(range.t0, page_of(range.t0, id0), 0);
     __syncthreads();
     load_values(range.t0);
-    score(range.t0, s);
+    {
+        uint32_t codes0[CODES], codes1[CODES];
+        int exponent0, exponent1;
+        v4u piece1[CPT][2];
+        load_codes(range.t0, id0, codes0, exponent0);
+        load_codes(range.t0 + 1, id1, codes1, exponent1);
+        load_codes(range.t0 + 2, id2, codes, exponent);
+        load_centroids(codes0, piece);
+        load_centroids(codes1, piece1);
+        put_keys(range.t0, id0, exponent0, piece);
+        put_keys(range.t0 + 1, id1, exponent1, piece1);
+    }
     put_values(range.t0);
+    __syncthreads();
+    score(range.t0, s);
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -425,8 +434,8 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
         load_values(t + 1);
         int e2 = exponent;
         asm volatile("" : "+v"(e2));      // (else its load is moved into the branch that stores it, and waited for there)
-        load_centroids();
-        load_codes(t + 3, id3);
+        load_centroids(codes, piece);
+        load_codes(t + 3, id3, codes, exponent);
         const int id4 = load_id(t + 4);
 
         // score i of block k belongs to token 32 k + 16 (i / 8) + 8 half + i % 8
@@ -487,7 +496,7 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
             }
         }
         // (these buffers were last read before the barrier that ended the tile before)
-        put_keys(t + 2, id2, e2);
+        put_keys(t + 2, id2, e2, piece);
         put_values(t + 1);
 #pragma unroll
         for (int k = 0; k < KB; ++k)
@@ -890,11 +899,15 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
 {
     ChunkCut c;
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
-    c.few = rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+    // The kernel for few rows, us a call with it / without: 416 (sequence, head) pairs x 64 rows x 600 tokens, d_k = 128 54 / 78, 32 x 40 x 1000 23 / 38,
+    // 8 x 64 x 8000 32 / 44, 256 x 64 x 4000 142 / 256, d_k = 64 96 x 64 x 1000 18 / 32; with nothing to see but the chunk's own tokens
+    // (1856 x 43) 40 / 27.  128 rows: 32 x 1000 26 / 36, 48 x 500 15 / 27, but 128 x 4000 138 / 108.
+    const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
+    const bool few = rows <= 32 || (longest > 256 && (rows <= 64 || (rows <= 128 && units <= 64)));
+    c.few = !few ? 0 : rows <= 16 ? 1 : 2;
     c.waves = c.few ? kFewWaves : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
-    const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
     c.splits = num_splits;
     if (!num_splits) {
         const int64_t target = 256 * 8 / c.waves, most = (longest + 511) / 512;
