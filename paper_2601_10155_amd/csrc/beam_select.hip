@@ -2,8 +2,8 @@
 //
 // Two launches.  In the first a wavefront takes 64 E consecutive logits of a row, E to a lane, in registers: their maximum m, their n best in order, and
 // the sum of exp(x - m).  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots); few logits reach
-// it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n, many equal logits) the n-th best itself is found
-// bit by bit, first its value, then among equal ones its place.  Listed logits near m enter the sum in 64 bits, so that the terms that
+// it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n) the n-th best itself is found bit by bit
+// among them, first its value, then among equal ones its place; where more than kListed do (many equal logits), among all.  Listed logits near m enter the sum in 64 bits, so that the terms that
 // dominate a row's sum carry no fp32 rounding; the others' roundings average out.
 // In the second launch a workgroup takes a request.  A lower bound on the n-th best score, found as above from a few entries of every sorted list,
 // leaves few candidates, whose places are counted.  Where more than kMostFound reach the bound (many equal scores) each wavefront takes the n best of its
@@ -32,6 +32,8 @@ struct SelectArgs {
 };
 
 constexpr int kSelectWaves = 4, kSelectThreads = kSelectWaves * kWave;
+constexpr int kShare = 8, kListed = kShare * kWave;       // logits of a part that reach the first border, at most, before the search goes over all
+constexpr int kPlaceBits = 11;                            // of a logit's number in its part
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kNear = 3.f;              // listed logits that are nearer to their part's maximum enter its sum in 64 bits
@@ -44,6 +46,12 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+// What this wavefront's lanes wrote to LDS before is there for its lanes' reads behind it.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 __device__ __forceinline__ int ballot_count(bool b) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b)); }
 
 __device__ __forceinline__ double wave_sum_double(double x)
@@ -58,7 +66,8 @@ template <typename FT, int E>
 __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs a)
 {
     constexpr int PER = 16 / (int)sizeof(FT), LOADS = E / PER;     // a load's logits
-    __shared__ uint64_t lists[kSelectWaves][kWave];
+    static_assert(kWave * E <= 1 << kPlaceBits, "a logit's number fits its bits");
+    __shared__ uint64_t lists[kSelectWaves][kListed];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t item = (int64_t)blockIdx.x * kSelectWaves + wave;
     const int row = (int)(item / a.parts), part = (int)(item - (int64_t)row * a.parts);
@@ -126,7 +135,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
             const uint64_t mask = __builtin_amdgcn_ballot_w64(list);
             if (mask) {
                 const int place = found + __builtin_popcountll(mask & below);
-                if (list && place < kWave)
+                if (list && place < kListed)
                     lists[wave][place] = (uint64_t)ordered(x[j]) << 32 | (uint32_t)~number(j);
                 found += __builtin_popcountll(mask);
             }
@@ -136,7 +145,41 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     };
     sweep(std::true_type(), border, 0);
     float ties = 0.f;                     // logits at the border that are not listed
-    if (found > kWave) {
+    if (found > kWave && found <= kListed) {
+        // The n greatest of the list, every lane with its share of it: first the n-th logit, then, of equal ones, the n-th place.
+        wave_fence();
+        uint64_t keys[kShare];
+#pragma unroll
+        for (int j = 0; j < kShare; ++j)
+            keys[j] = j * kWave + lane < found ? lists[wave][j * kWave + lane] : 0;
+        uint64_t nth = 0;
+#pragma unroll 1
+        for (int bit = 63; bit >= 0; bit = bit == 32 ? kPlaceBits - 1 : bit - 1) {
+            if (bit == kPlaceBits - 1)
+                nth |= 0xffffffffu >> kPlaceBits << kPlaceBits;       // (a place is the complement of a number below 2^kPlaceBits)
+            const uint64_t t = nth | 1ull << bit;
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < kShare; ++j)
+                if (j * kWave < found)
+                    c += ballot_count(keys[j] >= t);
+            nth = c >= a.n ? t : nth;
+        }
+        wave_fence();
+        int kept = 0;
+#pragma unroll
+        for (int j = 0; j < kShare; ++j)
+            if (j * kWave < found) {
+                const bool keep = keys[j] >= nth;
+                const uint64_t mask = __builtin_amdgcn_ballot_w64(keep);
+                if (keep)
+                    lists[wave][kept + __builtin_popcountll(mask & below)] = keys[j];
+                else if (keys[j])
+                    rest += fast_exp2((unordered((uint32_t)(keys[j] >> 32)) - base) * kLog2eF);
+                kept += __builtin_popcountll(mask);
+            }
+        found = kept;
+    } else if (found > kWave) {
         uint32_t nth = 0;
         for (int bit = 31; bit >= 0; --bit) {
             const float t = unordered(nth | 1u << bit);
@@ -171,8 +214,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
         }
         sweep(std::false_type(), border, most);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     const uint64_t key = lane < found ? lists[wave][lane] : 0;
     int rank = 0;
     for (int j = 0; j < found; ++j) {
@@ -220,17 +262,19 @@ __device__ __forceinline__ bool ahead(const Pick &a, const Pick &b)
 // A score as fp32; those below its range, which are candidates all the same, as its lowest number.
 __device__ __forceinline__ float rounded(double score) { return score > -(double)INFINITY ? fmaxf((float)score, kLowest) : -INFINITY; }
 
+// Four wavefronts: the bound is found by each of them from all threads' best (us for 4 beams of 50257, four / eight / sixteen 8.0 / 9.9 / 16.0).
+constexpr int kMergeWaves = 4, kMergeThreads = kMergeWaves * kWave;
 constexpr int kMostPicks = 64, kMostBeams = 1024, kMostFound = 1024, kBatch = 4;
 
-__global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs a)
+__global__ __launch_bounds__(kMergeThreads) void select_merge_kernel(SelectArgs a)
 {
     __shared__ double bases[kMostBeams];
     __shared__ Pick picks[kMostFound];
-    __shared__ uint32_t tops[kSelectThreads];
+    __shared__ uint32_t tops[kMergeThreads];
     __shared__ int found_s;
     const int q = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = a.n, parts = a.parts;
     const int64_t row0 = (int64_t)q * a.beams;
-    for (int r = wave; r < a.beams; r += kSelectWaves) {
+    for (int r = wave; r < a.beams; r += kMergeWaves) {
         const PartSum *stats = a.stats + (row0 + r) * parts;
         float m = -INFINITY;
         for (int j = lane; j < parts; j += kWave)
@@ -251,22 +295,23 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
     }
     __syncthreads();
 
-    const int lists = a.beams * parts, step = kSelectThreads;
+    const int lists = a.beams * parts, step = kMergeThreads;
+    const float *best = a.best + row0 * parts * n;        // the lists of a request follow each other
+    const int32_t *best_tokens = a.best_tokens + row0 * parts * n;
     auto candidate = [&](int list, int j) -> Pick {
         Pick c;
         c.row = list / parts;
-        const int64_t at = ((row0 + c.row) * parts + (list - c.row * parts)) * n + j;
-        c.logit = a.best[at];
-        c.token = a.best_tokens[at];      // (not looked at where the logit is -inf)
+        c.logit = best[(int64_t)list * n + j];
+        c.token = best_tokens[(int64_t)list * n + j];     // (not looked at where the logit is -inf)
         c.score = bases[c.row] + (double)c.logit;
         return c;
     };
     // the best of this lane's lists behind `last`
     auto next = [&](bool any, const Pick &last) -> Pick {
-        Pick best;
-        best.score = -(double)INFINITY;
-        best.row = best.token = 0x7fffffff;
-        best.logit = -INFINITY;
+        Pick first;
+        first.score = -(double)INFINITY;
+        first.row = first.token = 0x7fffffff;
+        first.logit = -INFINITY;
         for (int list = wave * kWave + lane; list < lists; list += step)
             for (int j = 0; j < n; ++j) {
                 const Pick c = candidate(list, j);
@@ -274,11 +319,11 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
                     break;
                 if (any && !ahead(last, c))
                     continue;
-                if (ahead(c, best))
-                    best = c;
+                if (ahead(c, first))
+                    first = c;
                 break;
             }
-        return best;
+        return first;
     };
     // the wavefronts' n best of their lists, into picks
     auto one_by_one = [&]() {
@@ -288,10 +333,10 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
 #pragma unroll
             for (int d = 1; d < kWave; d *= 2)
                 top = fmax(top, __shfl_xor(top, d));
-            Pick best;
-            best.score = top;
-            best.row = best.token = -1;
-            best.logit = -INFINITY;
+            Pick pick;
+            pick.score = top;
+            pick.row = pick.token = -1;
+            pick.logit = -INFINITY;
             int owner = -1;
             if (top > -(double)INFINITY) {
                 uint64_t tied = __builtin_amdgcn_ballot_w64(mine.score == top);
@@ -303,57 +348,74 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
                     c.row = __builtin_amdgcn_readlane(mine.row, l);
                     c.token = __builtin_amdgcn_readlane(mine.token, l);
                     c.logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.logit), l));
-                    if (owner < 0 || ahead(c, best)) {
-                        best = c;
+                    if (owner < 0 || ahead(c, pick)) {
+                        pick = c;
                         owner = l;
                     }
                 }
             }
             if (lane == 0)
-                picks[wave * n + k] = best;
+                picks[wave * n + k] = pick;
             if (lane == owner)
-                mine = next(true, best);
+                mine = next(true, pick);
         }
     };
     // A bound that n candidates reach, from the first `deep` entries of every list (rounded to fp32, which keeps their order).
-    const int deep = lists >= kSelectThreads ? 1 : (kSelectThreads + lists - 1) / lists < n ? (kSelectThreads + lists - 1) / lists : n;
+    const int deep = lists >= kMergeThreads ? 1 : (kMergeThreads + lists - 1) / lists < n ? (kMergeThreads + lists - 1) / lists : n;
     float top = -INFINITY;
-    for (int item = threadIdx.x; item < lists * deep; item += step) {
-        const int list = item / deep;
-        top = fmaxf(top, rounded(bases[list / parts] + (double)a.best[(row0 * parts + list) * n + item - list * deep]));
+    for (int item0 = threadIdx.x; item0 < lists * deep; item0 += kBatch * step) {
+        float x[kBatch];
+        int row[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int item = item0 + u * step < lists * deep ? item0 + u * step : item0, list = item / deep;
+            row[u] = list / parts;
+            x[u] = best[(int64_t)list * n + item - list * deep];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            top = fmaxf(top, rounded(bases[row[u]] + (double)x[u]));
     }
     tops[threadIdx.x] = ordered(top);
     if (threadIdx.x == 0)
         found_s = 0;
     __syncthreads();
-    uint32_t order[kSelectWaves], bound = 0;
+    uint32_t order[kMergeWaves], bound = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w)
+    for (int w = 0; w < kMergeWaves; ++w)
         order[w] = tops[w * kWave + lane];
 #pragma unroll
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t t = bound | 1u << bit;
         int c = 0;
 #pragma unroll
-        for (int w = 0; w < kSelectWaves; ++w)
+        for (int w = 0; w < kMergeWaves; ++w)
             c += ballot_count(order[w] >= t);
         bound = c >= n ? t : bound;
     }
     const float border = fmaxf(unordered(bound), kLowest);
-    for (int list = threadIdx.x; list < lists; list += step) {
-        bool more = true;
-        for (int j0 = 0; j0 < n && more; j0 += kBatch) {
-            Pick c[kBatch];
+    for (int list0 = threadIdx.x; list0 < lists; list0 += kBatch * step) {
+        float heads[kBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                c[i] = candidate(list, j0 + i < n ? j0 + i : n - 1);
+        for (int u = 0; u < kBatch; ++u)
+            heads[u] = best[(int64_t)(list0 + u * step < lists ? list0 + u * step : list0) * n];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                more = more && j0 + i < n && rounded(c[i].score) >= border;
-                if (more) {
-                    const int at = atomicAdd(&found_s, 1);
-                    if (at < kMostFound)
-                        picks[at] = c[i];
+        for (int u = 0; u < kBatch; ++u) {
+            const int list = list0 + u * step;
+            bool more = list < lists && rounded(bases[list / parts] + (double)heads[u]) >= border;
+            for (int j0 = 0; j0 < n && more; j0 += kBatch) {
+                Pick c[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    c[i] = candidate(list, j0 + i < n ? j0 + i : n - 1);
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    more = more && j0 + i < n && rounded(c[i].score) >= border;
+                    if (more) {
+                        const int at = atomicAdd(&found_s, 1);
+                        if (at < kMostFound)
+                            picks[at] = c[i];
+                    }
                 }
             }
         }
@@ -363,13 +425,13 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
     const bool listed = found > kMostFound;
     if (listed) {
         __syncthreads();
-        found = kSelectWaves * n;
+        found = kMergeWaves * n;
         one_by_one();
         __syncthreads();
     }
     __syncthreads();
     // a thread per candidate: its place is the number of those ahead of it
-    for (int i = threadIdx.x; i < found; i += kSelectThreads) {
+    for (int i = threadIdx.x; i < found; i += kMergeThreads) {
         const Pick c = picks[i];
         if (!(c.score > -(double)INFINITY))
             continue;
@@ -387,7 +449,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_merge_kernel(SelectArgs
     if (listed)
         for (int j = 0; j < found; ++j)
             real -= !(picks[j].score > -(double)INFINITY);
-    for (int j = real + threadIdx.x; j < n; j += kSelectThreads) {
+    for (int j = real + threadIdx.x; j < n; j += kMergeThreads) {
         a.scores_out[(int64_t)q * n + j] = -INFINITY;
         a.parents[(int64_t)q * n + j] = a.tokens[(int64_t)q * n + j] = -1;
     }
@@ -485,6 +547,6 @@ extern "C" int lookat_beam_select(int32_t Q, int32_t beams, int32_t V, int32_t n
     hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(kSelectThreads), 0, st, a);
     if (int rc = check_launch("lookat_beam_select (rows)"))
         return rc;
-    hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)Q), dim3(kSelectThreads), 0, st, a);
+    hipLaunchKernelGGL(select_merge_kernel, dim3((unsigned)Q), dim3(kMergeThreads), 0, st, a);
     return check_launch("lookat_beam_select");
 }
