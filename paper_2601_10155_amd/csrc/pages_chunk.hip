@@ -534,11 +534,11 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
 // Few rows (drafted tokens, the ends of prompts): 16 RB rows of a (sequence, head) to a workgroup, whose wavefronts take tiles of 32 tokens in turn, each
 // for itself: centroids go straight from the books to the operand's registers, values as in attention of one token, and the wavefronts'
 // results are merged in LDS.  v_mfma_f32_16x16x32_f16: keys are dealt to the two blocks of 16 such that a lane's eight scores belong to one octet.
-constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kFewKeys = 32;
-__host__ __device__ constexpr size_t few_lds_bytes(int d_k) { return (size_t)kFewWaves * 16 * (d_k + 4) * 4 + kFewWaves * 16 * 8; }
+constexpr int kFewWaves = 8, kBriefWaves = 2, kFewKeys = 32;
+__host__ __device__ constexpr size_t few_lds_bytes(int d_k, int waves) { return (size_t)waves * 16 * (d_k + 4) * 4 + waves * 16 * 8; }
 
-template <int DK, bool SMALL, bool Q32, bool FP8, int RB>
-__global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, ChunkArgs a)
+template <int DK, bool SMALL, bool Q32, bool FP8, int RB, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, ChunkArgs a)
 {
     constexpr int STEPS = DK / 32, CB = DK / 32, TQ = 16 * RB, ROW = DK + 4;
     extern __shared__ __align__(16) char few_s[];
@@ -612,8 +612,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
     };
 
     int t = range.t0 + wave;
-    int id_k0 = load_id(t, my_octet), id_k1 = load_id(t + kFewWaves, my_octet), id_k2 = load_id(t + 2 * kFewWaves, my_octet);
-    int id_v0 = load_id(t, quad), id_v1 = load_id(t + kFewWaves, quad);
+    int id_k0 = load_id(t, my_octet), id_k1 = load_id(t + WAVES, my_octet), id_k2 = load_id(t + 2 * WAVES, my_octet);
+    int id_v0 = load_id(t, quad), id_v1 = load_id(t + WAVES, quad);
 
     // the rows as operand: coordinates 32 s + 8 quad .. + 7 of row `col` of every block
     v8h qh[RB][STEPS], ql[Q32 ? RB : 1][STEPS];
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
     if (t < range.t1) {
         load_codes(t, id_k0);
         load_centroids();
-        load_codes(t + kFewWaves, id_k1);
+        load_codes(t + WAVES, id_k1);
     }
     while (t < range.t1) {
         // values of this tile
@@ -729,10 +729,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
                 }
             }
         // centroids of the next tile, codes of the one behind it, page ids of the third
-        const int id_kn = load_id(t + 3 * kFewWaves, my_octet), id_vn = load_id(t + 2 * kFewWaves, quad);
-        if (t + kFewWaves < range.t1) {
+        const int id_kn = load_id(t + 3 * WAVES, my_octet), id_vn = load_id(t + 2 * WAVES, quad);
+        if (t + WAVES < range.t1) {
             load_centroids();
-            load_codes(t + 2 * kFewWaves, id_k2);
+            load_codes(t + 2 * WAVES, id_k2);
         }
         if (edge) {
             const int have = id_v < 0 ? 0 : range.end - t * kFewKeys - 8 * quad;
@@ -800,7 +800,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
                 acc[j][c][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x1, __builtin_bit_cast(v8h, lo[j]), acc[j][c][1], 0, 0, 0);
             }
         }
-        t += kFewWaves;
+        t += WAVES;
         id_k0 = id_k1;
         id_k1 = id_k2;
         id_k2 = id_kn;
@@ -810,7 +810,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
 
     // The wavefronts' results, 16 rows at a time: references and sums first, so that every wavefront brings its own to the common reference.
     float *results = reinterpret_cast<float *>(few_s);
-    float2 *stats = reinterpret_cast<float2 *>(few_s + (size_t)kFewWaves * 16 * ROW * 4);
+    float2 *stats = reinterpret_cast<float2 *>(few_s + (size_t)WAVES * 16 * ROW * 4);
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
         float u, w;
@@ -821,7 +821,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
         __syncthreads();
         float top = kNoReference;
 #pragma unroll
-        for (int k = 0; k < kFewWaves; ++k)
+        for (int k = 0; k < WAVES; ++k)
             top = fmaxf(top, stats[k * 16 + col].x);
         const float f = fast_exp2(ref[j] - top);
         // register i of acc[c][x] is coordinate 32 c + 2 (4 quad + i) + x
@@ -832,18 +832,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_few_kernel(PoolArgs p, C
                 *reinterpret_cast<v4f *>(results + (wave * 16 + col) * ROW + 32 * c + 8 * quad + 2 * i) =
                     (v4f){acc[j][c][0][i] * f, acc[j][c][1][i] * f, acc[j][c][0][i + 1] * f, acc[j][c][1][i + 1] * f};
         __syncthreads();
-        for (int x = tid; x < 16 * (DK / 4); x += kFewThreads) {
+        for (int x = tid; x < 16 * (DK / 4); x += WAVES * kWave) {
             const int k = x / (DK / 4), d = x % (DK / 4) * 4;
             const int r = r0 + 16 * j + k, n = r / a.group, hq = h * a.group + r - n * a.group;
             if (n >= span.count)
                 continue;
             float best = kNoReference, sum = 0.f;
 #pragma unroll
-            for (int y = 0; y < kFewWaves; ++y)
+            for (int y = 0; y < WAVES; ++y)
                 best = fmaxf(best, stats[y * 16 + k].x);
             v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int y = 0; y < kFewWaves; ++y) {
+            for (int y = 0; y < WAVES; ++y) {
                 const float2 st = stats[y * 16 + k];
                 sum = fmaf(fast_exp2(st.x - best), st.y, sum);
                 o += *reinterpret_cast<const v4f *>(results + (y * 16 + k) * ROW + d);
@@ -905,7 +905,9 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
     const bool few = rows <= 32 || (longest > 256 && (rows <= 64 || (rows <= 128 && units <= 64)));
     c.few = !few ? 0 : rows <= 16 ? 1 : 2;
-    c.waves = c.few ? kFewWaves : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
+    // Two wavefronts instead of eight where many heads have little to see: 1125 x 16 rows x 8 tokens 23 / 41 us, 2048 x 8 x 208 51 / 74, but 192 x 8 x 208
+    // 12.1 / 10.4.
+    c.waves = c.few ? (longest > 256 || units < 512 ? kFewWaves : kBriefWaves) : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
     c.splits = num_splits;
@@ -955,26 +957,28 @@ static int launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp
     hipLaunchKernelGGL(f, dim3(groups), dim3(NW * kWave), 0, st, p, a);
     return check_launch("lookat_attend_pages_chunk");
 }
-template <int DK, bool SMALL, int RB>
+template <int DK, bool SMALL, int RB, int WAVES>
 static int launch_few(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
-    const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, RB> : &chunk_few_kernel<DK, SMALL, true, false, RB>)
-                       : (fp8 ? &chunk_few_kernel<DK, SMALL, false, true, RB> : &chunk_few_kernel<DK, SMALL, false, false, RB>);
-    constexpr size_t lds = few_lds_bytes(DK);
+    const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, true, false, RB, WAVES>)
+                       : (fp8 ? &chunk_few_kernel<DK, SMALL, false, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, false, false, RB, WAVES>);
+    constexpr size_t lds = few_lds_bytes(DK, WAVES);
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
             return fail(LOOKAT_ERR_HIP, "lookat_attend_pages_chunk: %s", hipGetErrorString(e));
     }
-    hipLaunchKernelGGL(f, dim3(groups), dim3(kFewThreads), lds, st, p, a);
+    hipLaunchKernelGGL(f, dim3(groups), dim3(WAVES * kWave), lds, st, p, a);
     return check_launch("lookat_attend_pages_chunk");
 }
 template <int DK, bool SMALL>
 static int launch_rows(const ChunkCut &c, const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
     switch (c.few) {
-    case 1: return launch_few<DK, SMALL, 1>(p, a, q32, fp8, groups, st);
-    case 2: return launch_few<DK, SMALL, 2>(p, a, q32, fp8, groups, st);
+    case 1: return c.waves == kFewWaves ? launch_few<DK, SMALL, 1, kFewWaves>(p, a, q32, fp8, groups, st)
+                                        : launch_few<DK, SMALL, 1, kBriefWaves>(p, a, q32, fp8, groups, st);
+    case 2: return c.waves == kFewWaves ? launch_few<DK, SMALL, 2, kFewWaves>(p, a, q32, fp8, groups, st)
+                                        : launch_few<DK, SMALL, 2, kBriefWaves>(p, a, q32, fp8, groups, st);
     default:
         if constexpr (DK == 128)
             if (c.waves == 8)

@@ -228,3 +228,57 @@ def test_one_row_is_attention_of_one_token(lk):  # noqa: F811
     one = lk.lookat_attend_pages(lut, on_gpu(lk, c), dev(table), i32(*lengths), 0.125).cpu().numpy()
     _, bound = reference(c, q, books, table, lengths, None, 0.125, np.zeros(q.shape))
     assert np.all(np.abs(got[:, :, 0] - one) <= 2 * bound[:, :, 0])
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page", [
+    (8, 32, 1, 260, 150, 128, 8, 32),     # 256 rows to a workgroup
+    (3, 90, 2, 140, 0, 128, 16, 128),     # ... with two rows to a token, prompts
+    (6, 2, 4, 100, 900, 128, 2, 64),      # 128 rows to a workgroup
+    (5, 20, 3, 70, 333, 64, 16, 16),
+    (40, 16, 4, 4, 60, 64, 4, 64),        # few rows of many heads that see little: two wavefronts
+    (40, 16, 5, 6, 100, 128, 4, 128),
+    (2, 3, 8, 16, 5000, 64, 8, 64),       # few rows in ranges: 128 of few heads
+    (1, 1, 4, 8, 9000, 128, 8, 128)])
+def test_every_kernel(lk, B, H, g, N, before, d_k, m, page, dtype, kind):  # noqa: F811
+    """The kernels that large and small launches take, against torch in 64 bits.  The bound is that of `reference`, with the row's own sizes."""
+    gen = torch.Generator(device="cuda").manual_seed(B + N)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    lengths = [N + before - 3 * b for b in range(B)]
+    counts = [max(1, N - 2 * b) for b in range(B)]
+    W = -(-max(lengths) // page)
+    P = B * W
+    v = rnd(P, H, page // 8, d_k, 8) * 30
+    v = v.round().clamp(-127, 127).to(torch.int8) if kind == "int8" else v.to(torch.float8_e4m3fn)
+    pool = lk.PagePool(torch.randint(0, 256, (P, H, page, m), generator=gen, device="cuda", dtype=torch.uint8), v,
+                       torch.randint(-8, -2, (P, H), generator=gen, device="cuda").to(torch.int8))
+    table = torch.randperm(P, generator=gen, device="cuda").to(torch.int32).view(B, W)
+    books = rnd(H, m, 256, d_k // m)
+    q = rnd(B, N, H * g, d_k).to(getattr(torch, dtype)).transpose(1, 2)
+    scale = 1 / math.sqrt(d_k)
+    got = lk.lookat_attend_pages_chunk(q, books, pool, table, i32(*lengths), scale, counts=i32(*counts))
+    head, sub = torch.arange(H, device="cuda")[:, None, None], torch.arange(m, device="cuda")
+    for b in range(B):
+        n, k, ids = lengths[b], counts[b], table[b].long()
+        code = pool.codes[ids].permute(1, 0, 2, 3).reshape(H, -1, m)[:, :n].long()
+        key = books.double()[head, sub, code].reshape(H, n, d_k)
+        val = pool.values[ids].double() * torch.exp2(pool.exponents[ids].double())[..., None, None, None]
+        val = val.permute(1, 0, 2, 4, 3).reshape(H, -1, d_k)[:, :n]
+        x = q[b, :, :k].double().reshape(H, g * k, d_k)
+        y = torch.matmul(x, key.transpose(1, 2).contiguous()).view(H, g, k, n) * scale
+        size = torch.matmul(x.abs(), key.abs().transpose(1, 2).contiguous()).amax(-1).view(H, g, k, 1) * scale * 1.4427
+        seen = torch.arange(n, device="cuda") <= n - k + torch.arange(k, device="cuda")[:, None]
+        p = torch.softmax(y.masked_fill(~seen, -math.inf), -1)
+        p = torch.where(seen.any(-1, keepdim=True), p, 0.0)       # (rows ahead of the first token: zeros)
+        want = torch.matmul(p.view(H, g * k, n), val).view(H * g, k, d_k)
+        d = (3 * 2.0 ** -22 + (d_k + 3) * U) * size + 6 * U * (size + 64) \
+            + d_k * 2.0 ** -38 * x.abs().amax(-1).view(H, g, k, 1) * books.abs().amax().double() * scale * 1.4427
+        rel = 2 * (d * 0.6932 + 2.0 ** -21) + 4 * math.sqrt(n + 64) * U
+        # (the last term of `reference`, with every exponent at its largest)
+        floor = 1.01 * 2.0 ** (-3 - 32) * pool.values[ids].double().abs().amax() * n
+        bound = (rel * torch.matmul(p.view(H, g * k, n), val.abs()).view(H, g, k, d_k)).reshape(H * g, k, d_k) + floor
+        off = (got[b, :, :k].double() - want).abs()
+        record("chunk attention, every kernel", float(off.max()))
+        assert bool((off <= bound).all()), (b, float((off - bound).max()))
+        assert not got[b, :, k:].any()
