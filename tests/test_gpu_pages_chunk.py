@@ -245,7 +245,7 @@ def test_every_kernel(lk, B, H, g, N, before, d_k, m, page, dtype, kind):  # noq
     """The kernels that large and small launches take, against torch in 64 bits.  The bound is that of `reference`, with the row's own sizes."""
     gen = torch.Generator(device="cuda").manual_seed(B + N)
     rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
-    lengths = [N + before - 3 * b for b in range(B)]
+    lengths = [max(1, N + before - 3 * b) for b in range(B)]
     counts = [max(1, N - 2 * b) for b in range(B)]
     W = -(-max(lengths) // page)
     P = B * W
