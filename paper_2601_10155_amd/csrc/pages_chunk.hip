@@ -42,7 +42,7 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 __device__ __forceinline__ int lift_of(uint32_t bits)
 {
     const int s = bits ? kBookTop + 127 - (int)(bits >> 23) : 0;
-    return s > 100 ? 100 : s < -100 ? -100 : s;
+    return s > 126 ? 126 : s < -126 ? -126 : s;
 }
 
 constexpr int kBookThreads = 512, kBookParts = 8;

@@ -697,7 +697,7 @@ static WeighCut weigh_cut(const lookat_page_pool *p, int32_t B, int32_t G, int32
     want = want < useful ? want : useful;
     int64_t chunk = (longest + want - 1) / want;
     chunk = (chunk + kWeighThreads - 1) / kWeighThreads * kWeighThreads;
-    chunk = chunk < most ? chunk : most;
+    chunk = chunk < most && room <= 1024 * chunk ? chunk : most;      // (rows with far more room than the caller knows of tokens: few workgroups)
     WeighCut c;
     c.chunk = (int)chunk;
     c.splits = (int)((room + chunk - 1) / chunk);

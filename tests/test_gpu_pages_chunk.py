@@ -173,6 +173,21 @@ def test_scores_that_are_not_finite(lk):  # noqa: F811
     assert np.all(np.abs(got - want) <= bound)
 
 
+@pytest.mark.parametrize("q_size,book_size,scale", [(1e-6, 1.0, 1e5), (1.0, 1e-30, 1e29), (1e30, 1e-28, 0.01), (1e37, 1e-37, 0.3), (1e-37, 1e36, 1.0), (2.0, 1.0, -0.2),
+                                                    (1.0, 1.0, 0.0)])
+def test_sizes_and_scales(lk, q_size, book_size, scale):  # noqa: F811
+    """Queries and centroids near both ends of their types, a scale below zero and one of zero."""
+    rng = np.random.default_rng(13)
+    for dtype in ("float16", "float32"):
+        if dtype == "float16" and not 1e-7 < q_size < 1e4:
+            continue
+        for N, before in ((6, 90), (140, 0)):
+            c = random_cache(rng, 20, 2, 64, 4, 16, "int8")
+            table = random_table(rng, [N + before, N], 16, 10, 20)
+            q = (rng.standard_normal((2, 2, N, 64)) * q_size).astype(dtype)
+            check(lk, c, q, books_of(rng, 2, 4, 64, book_size), table, [N + before, N], None, scale)
+
+
 def test_strides_offsets_and_graphs(lk):  # noqa: F811
     """Queries inside a larger projection, tables with room behind the rows, another stream, a captured call replayed on new inputs."""
     rng = np.random.default_rng(11)
