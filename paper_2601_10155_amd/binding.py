@@ -866,13 +866,21 @@ def lookat_attend_pages_chunk(q: torch.Tensor, codebooks: torch.Tensor, pool: Pa
         raise ValueError("out must live on the pool's device")
     if not N or not B:
         return out
+    num_splits = _int32(num_splits, "num_splits")
     with _OnDevice(pool) as stream:
         need = lib.lookat_attend_pages_chunk_workspace_bytes(ctypes.byref(c_pool), B, N, Hq // H, W, max_length, num_splits)
         workspace = _scratch(workspace, need, pool)
         _check(lib.lookat_attend_pages_chunk(ctypes.byref(c_pool), B, N, Hq // H, q.data_ptr(), tag, sb, sh, sn, codebooks.data_ptr(), t_ptr, W, stride,
-                                             l_ptr, n_ptr, int(max_length), float(scale), int(num_splits), _ptr(workspace), _bytes(workspace),
+                                             l_ptr, n_ptr, int(max_length), float(scale), num_splits, _ptr(workspace), _bytes(workspace),
                                              out.data_ptr(), stream))
     return out
+
+
+def _int32(x: int, name: str) -> int:
+    """(ctypes would cut a larger number to its low bits.)"""
+    if not -2 ** 31 <= int(x) < 2 ** 31:
+        raise ValueError(f"{name} = {x} is out of range")
+    return int(x)
 
 
 def _weight_rows(t: torch.Tensor, name: str, pool: PagePool, B: int, H: int) -> tuple[int, int, int]:
@@ -948,7 +956,8 @@ def lookat_pages_evict(pool: PagePool, table: torch.Tensor, lengths: torch.Tenso
     out = (0, 0, None) if weights_out is None else _weight_rows(weights_out, "weights_out", pool, B, c_pool.H)
     with _OnDevice(pool) as stream:
         workspace = _scratch(workspace, lib.lookat_pages_evict_workspace_bytes(ctypes.byref(c_pool), B, W_out), pool)
-        _check(lib.lookat_pages_evict(ctypes.byref(c_pool), B, t_ptr, W, stride, l_ptr, w_ptr, columns, w_stride, k_ptr, int(first), int(recent),
+        _check(lib.lookat_pages_evict(ctypes.byref(c_pool), B, t_ptr, W, stride, l_ptr, w_ptr, columns, w_stride, k_ptr, _int32(first, "first"),
+                                      _int32(recent, "recent"),
                                       o_ptr, W_out, out_stride, out[2], out[0], out[1], _ptr(workspace), _bytes(workspace), stream))
 
 
@@ -1084,6 +1093,7 @@ def lookat_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, n
         if rc:
             _check(rc)
     lib = load_library()
+    beams, n, first_parent = _int32(beams, "beams"), _int32(n, "n"), _int32(first_parent, "first_parent")
     device = _dev(logits, "logits").device
     if logits.dim() != 2 or beams < 1 or n < 1 or not logits.shape[0] or logits.shape[0] % beams or not logits.shape[1]:
         raise ValueError("logits must be [Q*beams,V]")
@@ -1106,7 +1116,7 @@ def lookat_beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, n
         need = lib.lookat_beam_select_workspace_bytes(Q, beams, V, n)
         if need and (workspace is None or _bytes(workspace) < need):
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        _check(lib.lookat_beam_select(Q, beams, V, n, logits.data_ptr(), tag, logits.stride(0) if R > 1 else V, scores.data_ptr(), int(first_parent),
+        _check(lib.lookat_beam_select(Q, beams, V, n, logits.data_ptr(), tag, logits.stride(0) if R > 1 else V, scores.data_ptr(), first_parent,
                                       scores_out.data_ptr(), parents.data_ptr(), tokens.data_ptr(), _ptr(workspace), _bytes(workspace),
                                       torch._C._cuda_getCurrentRawStream(device.index)))
     return scores_out, parents, tokens

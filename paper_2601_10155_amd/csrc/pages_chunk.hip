@@ -131,7 +131,7 @@ __device__ __forceinline__ KeyRange key_range(const ChunkSpan &s, int last_row, 
 // Which work a workgroup has.  Units (sequence, head) are dealt to the dies in turn, all workgroups of a unit on one die (they read the same keys,
 // values and centroids); the units that eight dies do not divide are dealt by workgroups.  The last rows come first: they see most.  A die's
 // workgroups go round its 32 compute units, and every second round turns back, so that no compute unit gets the longest of each (prompts of 400 to
-// 1000 rows, all workgroups in flight at once: unit by unit 60.7 us, so 57.9.
+// 1000 rows, all workgroups in flight at once: unit by unit 60.7 us, so 57.9).
 struct Place {
     int unit, tile, split;
     bool any;

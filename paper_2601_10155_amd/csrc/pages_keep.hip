@@ -744,7 +744,8 @@ static int launch_weigh_phases(const PoolArgs &p, const WeighArgs &a, int64_t gr
         return rc;
     return launch_weigh_phase<M, G, kWeighAdd, T>(p, a, groups, st);
 }
-// Few scores a thread where that is enough: short code ({WSHORT}).
+// Few scores a thread where that is enough: short code (us a call with it / with the long code: 12 heads x 1024 tokens 4.2 / 8.1, 16 x 8 x 1000 in groups of
+// 4 7.0 / 9.7).
 template <int M, int G>
 static int launch_weigh(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
 {
@@ -908,7 +909,8 @@ extern "C" int lookat_pages_evict(const lookat_page_pool *pool, int32_t B, const
     a.first = first;
     a.recent = recent;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // (by the room of a row; a variant for few tokens is short code: {PICK})
+    // By the room of a row: a variant for few tokens is short code, and weights that stay in registers are read once (us a call of 48 heads x 1024 tokens
+    // to half, kept by 2 / by 32 / read again 15.6 / 23.9 / 16.5, x 8000 24.3 / 30.6 / 34.4 (by 8 first), 128 x 20000 - / 134 / 159).
     const int64_t each = ((int64_t)W * pool->page + kPickThreads - 1) / kPickThreads;
     const auto pick = each <= 2    ? &evict_pick_kernel<2>
                       : each <= 8  ? &evict_pick_kernel<8>

@@ -191,3 +191,16 @@ def test_calls_that_are_left_or_refused(lk, both):  # noqa: F811
                       ({"scores": s["scores"].cpu()}, ValueError), ({"first_parent": -1}, lk.LookatError)):
         with pytest.raises(error):
             select(**kw)
+
+
+def test_numbers_beyond_32_bits_are_refused(lk):  # noqa: F811
+    s = serving_case(lk, torch.float16)
+    for big in (2 ** 32, 2 ** 32 + 1, -2 ** 32):
+        with pytest.raises(ValueError, match="num_splits"):
+            lk.lookat_attend_pages_chunk(s["q"], s["books"], s["pool"], s["table"], s["lengths"], 0.1, num_splits=big)
+        for name in ("first", "recent"):
+            with pytest.raises(ValueError, match=name):
+                lk.lookat_pages_evict(s["pool"], s["table"], s["lengths"], s["weights"], s["keep"], s["out"], **{name: big})
+        for name in ("n", "beams", "first_parent"):
+            with pytest.raises(ValueError, match=name):
+                lk.lookat_beam_select(s["logits"], s["scores"], **{"beams": 3, "n": 5, name: big})
