@@ -217,11 +217,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     wave_fence();
     const uint64_t key = lane < found ? lists[wave][lane] : 0;
     int rank = 0;
-    for (int j = 0; j < found; ++j) {
-        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 |
-                               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, j);
-        rank += other > key;
-    }
+    // (out of LDS, the same address for all lanes: read across lanes instead 62.5 us for 64 x 8 x 131072, n = 16, so 59.9)
+    for (int j = 0; j < found; ++j)
+        rank += lists[wave][j] > key;
     const float logit = unordered((uint32_t)(key >> 32));
     const bool listed = lane < found && rank < a.n;
     // listed logits near the maximum in 64 bits, the others of them as the rest
