@@ -3,8 +3,8 @@
 // Two launches.  In the first a wavefront takes 64 E consecutive logits of a row, E to a lane, in registers: their maximum m, their n best in order, and
 // the sum of exp(x - m).  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots); few logits reach
 // it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n) the n-th best itself is found bit by bit
-// among them, first its value, then among equal ones its place; where more than kListed do (many equal logits), among all.  Listed logits near m enter the sum in 64 bits, so that the terms that
-// dominate a row's sum carry no fp32 rounding; the others' roundings average out.
+// among them, first its value, then among equal ones its place; where more than kListed do (many equal logits), among all.  Listed logits near m
+// enter the sum in 64 bits, so that the terms that dominate a row's sum carry no fp32 rounding; the others' roundings average out.
 // In the second launch a workgroup takes a request.  A lower bound on the n-th best score, found as above from a few entries of every sorted list,
 // leaves few candidates, whose places are counted.  Where more than kMostFound reach the bound (many equal scores) each wavefront takes the n best of its
 // share of the lists one by one, and those are merged by counting.
@@ -164,6 +164,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
                 if (j * kWave < found)
                     c += ballot_count(keys[j] >= t);
             nth = c >= a.n ? t : nth;
+            if (c == a.n)                 // (these are the n greatest: us a call for 16 x 4 x 50257, n = 64, all digits 43, so 26)
+                break;
         }
         wave_fence();
         int kept = 0;
@@ -272,25 +274,50 @@ __global__ __launch_bounds__(kMergeThreads) void select_merge_kernel(SelectArgs 
     __shared__ int found_s;
     const int q = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = a.n, parts = a.parts;
     const int64_t row0 = (int64_t)q * a.beams;
-    for (int r = wave; r < a.beams; r += kMergeWaves) {
-        const PartSum *stats = a.stats + (row0 + r) * parts;
-        float m = -INFINITY;
-        for (int j = lane; j < parts; j += kWave)
-            m = fmaxf(m, stats[j].top);
-        m = wave_max(m);
-        double sum = 0;
-        for (int j = lane; j < parts; j += kWave) {
-            const PartSum s = stats[j];
+    // The rows' sums, 64 or 16 lanes a row, each with up to kHeld parts in registers (a wavefront a row whatever their number: us a call for 4 x 16 x 1000
+    // 22.7, so 14.6).
+    auto sum_up = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value, kHeld = 128 / L;
+        const int within = lane & (L - 1);
+        for (int r = (wave * kWave + lane) / L; r < a.beams; r += kMergeThreads / L) {
+            const PartSum *stats = a.stats + (row0 + r) * parts;
+            const float score = a.scores[row0 + r];
+            const PartSum nothing = {0, -INFINITY, 0.f};
+            PartSum held[kHeld];
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k)
+                held[k] = k * L + within < parts ? stats[k * L + within] : nothing;
+            float m = held[0].top;
+#pragma unroll
+            for (int k = 1; k < kHeld; ++k)
+                m = fmaxf(m, held[k].top);
+            for (int j = kHeld * L + within; j < parts; j += L)
+                m = fmaxf(m, stats[j].top);
+#pragma unroll
+            for (int d = 1; d < L; d *= 2)
+                m = fmaxf(m, __shfl_xor(m, d));
             // (a part of -inf alone has a sum of zero, or NaN)
-            sum += s.sum * (s.top == -INFINITY ? 1.0 : exp((double)s.top - (double)m));
+            auto scaled = [&](const PartSum &s) -> double { return s.sum * (s.top == -INFINITY ? 1.0 : exp((double)s.top - (double)m)); };
+            double sum = scaled(held[0]);
+#pragma unroll
+            for (int k = 1; k < kHeld; ++k)
+                if (k * L < parts)
+                    sum += scaled(held[k]);
+            for (int j = kHeld * L + within; j < parts; j += L)
+                sum += scaled(stats[j]);
+#pragma unroll
+            for (int d = 1; d < L; d *= 2)
+                sum += __shfl_xor(sum, d);
+            // -inf: no candidates (a sum that is NaN or infinite, a score that is not finite)
+            const bool none = !(fabsf(m) < INFINITY) || !(sum < (double)INFINITY) || !(fabsf(score) < INFINITY);
+            if (within == 0)
+                bases[r] = none ? -(double)INFINITY : (double)score - ((double)m + log(sum));
         }
-        sum = wave_sum_double(sum);
-        const float score = a.scores[row0 + r];
-        // -inf: no candidates (a sum that is NaN or infinite, a score that is not finite)
-        const bool none = !(fabsf(m) < INFINITY) || !(sum < (double)INFINITY) || !(fabsf(score) < INFINITY);
-        if (lane == 0)
-            bases[r] = none ? -(double)INFINITY : (double)score - ((double)m + log(sum));
-    }
+    };
+    if (a.beams <= kMergeWaves)
+        sum_up(std::integral_constant<int, kWave>());
+    else
+        sum_up(std::integral_constant<int, 16>());
     __syncthreads();
 
     const int lists = a.beams * parts, step = kMergeThreads;
@@ -382,16 +409,26 @@ __global__ __launch_bounds__(kMergeThreads) void select_merge_kernel(SelectArgs 
 #pragma unroll
     for (int w = 0; w < kMergeWaves; ++w)
         order[w] = tops[w * kWave + lane];
-#pragma unroll
-    for (int bit = 31; bit >= 0; --bit) {
+    int reached = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0 && reached != n; --bit) {
         const uint32_t t = bound | 1u << bit;
         int c = 0;
 #pragma unroll
         for (int w = 0; w < kMergeWaves; ++w)
             c += ballot_count(order[w] >= t);
         bound = c >= n ? t : bound;
+        reached = c >= n ? c : reached;
     }
-    const float border = fmaxf(unordered(bound), kLowest);
+    float border = unordered(bound);
+    if (reached == n) {
+        border = INFINITY;
+#pragma unroll
+        for (int w = 0; w < kMergeWaves; ++w)
+            border = order[w] >= bound ? fminf(border, unordered(order[w])) : border;
+        border = -wave_max(-border);
+    }
+    border = fmaxf(border, kLowest);
     for (int list0 = threadIdx.x; list0 < lists; list0 += kBatch * step) {
         float heads[kBatch];
 #pragma unroll
@@ -433,9 +470,19 @@ __global__ __launch_bounds__(kMergeThreads) void select_merge_kernel(SelectArgs 
         const Pick c = picks[i];
         if (!(c.score > -(double)INFINITY))
             continue;
-        int rank = 0;
-        for (int j = 0; j < found; ++j)
-            rank += ahead(picks[j], c);
+        // (scores first: who is ahead of whom among equal ones is looked at only where there are any)
+        int rank = 0, equal = 0;
+#pragma unroll 4
+        for (int j = 0; j < found; ++j) {
+            const double other = picks[j].score;
+            rank += other > c.score;
+            equal += other == c.score;
+        }
+        if (equal > 1) {                  // (not with itself alone)
+            rank = 0;
+            for (int j = 0; j < found; ++j)
+                rank += ahead(picks[j], c);
+        }
         if (rank < n) {
             a.scores_out[(int64_t)q * n + rank] = rounded(c.score);
             a.parents[(int64_t)q * n + rank] = a.first_parent + (int)row0 + c.row;
@@ -463,8 +510,10 @@ static SelectCut select_cut(int32_t Q, int32_t beams, int32_t V, int32_t n)
     SelectCut c;
     const int64_t rows = (int64_t)Q * beams;
     // Logits of a lane: 32, or 16 where there would be few wavefronts.  us of the launch, 8 / 16 / 32 / 64: 4 x 50257 fp32 4.7 / 5.0 / 6.0 / - (and 10.0
-    // / 8.3 / 7.9 / - of the merge), 128 x 32001 fp16 9.5 / 7.7 / 9.0 / -, 512 x 131072 fp32 (a call) 133 / 80.9 / 63.5 / 79.8.
-    c.each = rows * V < (16LL << 20) ? 16 : 32;
+    // / 8.3 / 7.9 / - of the merge), 128 x 32001 fp16 9.5 / 7.7 / 9.0 / -, 512 x 131072 fp32 (a call) 133 / 80.9 / 63.5 / 79.8.  And 32 where a request
+    // would have more than 512 lists to merge: us a call, 16 / 32, 1 x 16 x 262144 (4096 lists) 30.7 / 22.2, 8 x 8 x 131072 (1024) 20.3 / 18.8,
+    // but 16 x 4 x 50257, n = 64 (200) 25.9 / 34.8.
+    c.each = rows * V < (16LL << 20) && beams * ((V + 1023) / 1024) <= 512 ? 16 : 32;
     const int64_t per = (int64_t)kWave * c.each;
     c.parts = (int)((V + per - 1) / per);
     c.stats = ((size_t)rows * c.parts * sizeof(PartSum) + 15) / 16 * 16;

@@ -106,6 +106,19 @@ def test_masks_and_values_that_are_not_finite(lk):
     check(lk, half, scores, 2, n)
 
 
+@pytest.mark.parametrize("Q,beams,V,n", [(1, 2, 200001, 5), (1, 5, 300000, 9), (2, 17, 3000, 30), (1, 1024, 1025, 12), (3, 6, 1024, 63)])
+def test_many_parts_and_many_beams(lk, Q, beams, V, n):
+    """More parts of a row than its lanes hold, rows that do not fill the last wavefront; a row without tokens and one of NaN among them."""
+    rng = np.random.default_rng(V)
+    logits = (3 * rng.standard_normal((Q * beams, V))).astype(np.float32)
+    scores = (-4 * rng.random(Q * beams)).astype(np.float32)
+    if beams > 2:
+        logits[1] = -math.inf
+        logits[Q * beams - 1, V - 1] = math.nan
+        logits[2, : V - 3] = -math.inf
+    check(lk, logits, scores, beams, n)
+
+
 def test_peaked_and_flat_rows(lk):
     """Sums that one logit makes, sums that all make, logits and scores of large size."""
     rng = np.random.default_rng(3)
