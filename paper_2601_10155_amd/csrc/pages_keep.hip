@@ -1,4 +1,6 @@
 // Holding a cache to a budget: every token's sum of the attention it was paid, and moving the heaviest tokens into fewer pages.
+#include <type_traits>
+
 #include "pages_quantise.h"
 #include "decode_common.h"
 
@@ -7,8 +9,8 @@ namespace lookat {
 // ---- attention sums ---------------------------------------------------------------------------------------------
 //   w_l = decay w_l + sum_g 2^(y_gl - M_g) / Z_g,   y_gl = scale log2(e) sum_i lut_gi[code_li],   M_g = max_l y_gl,  Z_g = sum_l 2^(y_gl - M_g)
 //
-// A workgroup of 1024 threads takes a range of one (sequence, key/value head): its scores stay in registers (kWeighScores a thread, over the
-// group's query heads) from the maximum to the weights, so that codes are read and looked up once.  Where one range does not hold a sequence or
+// A workgroup of 1024 or 256 threads takes a range of one (sequence, key/value head): its scores stay in registers (kWeighScores a thread, over
+// the group's query heads) from the maximum to the weights, so that codes are read and looked up once.  Where one range does not hold a sequence or
 // there are few of them, sequences are cut: a first launch brings the ranges' maxima and sums, a second one scores again and adds.
 struct WeighArgs {
     const float *lut;
@@ -20,18 +22,20 @@ struct WeighArgs {
     float scale_log2e, decay;
 };
 
-constexpr int kWeighThreads = 1024, kWeighWaves = kWeighThreads / kWave, kWeighScores = 32, kWeighFew = 4;
-__host__ __device__ constexpr int weigh_tokens(int G) { return kWeighThreads * (kWeighScores / G); }     // of a range, at most
+constexpr int kWeighThreads = 1024, kWeighSmall = 256, kWeighScores = 32, kWeighFew = 4;
+__host__ __device__ constexpr int weigh_tokens(int G, int threads) { return threads * (kWeighScores / G); }     // of a range, at most
+__host__ __device__ constexpr int weigh_few(int G) { return kWeighFew / G > 0 ? kWeighFew / G : 1; }                          // scores of a thread in the short code
 
 enum WeighPhase { kWeighAll, kWeighStats, kWeighAdd };
 
-template <int M, int G, int PHASE, int T>
-__global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighArgs a)
+template <int M, int G, int PHASE, int T, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void weigh_kernel(PoolArgs p, WeighArgs a)
 {
+    constexpr int WAVES = THREADS / kWave;
     constexpr int GP = G < 4 ? G : 4, PLANES = G / GP;
     typedef float vg __attribute__((ext_vector_type(GP)));
     extern __shared__ __align__(16) float tables[];       // [plane][i][c][head of the plane]
-    __shared__ float red[2][G][kWeighWaves];
+    __shared__ float red[2][G][WAVES];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int unit = (int)(blockIdx.x / kXcds) / a.splits * kXcds + (int)(blockIdx.x % kXcds), split = (int)(blockIdx.x / kXcds) % a.splits;
     if (unit >= a.units)
@@ -56,12 +60,12 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         int id[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int key = k0 + (t0 + u) * kWeighThreads + tid;
+            const int key = k0 + (t0 + u) * THREADS + tid;
             id[u] = row[(key < k1 ? key : k1 - 1) >> p.page_log2];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int key = k0 + (t0 + u) * kWeighThreads + tid;
+            const int key = k0 + (t0 + u) * THREADS + tid;
             there[t0 / U & 1][u] = key < k1 && (uint32_t)id[u] < (uint32_t)p.pages;
             const uint8_t *c = head_codes + (uint64_t)(uint32_t)(there[t0 / U & 1][u] ? id[u] : 0) * code_step + (uint32_t)(key & page_mask) * M;
             if constexpr (M == 2) {
@@ -80,7 +84,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
     request(0);
     {
         const v4f *lut = reinterpret_cast<const v4f *>(a.lut + (int64_t)unit * G * M * kCentroids);
-        for (int j = tid; j < PLANES * M * (kCentroids / 4); j += kWeighThreads) {
+        for (int j = tid; j < PLANES * M * (kCentroids / 4); j += THREADS) {
             const int plane = j / (M * (kCentroids / 4)), entry = j % (M * (kCentroids / 4));
             v4f x[GP];
 #pragma unroll
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
     if constexpr (PHASE != kWeighStats) {
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const int key = k0 + t * kWeighThreads + tid;
+            const int key = k0 + t * THREADS + tid;
             old[t] = a.decay != 0.f && key < k1 && key < a.columns ? weights[key] : 0.f;
         }
     }
@@ -113,7 +117,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         top[g] = -INFINITY;
 #pragma unroll
     for (int t0 = 0; t0 < T; t0 += U) {
-        if (k0 + t0 * kWeighThreads >= k1) {
+        if (k0 + t0 * THREADS >= k1) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -121,7 +125,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
                     y[t0 + u][g] = -INFINITY;
             continue;
         }
-        if (t0 + U < T && k0 + (t0 + U) * kWeighThreads < k1)
+        if (t0 + U < T && k0 + (t0 + U) * THREADS < k1)
             request(t0 + U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -159,13 +163,13 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            top[g] = wave_max(red[0][g][lane & (kWeighWaves - 1)]);
+            top[g] = wave_max(red[0][g][lane & (WAVES - 1)]);
             top[g] = top[g] == -INFINITY ? 0.f : top[g];
             sum[g] = 0.f;
         }
 #pragma unroll
         for (int t = 0; t < T; ++t)
-            if (k0 + t * kWeighThreads < k1)
+            if (k0 + t * THREADS < k1)
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     y[t][g] = fast_exp2(y[t][g] - top[g]);
@@ -180,7 +184,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            sum[g] = wave_sum(lane < kWeighWaves ? red[1][g][lane] : 0.f);
+            sum[g] = wave_sum(lane < WAVES ? red[1][g][lane] : 0.f);
         }
         if constexpr (PHASE == kWeighStats) {
             if (tid < G) {
@@ -214,7 +218,7 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         }
 #pragma unroll
         for (int t = 0; t < T; ++t)
-            if (k0 + t * kWeighThreads < k1)
+            if (k0 + t * THREADS < k1)
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     y[t][g] = fast_exp2(y[t][g] - top[g]);
@@ -224,8 +228,8 @@ __global__ __launch_bounds__(kWeighThreads) void weigh_kernel(PoolArgs p, WeighA
         sum[g] = sum[g] == 0.f ? 0.f : 1.f / sum[g];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-        const int key = k0 + t * kWeighThreads + tid;
-        if (k0 + t * kWeighThreads < k1 && key < k1 && key < a.columns) {
+        const int key = k0 + t * THREADS + tid;
+        if (k0 + t * THREADS < k1 && key < k1 && key < a.columns) {
             float w = y[t][0] * sum[0];
 #pragma unroll
             for (int g = 1; g < G; ++g)
@@ -618,11 +622,21 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PoolArgs p, Ev
 #pragma unroll
                 for (int i = 0; i < kMoveAhead; ++i)
                     take(sources[octet * 8 + i], ahead[batch & 1][r][i]);
-#pragma unroll 1
-                for (int i = kMoveAhead; i < count; ++i) {
-                    const MoveSource s = sources[octet * 8 + i];
-                    take(s, *reinterpret_cast<const uint64_t *>(values + s.at + d * 8));
-                }
+                auto take_more = [&](auto upto) {
+                    constexpr int N = decltype(upto)::value;
+                    uint64_t more[N - kMoveAhead];
+#pragma unroll
+                    for (int i = kMoveAhead; i < N; ++i)
+                        more[i - kMoveAhead] = *reinterpret_cast<const uint64_t *>(values + sources[octet * 8 + i].at + d * 8);
+#pragma unroll
+                    for (int i = kMoveAhead; i < N; ++i)
+                        take(sources[octet * 8 + i], more[i - kMoveAhead]);
+                };
+                // (the others at once: few kept tokens come from as many octets)
+                if (count > kMoveAhead + 1)
+                    take_more(std::integral_constant<int, 8>());
+                else if (count > kMoveAhead)
+                    take_more(std::integral_constant<int, kMoveAhead + 1>());
                 if (!count)
                     continue;
                 const int e = __builtin_amdgcn_readfirstlane(octet_e[octet]);
@@ -685,20 +699,31 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PoolArgs p, Ev
 
 // ---- host -------------------------------------------------------------------------------------------------------
 struct WeighCut {
-    int splits, chunk;
+    int splits, chunk, threads;
 };
 static WeighCut weigh_cut(const lookat_page_pool *p, int32_t B, int32_t G, int32_t W, int64_t max_length)
 {
     const int64_t units = (int64_t)B * p->H, room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
+    WeighCut c;
+    // Small workgroups where there are more heads than large ones run at once, or where their short code holds a row (us a call of large / small ones:
+    // 40 x 32 heads x 90 to 900 tokens, m = 16, 16.2 / 11.0, 64 x 32 x 30 to 300 in groups of 2 21.1 / 10.4, 64 x 12 x 500 to 5000 32.0 / 15.3, 16 x 12 x 900
+    // 4.7 / 3.8, but 16 x 32 x 2000 6.4 / 8.1), while their tables leave room for 16 wavefronts of them.
+    const bool brief = units >= 96 && room <= weigh_few(G) * kWeighSmall;
+    if ((units > 512 || brief) && G * p->m <= 32 && room <= weigh_tokens(G, kWeighSmall)) {
+        c.threads = kWeighSmall;
+        c.chunk = (int)((room + kWeighSmall - 1) / kWeighSmall * kWeighSmall);
+        c.splits = 1;
+        return c;
+    }
+    c.threads = kWeighThreads;
     // Every token in reach has its range: the cut goes by the row's room where the caller's longest length does not hold.
-    const int64_t most = weigh_tokens(G);
+    const int64_t most = weigh_tokens(G, kWeighThreads);
     int64_t want = units >= 128 ? 1 : (256 + units - 1) / units;
     const int64_t useful = (longest + 2047) / 2048;
     want = want < useful ? want : useful;
     int64_t chunk = (longest + want - 1) / want;
     chunk = (chunk + kWeighThreads - 1) / kWeighThreads * kWeighThreads;
     chunk = chunk < most && room <= 1024 * chunk ? chunk : most;      // (rows with far more room than the caller knows of tokens: few workgroups)
-    WeighCut c;
     c.chunk = (int)chunk;
     c.splits = (int)((room + chunk - 1) / chunk);
     return c;
@@ -722,44 +747,48 @@ static int check_weigh(const lookat_page_pool *pool, int32_t B, int32_t group, i
     return LOOKAT_OK;
 }
 
-template <int M, int G, int PHASE, int T>
+template <int M, int G, int PHASE, int T, int THREADS>
 static int launch_weigh_phase(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
 {
     constexpr size_t lds = (size_t)G * M * kCentroids * 4;
-    const auto f = &weigh_kernel<M, G, PHASE, T>;
+    const auto f = &weigh_kernel<M, G, PHASE, T, THREADS>;
     if (lds > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
             return fail(LOOKAT_ERR_HIP, "lookat_pages_weigh: %s", hipGetErrorString(e));
     }
-    hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(kWeighThreads), lds, st, p, a);
+    hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(THREADS), lds, st, p, a);
     return check_launch("lookat_pages_weigh");
 }
 template <int M, int G, int T>
-static int launch_weigh_phases(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
+static int launch_weigh_phases(const PoolArgs &p, const WeighArgs &a, int threads, int64_t groups, hipStream_t st)
 {
+    if constexpr (G * M <= 32)
+        if (threads == kWeighSmall)
+            return launch_weigh_phase<M, G, kWeighAll, T, kWeighSmall>(p, a, groups, st);
     if (a.splits == 1)
-        return launch_weigh_phase<M, G, kWeighAll, T>(p, a, groups, st);
-    if (int rc = launch_weigh_phase<M, G, kWeighStats, T>(p, a, groups, st))
+        return launch_weigh_phase<M, G, kWeighAll, T, kWeighThreads>(p, a, groups, st);
+    if (int rc = launch_weigh_phase<M, G, kWeighStats, T, kWeighThreads>(p, a, groups, st))
         return rc;
-    return launch_weigh_phase<M, G, kWeighAdd, T>(p, a, groups, st);
+    return launch_weigh_phase<M, G, kWeighAdd, T, kWeighThreads>(p, a, groups, st);
 }
 // Few scores a thread where that is enough: short code (us a call with it / with the long code: 12 heads x 1024 tokens 4.2 / 8.1, 16 x 8 x 1000 in groups of
 // 4 7.0 / 9.7).
 template <int M, int G>
-static int launch_weigh(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
+static int launch_weigh(const PoolArgs &p, const WeighArgs &a, int threads, int64_t groups, hipStream_t st)
 {
-    constexpr int few = kWeighFew / G > 0 ? kWeighFew / G : 1;
-    return a.chunk <= few * kWeighThreads ? launch_weigh_phases<M, G, few>(p, a, groups, st) : launch_weigh_phases<M, G, kWeighScores / G>(p, a, groups, st);
+    constexpr int few = weigh_few(G);
+    return a.chunk <= few * threads ? launch_weigh_phases<M, G, few>(p, a, threads, groups, st)
+                                    : launch_weigh_phases<M, G, kWeighScores / G>(p, a, threads, groups, st);
 }
 template <int M>
-static int launch_weigh_g(int G, const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
+static int launch_weigh_g(int G, const PoolArgs &p, const WeighArgs &a, int threads, int64_t groups, hipStream_t st)
 {
     switch (G) {
-    case 1: return launch_weigh<M, 1>(p, a, groups, st);
-    case 2: return launch_weigh<M, 2>(p, a, groups, st);
-    case 4: return launch_weigh<M, 4>(p, a, groups, st);
-    default: return launch_weigh<M, 8>(p, a, groups, st);
+    case 1: return launch_weigh<M, 1>(p, a, threads, groups, st);
+    case 2: return launch_weigh<M, 2>(p, a, threads, groups, st);
+    case 4: return launch_weigh<M, 4>(p, a, threads, groups, st);
+    default: return launch_weigh<M, 8>(p, a, threads, groups, st);
     }
 }
 
@@ -819,7 +848,7 @@ extern "C" int lookat_pages_weigh(const lookat_page_pool *pool, int32_t B, int32
             return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
     }
     const int64_t units = (int64_t)B * pool->H, groups = (units + kXcds - 1) / kXcds * kXcds * cut.splits;
-    if (!fits_launch(groups, kWeighThreads))
+    if (!fits_launch(groups, cut.threads))
         return fail(LOOKAT_ERR_UNSUPPORTED, "B*H*ranges: %lld workgroups exceed one launch", (long long)groups);
     const PoolArgs p = pool_args(pool);
     WeighArgs a;
@@ -839,10 +868,10 @@ extern "C" int lookat_pages_weigh(const lookat_page_pool *pool, int32_t B, int32
     a.decay = decay;
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (p.m) {
-    case 2: return launch_weigh_g<2>(group, p, a, groups, st);
-    case 4: return launch_weigh_g<4>(group, p, a, groups, st);
-    case 8: return launch_weigh_g<8>(group, p, a, groups, st);
-    default: return launch_weigh_g<16>(group, p, a, groups, st);
+    case 2: return launch_weigh_g<2>(group, p, a, cut.threads, groups, st);
+    case 4: return launch_weigh_g<4>(group, p, a, cut.threads, groups, st);
+    case 8: return launch_weigh_g<8>(group, p, a, cut.threads, groups, st);
+    default: return launch_weigh_g<16>(group, p, a, cut.threads, groups, st);
     }
 }
 

@@ -98,6 +98,47 @@ def test_weigh_long_and_many(lk, B, H, L, g):  # noqa: F811
         assert torch.equal(weights, again)
 
 
+@pytest.mark.parametrize("m,g,B,H,L", [(2, 1, 33, 3, 1000), (16, 2, 33, 3, 500), (8, 4, 33, 3, 250), (4, 8, 33, 3, 250), (4, 1, 35, 16, 8190),
+                                       (16, 2, 35, 16, 4090), (8, 4, 35, 16, 2040), (4, 8, 35, 16, 1020), (16, 1, 1, 600, 31)])
+def test_weigh_many_heads(lk, m, g, B, H, L):  # noqa: F811
+    """Small workgroups, short code and long: lengths from none to the row's room, pages outside the pool, tables that are not finite."""
+    rng = np.random.default_rng(L + m)
+    page = 16
+    lengths = [L - b * L // max(1, B - 1) for b in range(B)]
+    W = -(-L // page)
+    P = 50
+    table = rng.integers(0, P, (B, W)).astype(np.int32)           # (values are not read, so sequences may hold the same page)
+    table[0, W // 2], table[B // 3, 0] = -1, P
+    codes = torch.from_numpy(rng.integers(0, 256, (P, H, page, m), dtype=np.uint8)).cuda()
+    pool = lk.PagePool(codes, torch.zeros((P, H, page // 8, 64, 8), dtype=torch.int8, device="cuda"), torch.zeros((P, H), dtype=torch.int8, device="cuda"))
+    lut = random_lut(rng, B, H * g, m, 2.0)
+    if B > 1:
+        lut[0, g] = -np.inf                                       # (a query head without weight; one of NaN where there is another key/value head)
+        lut[B // 2, 2 * g, 0] = np.nan
+    d_lut, d_table, d_len = dev(lut), dev(table), i32(*lengths)
+    start = torch.from_numpy(rng.random((B, H, W * page)).astype(np.float32) / L).cuda()
+    weights = start.clone()
+    lk.lookat_pages_weigh(d_lut, pool, d_table, d_len, 0.5, weights, decay=0.75)
+    there = ((d_table >= 0) & (d_table < P)).repeat_interleave(page, 1) & (torch.arange(W * page, device="cuda") < d_len[:, None])
+    size = float(d_lut.abs().nan_to_num(0, 0, 0).amax(-1).sum(-1).max()) * 0.5 * 1.4427
+    rel = 2 * ((m + 3) * U * 2 * size * 0.6932 + 2 * U) + (4 * math.sqrt(L + 64) + 4 + g) * U
+    for b in range(B):
+        n = lengths[b]
+        assert torch.equal(weights[b, :, n:], start[b, :, n:])
+        if not n:
+            continue
+        code = codes[d_table[b].clamp(0, P - 1).long()].permute(1, 3, 0, 2).reshape(H, 1, m, -1)[..., :n].long()
+        x = d_lut[b].double().view(H, g, m, 256).gather(3, code.expand(H, g, m, n)).sum(2) * 0.5
+        x = x.masked_fill(~there[b, :n], -math.inf)
+        top = x.amax(-1, keepdim=True)
+        w = torch.exp(x - torch.where(top == -math.inf, 0.0, top))
+        p = (w / torch.where(w.sum(-1, keepdim=True) == 0, 1.0, w.sum(-1, keepdim=True))).sum(1)
+        want = 0.75 * start[b, :, :n].double() + p
+        nan = p.isnan()
+        assert torch.equal(weights[b, :, :n].isnan(), nan)
+        assert bool(((weights[b, :, :n].double() - want).abs() <= rel * p + 4 * U * want)[~nan].all())
+
+
 @pytest.mark.parametrize("W", [3, 200])
 def test_weigh_scores_that_are_not_finite(lk, W):  # noqa: F811
     """A head of -inf alone adds nothing, far negative scores keep their weight (also where other ranges hold -inf alone), NaN and +inf show."""
