@@ -268,13 +268,14 @@ __device__ __forceinline__ uint32_t order_of(float w)
 
 __device__ __forceinline__ int ballot_count(bool b) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b)); }
 
-constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / kWave, kPickBins = 2048, kPickCopies = 4;
+constexpr int kPickThreads = 1024, kPickSmall = 256, kPickBins = 2048;
 
-// KEYS: the weights of up to so many tokens a thread stay in registers; 0: they are read again in every pass.  Token i * 1024 + tid is the thread's i-th.
-template <int KEYS>
-__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, int H, int page_log2)
+// KEYS: the weights of up to so many tokens a thread stay in registers; 0: they are read again in every pass.  Token i * THREADS + tid is the thread's i-th.
+template <int KEYS, int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_pick_kernel(EvictArgs a, int H, int page_log2)
 {
-    __shared__ uint32_t bins[kPickBins * kPickCopies];    // (a bin's copies side by side: many tokens have the same weight, zero among them)
+    constexpr int kPickWaves = THREADS / kWave, kPickCopies = THREADS / 256, kBinsEach = kPickBins / THREADS;
+    __shared__ __align__(16) uint32_t bins[kPickBins * kPickCopies];    // (a bin's copies side by side: many tokens have the same weight, zero among them)
     __shared__ uint32_t sums[kPickWaves];
     __shared__ uint32_t found[2];
     constexpr bool HELD = KEYS > 0;
@@ -296,27 +297,27 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, i
     if constexpr (HELD) {
 #pragma unroll
         for (int i = 0; i < kPickKeys; ++i)
-            held_w[i] = i * kPickThreads < n ? weight_at(i * kPickThreads + tid) : 0.f;
+            held_w[i] = i * THREADS < n ? weight_at(i * THREADS + tid) : 0.f;
 #pragma unroll
         for (int i = 0; i < kPickKeys; ++i)
-            held[i] = order_at(i * kPickThreads + tid, held_w[i]);
+            held[i] = order_at(i * THREADS + tid, held_w[i]);
     }
     // f(token, its order, its weight, index) for every token of this thread
     auto each = [&](auto f) {
         if constexpr (HELD) {
 #pragma unroll
             for (int i = 0; i < kPickKeys; ++i)
-                if (i * kPickThreads < n)
-                    f(i * kPickThreads + tid, held[i], held_w[i], i);
+                if (i * THREADS < n)
+                    f(i * THREADS + tid, held[i], held_w[i], i);
         } else {
-            for (int64_t at = tid, i = 0; at - tid < n; at += kPickThreads, ++i) {
+            for (int64_t at = tid, i = 0; at - tid < n; at += THREADS, ++i) {
                 const float w = weight_at((int)at);
                 f((int)at, order_at((int)at, w), w, (int)i);
             }
         }
     };
     uint32_t border = 0;                  // digits found so far
-    for (int j = tid; j < kPickBins * kPickCopies; j += kPickThreads)
+    for (int j = tid; j < kPickBins * kPickCopies; j += THREADS)
         bins[j] = 0;
     __syncthreads();
 #pragma unroll
@@ -328,13 +329,22 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, i
                 atomicAdd(&bins[((u >> shift) & ((1u << width) - 1)) * kPickCopies + (lane & (kPickCopies - 1))], 1u);
         });
         __syncthreads();
-        // the bin in which the tokens above make `left`: bins from the top, two to a thread, cleared for the next pass
-        const int j1 = kPickBins - 1 - 2 * tid, j0 = j1 - 1;
-        u32x4 *mine = reinterpret_cast<u32x4 *>(bins) + j0;
-        const u32x4 x0 = mine[0], x1 = mine[1];
+        // the bin in which the tokens above make `left`: bins from the top, kBinsEach to a thread, cleared for the next pass
+        const int low = kPickBins - (tid + 1) * kBinsEach;
+        static_assert(kBinsEach * kPickCopies == 8, "two loads");
+        u32x4 *mine = reinterpret_cast<u32x4 *>(bins + low * kPickCopies);
+        const u32x4 words[2] = {mine[0], mine[1]};
         mine[0] = mine[1] = (u32x4){0, 0, 0, 0};
-        const uint32_t c1 = x1.x + x1.y + x1.z + x1.w, c0 = x0.x + x0.y + x0.z + x0.w;
-        uint32_t upto = c1 + c0;
+        uint32_t c[kBinsEach], upto = 0;
+#pragma unroll
+        for (int j = 0; j < kBinsEach; ++j) {
+            c[j] = 0;
+#pragma unroll
+            for (int x = j * kPickCopies; x < (j + 1) * kPickCopies; ++x)
+                c[j] += words[x / 4][x % 4];
+            upto += c[j];
+        }
+        const uint32_t total = upto;
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) {
             const uint32_t x = __shfl_up(upto, d);
@@ -346,13 +356,14 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, i
 #pragma unroll
         for (int w = 0; w < kPickWaves; ++w)
             upto += w < wave ? sums[w] : 0;
-        const uint32_t above1 = upto - c1 - c0, above0 = upto - c0, want = (uint32_t)left;
-        if (above1 < want && above1 + c1 >= want) {
-            found[0] = (uint32_t)j1;
-            found[1] = above1;
-        } else if (above0 < want && above0 + c0 >= want) {
-            found[0] = (uint32_t)j0;
-            found[1] = above0;
+        uint32_t above = upto - total;
+#pragma unroll
+        for (int j = kBinsEach - 1; j >= 0; --j) {
+            if (above < (uint32_t)left && above + c[j] >= (uint32_t)left) {
+                found[0] = (uint32_t)(low + j);
+                found[1] = above;
+            }
+            above += c[j];
         }
         __syncthreads();
         border = border << width | found[0];
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a, i
         __syncthreads();
         // (two wavefronts, one for each kind, up to eight counts a lane; those of tokens that are not there are left out)
         if (wave < 2) {
-            const int used = (n + kPickThreads - 1) / kPickThreads * kPickWaves;
+            const int used = (n + THREADS - 1) / THREADS * kPickWaves;
             uint32_t c[kEach], total = 0;
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
@@ -939,13 +950,16 @@ extern "C" int lookat_pages_evict(const lookat_page_pool *pool, int32_t B, const
     a.recent = recent;
     hipStream_t st = static_cast<hipStream_t>(stream);
     // By the room of a row: a variant for few tokens is short code, and weights that stay in registers are read once (us a call of 48 heads x 1024 tokens
-    // to half, kept by 2 / by 32 / read again 15.6 / 23.9 / 16.5, x 8000 24.3 / 30.6 / 34.4 (by 8 first), 128 x 20000 - / 134 / 159).
+    // to half, kept by 2 / by 32 / read again 15.6 / 23.9 / 16.5, x 8000 24.3 / 30.6 / 34.4 (by 8 first), 128 x 20000 - / 134 / 159).  Small workgroups
+    // where there are more heads than large ones run at once: 1024 x 700 37.0, so 29.5, 1024 x 500 to 5000 69.0 / 63.6, 768 x 300 24.8 / 19.1.
     const int64_t each = ((int64_t)W * pool->page + kPickThreads - 1) / kPickThreads;
-    const auto pick = each <= 2    ? &evict_pick_kernel<2>
-                      : each <= 8  ? &evict_pick_kernel<8>
-                      : each <= 32 ? &evict_pick_kernel<32>
-                                   : &evict_pick_kernel<0>;
-    hipLaunchKernelGGL(pick, dim3((unsigned)units), dim3(kPickThreads), 0, st, a, p.H, p.page_log2);
+    const bool small = units > 512 && each <= 8;
+    const auto pick = small        ? (each <= 2 ? &evict_pick_kernel<8, kPickSmall> : &evict_pick_kernel<32, kPickSmall>)
+                      : each <= 2  ? &evict_pick_kernel<2, kPickThreads>
+                      : each <= 8  ? &evict_pick_kernel<8, kPickThreads>
+                      : each <= 32 ? &evict_pick_kernel<32, kPickThreads>
+                                   : &evict_pick_kernel<0, kPickThreads>;
+    hipLaunchKernelGGL(pick, dim3((unsigned)units), dim3(small ? kPickSmall : kPickThreads), 0, st, a, p.H, p.page_log2);
     if (int rc = check_launch("lookat_pages_evict (choice)"))
         return rc;
     const bool fp8 = pool->value_type == LOOKAT_VALUES_E4M3;

@@ -250,6 +250,32 @@ def test_evict(lk, d_k, m, page, kind, first, recent, room):  # noqa: F811
     assert_pool(pool, after)
 
 
+@pytest.mark.parametrize("longest", [100, 2047, 3000])
+def test_evict_many_heads(lk, longest):  # noqa: F811
+    """Small workgroups for the choice: a long sequence among short ones, equal weights and NaN, kept tokens from as many octets as there are."""
+    rng = np.random.default_rng(longest)
+    B, H, page, keep = 33, 16, 16, 40
+    lengths = [longest] + [int(n) for n in rng.integers(0, 60, B - 1)]
+    W, W_out = -(-longest // page), 3
+    P = sum(-(-n // page) for n in lengths) + B * W_out
+    c = random_cache(rng, P, H, 64, 4, page, "int8", -6, -3)
+    ids = rng.permutation(P).astype(np.int32)
+    table, used = np.full((B, W), -1, np.int32), 0
+    for b, n in enumerate(lengths):
+        held = -(-n // page)
+        table[b, :held], used = ids[used:used + held], used + held
+    table_out = ids[used:].reshape(B, W_out)
+    weights = spread_weights(rng, B, H, W * page)
+    weights[:, 1] = np.round(weights[:, 1])
+    weights[:, 2, ::3] = np.nan
+    weights[0, 3] = 0.5
+    pool, out = on_gpu(lk, c), torch.full((B, H, W_out * page), -2.0, device="cuda")
+    lk.lookat_pages_evict(pool, dev(table), i32(*lengths), dev(weights), i32(*[keep] * B), dev(table_out), first=2, recent=3, weights_out=out)
+    after, _, want = evict_reference(c, table, lengths, weights, [keep] * B, 2, 3, table_out, np.full((B, H, W_out * page), -2.0, np.float32))
+    assert np.array_equal(out.cpu().numpy(), want, equal_nan=True)
+    assert_pool(pool, after)
+
+
 def test_evict_weights_of_all_kinds(lk):  # noqa: F811
     """Equal weights, zeros of both signs, infinities, NaN, subnormals, fewer columns than tokens, strided weights, ids outside the pool."""
     rng = np.random.default_rng(3)
