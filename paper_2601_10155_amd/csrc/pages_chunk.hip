@@ -12,7 +12,7 @@
 //   * O^T = V^T P^T: keys are dealt to the rows of K^ (bits 2 and 3 of a row's number exchanged) such that the eight weights that a lane holds
 //     of an operand belong to eight consecutive tokens: the weights, as two fp16 terms, are the operand where they are, and the values' operand
 //     is eight consecutive stored bytes, as the page holds them.
-// The centroids are split once per call by a small kernel, into the workspace.  A workgroup of NW wavefronts (32 NW rows of one key/value head,
+// The centroids are split once per call by a small kernel, into the workspace (or by every workgroup, see below).  A workgroup of NW wavefronts (32 NW rows of one key/value head,
 // query heads of a group side by side) fetches the centroids of 64 keys by code into LDS, two buffers of 64 keys in turn; their ids, codes and
 // centroids are requested three, two and one tiles ahead.
 #include "pages_values.h"
@@ -23,6 +23,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 struct ChunkArgs {
     const void *q;
+    const float *codebooks;
     const char *books;                    // [H, m, 256, 2, d_sub] fp16: both terms of a centroid
     const float *unscale;                 // [H] 2^-s
     const int32_t *table, *lengths, *counts;
@@ -45,6 +46,34 @@ __device__ __forceinline__ int lift_of(uint32_t bits)
     return s > 126 ? 126 : s < -126 ? -126 : s;
 }
 
+// The largest magnitude of four coordinates and those before, as bits.  (Entries that are not finite do not count: no token may have them.)
+__device__ __forceinline__ uint32_t finite_top(const v4u &x, uint32_t top)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t a = x[k] & 0x7fffffffu;
+        top = a < 0x7f800000u && a > top ? a : top;
+    }
+    return top;
+}
+// Coordinates 4 u .. 4 u + 3 of a head's [m, 256, d_sub], times f, as two fp16 terms to their places in its [m, 256, 2, d_sub].
+__device__ __forceinline__ void split_book(const v4u &x, float f, int u, int dsub_log2, char *book)
+{
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float a = __uint_as_float(x[2 * k]) * f, b = __uint_as_float(x[2 * k + 1]) * f;
+        const v2h hh = {(_Float16)a, (_Float16)b};
+        const v2h ll = {(_Float16)(a - (float)hh.x), (_Float16)(b - (float)hh.y)};
+        hi[k] = __builtin_bit_cast(uint32_t, hh);
+        lo[k] = __builtin_bit_cast(uint32_t, ll);
+    }
+    const int first = 4 * u, centroid = first >> dsub_log2, j = first & ((1 << dsub_log2) - 1);
+    char *to = book + ((((centroid << dsub_log2) * 2) + j) << 1);
+    *reinterpret_cast<v2u *>(to) = (v2u){hi[0], hi[1]};
+    *reinterpret_cast<v2u *>(to + (2 << dsub_log2)) = (v2u){lo[0], lo[1]};
+}
+
 constexpr int kBookThreads = 512, kBookParts = 8;
 // grid: (part, head)
 __global__ __launch_bounds__(kBookThreads) void chunk_books_kernel(const float *codebooks, char *books, float *unscale, int d_k, int dsub_log2)
@@ -55,11 +84,7 @@ __global__ __launch_bounds__(kBookThreads) void chunk_books_kernel(const float *
     uint32_t top = 0;
     for (int u = tid; u < units; u += kBookThreads) {
         const v4u x = src[u];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t a = x[k] & 0x7fffffffu;
-            top = a < 0x7f800000u && a > top ? a : top;       // (entries that are not finite do not count: no token may have them)
-        }
+        top = finite_top(x, top);
     }
     top = __float_as_uint(wave_max(__uint_as_float(top)));
     if ((tid & (kWave - 1)) == 0)
@@ -73,22 +98,8 @@ __global__ __launch_bounds__(kBookThreads) void chunk_books_kernel(const float *
         unscale[h] = power_of_two(-s);
     const float f = power_of_two(s);
     const int per = units / kBookParts;
-    for (int u = blockIdx.x * per + tid; u < (int)(blockIdx.x + 1) * per; u += kBookThreads) {
-        const v4u x = src[u];
-        uint32_t hi[2], lo[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const float a = __uint_as_float(x[2 * k]) * f, b = __uint_as_float(x[2 * k + 1]) * f;
-            const v2h hh = {(_Float16)a, (_Float16)b};
-            const v2h ll = {(_Float16)(a - (float)hh.x), (_Float16)(b - (float)hh.y)};
-            hi[k] = __builtin_bit_cast(uint32_t, hh);
-            lo[k] = __builtin_bit_cast(uint32_t, ll);
-        }
-        const int first = 4 * u, centroid = first >> dsub_log2, j = first & ((1 << dsub_log2) - 1);
-        char *to = books + ((((int64_t)h * kCentroids * d_k + ((int64_t)centroid << dsub_log2)) * 2 + j) << 1);
-        *reinterpret_cast<v2u *>(to) = (v2u){hi[0], hi[1]};
-        *reinterpret_cast<v2u *>(to + (2 << dsub_log2)) = (v2u){lo[0], lo[1]};
-    }
+    for (int u = blockIdx.x * per + tid; u < (int)(blockIdx.x + 1) * per; u += kBookThreads)
+        split_book(src[u], f, u, dsub_log2, books + (int64_t)h * kCentroids * d_k * 4);
 }
 
 // What a tile of rows of one sequence sees.
@@ -531,16 +542,22 @@ __global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_k
         }
 }
 
-// Few rows (drafted tokens, the ends of prompts): 16 RB rows of a (sequence, head) to a workgroup, whose wavefronts take tiles of 32 tokens in turn, each
-// for itself: centroids go straight from the books to the operand's registers, values as in attention of one token, and the wavefronts'
-// results are merged in LDS.  v_mfma_f32_16x16x32_f16: keys are dealt to the two blocks of 16 such that a lane's eight scores belong to one octet.
+// Few rows (drafted tokens, the ends of prompts), and few heads: 16 RB rows of a (sequence, head) to a workgroup, whose wavefronts take tiles of 32 tokens in
+// turn, each for itself, values as in attention of one token, and the wavefronts' results are merged in LDS.  v_mfma_f32_16x16x32_f16: keys are dealt to
+// the two blocks of 16 such that a lane's eight scores belong to one octet.
+// A workgroup of eight wavefronts splits its head's codebook itself, into LDS (64 or 128 KB), and looks its operands up there; one of two takes them from the
+// books in memory.  Looked up in memory by eight wavefronts a tile's operands were 4 KB to 16 KB of scattered 64-byte pieces: us a call, so / from LDS, 16 x 12
+// x 8 rows behind 1000 tokens 18.0 / 11.1, 32 x 2 behind 20000, d_k = 128 62.8 / 30.3, 1280 x 2 behind 200 to 2000, d_k = 128 144 / 81.
 constexpr int kFewWaves = 8, kBriefWaves = 2, kFewKeys = 32;
+__host__ __device__ constexpr bool few_staged(int waves) { return waves == kFewWaves; }
 __host__ __device__ constexpr size_t few_lds_bytes(int d_k, int waves) { return (size_t)waves * 16 * (d_k + 4) * 4 + waves * 16 * 8; }
 
 template <int DK, bool SMALL, bool Q32, bool FP8, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, ChunkArgs a)
 {
+    constexpr bool STAGED = few_staged(WAVES);
     constexpr int STEPS = DK / 32, CB = DK / 32, TQ = 16 * RB, ROW = DK + 4;
+    __shared__ float tops_s[STAGED ? WAVES : 1];
     extern __shared__ __align__(16) char few_s[];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, quad = lane >> 4, col = lane & 15;
     const Place at = place_of(a);
@@ -591,7 +608,7 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
                 }
     };
     v4u piece[2][STEPS][2];
-    const char *books = a.books + (int64_t)h * kCentroids * DK * 4;
+    const char *books = STAGED ? few_s : a.books + (int64_t)h * kCentroids * DK * 4;
     auto load_centroids = [&]() {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -619,7 +636,37 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
     v8h qh[RB][STEPS], ql[Q32 ? RB : 1][STEPS];
     float to_log2[RB];
     int seen[RB];
-    const float unscale = a.unscale[h];
+    float unscale;
+    if constexpr (STAGED) {
+        // the head's centroids into LDS, scaled and split as in chunk_books_kernel
+        constexpr int EACH = kCentroids * DK / 4 / (WAVES * kWave);
+        const v4u *src = reinterpret_cast<const v4u *>(a.codebooks) + (int64_t)h * (kCentroids * DK / 4);
+        v4u x[EACH];
+        uint32_t top = 0;
+#pragma unroll
+        for (int u = 0; u < EACH; ++u)
+            x[u] = src[u * (WAVES * kWave) + tid];
+#pragma unroll
+        for (int u = 0; u < EACH; ++u)
+            top = finite_top(x[u], top);
+        const float wave_top = wave_max(__uint_as_float(top));
+        if (lane == 0)
+            tops_s[wave] = wave_top;
+        __syncthreads();
+        float head_top = tops_s[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+            head_top = fmaxf(head_top, tops_s[w]);
+        const int lift = lift_of(__float_as_uint(head_top));
+        unscale = power_of_two(-lift);
+        const float f = power_of_two(lift);
+#pragma unroll
+        for (int u = 0; u < EACH; ++u)
+            split_book(x[u], f, u * (WAVES * kWave) + tid, a.dsub_log2, few_s);
+        __syncthreads();
+    } else {
+        unscale = a.unscale[h];
+    }
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
         const int r = r0 + 16 * j + col, n = r / a.group, hq = h * a.group + r - n * a.group;
@@ -682,8 +729,10 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
     }
     if (t < range.t1) {
         load_codes(t, id_k0);
-        load_centroids();
-        load_codes(t + WAVES, id_k1);
+        if constexpr (!STAGED) {
+            load_centroids();
+            load_codes(t + WAVES, id_k1);
+        }
     }
     while (t < range.t1) {
         // values of this tile
@@ -696,6 +745,10 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
             v[c] = *reinterpret_cast<const v4u *>(src + c * 256);
         const int stored_e = head_exponents[(uint64_t)page * (uint32_t)p.H];
         const float e = id_v < 0 ? 0.f : (float)stored_e;
+        if constexpr (STAGED) {
+            load_centroids();
+            load_codes(t + WAVES, id_k1);
+        }
         // scores: element 4 k + i belongs to token 8 quad + 4 k + i
         const bool edge = (t + 1) * kFewKeys > seen_by_all || __builtin_amdgcn_ballot_w64(id_k < 0 || id_v < 0);
         if (edge) {
@@ -730,10 +783,11 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
             }
         // centroids of the next tile, codes of the one behind it, page ids of the third
         const int id_kn = load_id(t + 3 * WAVES, my_octet), id_vn = load_id(t + 2 * WAVES, quad);
-        if (t + WAVES < range.t1) {
-            load_centroids();
-            load_codes(t + 2 * WAVES, id_k2);
-        }
+        if constexpr (!STAGED)
+            if (t + WAVES < range.t1) {
+                load_centroids();
+                load_codes(t + 2 * WAVES, id_k2);
+            }
         if (edge) {
             const int have = id_v < 0 ? 0 : range.end - t * kFewKeys - 8 * quad;
 #pragma unroll
@@ -811,6 +865,8 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
     // The wavefronts' results, 16 rows at a time: references and sums first, so that every wavefront brings its own to the common reference.
     float *results = reinterpret_cast<float *>(few_s);
     float2 *stats = reinterpret_cast<float2 *>(few_s + (size_t)WAVES * 16 * ROW * 4);
+    if constexpr (STAGED)
+        __syncthreads();                  // (the centroids were read)
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
         float u, w;
@@ -899,15 +955,17 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
 {
     ChunkCut c;
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
-    // The kernel for few rows, us a call with it / without: 416 (sequence, head) pairs x 64 rows x 600 tokens, d_k = 128 54 / 78, 32 x 40 x 1000 23 / 38,
-    // 8 x 64 x 8000 32 / 44, 256 x 64 x 4000 142 / 256, d_k = 64 96 x 64 x 1000 18 / 32; with nothing to see but the chunk's own tokens
-    // (1856 x 43) 40 / 27.  128 rows: 32 x 1000 26 / 36, 48 x 500 15 / 27, but 128 x 4000 138 / 108.
-    const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room;
-    const bool few = rows <= 32 || (longest > 256 && (rows <= 64 || (rows <= 128 && units <= 64)));
+    // The kernel for few rows, us a call with it / without.  Few workgroups of it: 8 (sequence, head) pairs x 48 rows x 200 tokens, d_k = 64 9.0 / 16.5, 40 x 256 x
+    // 1256 25 / 36, 16 x 1024 x 9024, d_k = 128 158 / 184, 1 x 2048 x 10048 38 / 59.  Up to 64 rows: 800 x 48 x 1048, d_k = 128 137 / 266, 200 x 64 x 4064 85 / 177.
+    // Some more, with something to see: 100 x 256 x 1156, d_k = 64 48 / 53, d_k = 128 76 / 90, but 200 x 128 x 228 31 / 20, 200 x 256 x 1256 88 / 64, 96 x 600 x
+    // 600 56 / 33.
+    const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room, groups = units * ((rows + 31) / 32);
+    const bool few = rows <= 64 || groups <= 512 || (groups <= 1100 && longest > 512);
     c.few = !few ? 0 : rows <= 16 ? 1 : 2;
-    // Two wavefronts instead of eight where many heads have little to see: 1125 x 16 rows x 8 tokens 23 / 41 us, 2048 x 8 x 208 51 / 74, but 192 x 8 x 208
-    // 12.1 / 10.4.
-    c.waves = c.few ? (longest > 256 || units < 512 ? kFewWaves : kBriefWaves) : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
+    // Its workgroups have eight wavefronts, or two where there are many and a head has little to see, not worth its centroids in LDS: us a call, eight / two,
+    // 768 x 8 rows x 8 tokens 13.2 / 9.8, 1280 x 8 x 308 24.3 / 26.8, 1280 x 20 x 320 40.5 / 30.2, 768 x 64 x 514 55 / 43, 768 x 20 x 470, d_k = 128 43 / 42.
+    c.waves = c.few ? (groups <= 512 || longest > (rows <= 16 ? 256 : rows <= 32 ? 512 : 768) ? kFewWaves : kBriefWaves)
+                    : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
     c.splits = num_splits;
@@ -962,8 +1020,8 @@ static int launch_few(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8,
 {
     const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, true, false, RB, WAVES>)
                        : (fp8 ? &chunk_few_kernel<DK, SMALL, false, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, false, false, RB, WAVES>);
-    constexpr size_t lds = few_lds_bytes(DK, WAVES);
-    if (lds > 64 * 1024) {
+    constexpr size_t results = few_lds_bytes(DK, WAVES), book = few_staged(WAVES) ? (size_t)kCentroids * DK * 4 : 0, lds = results > book ? results : book;
+    if (lds > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess)
             return fail(LOOKAT_ERR_HIP, "lookat_attend_pages_chunk: %s", hipGetErrorString(e));
@@ -1039,6 +1097,7 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
     const int dsub = p.d_k / p.m, dsub_log2 = 31 - __builtin_clz((unsigned)dsub);
     ChunkArgs a;
     a.q = q;
+    a.codebooks = codebooks;
     char *books = static_cast<char *>(workspace);
     float *unscale = reinterpret_cast<float *>(books + cut.books);
     a.books = books;
@@ -1064,9 +1123,11 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
     a.per_die = (int32_t)per_die;
     a.scale_log2e = scale * kLog2e;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(chunk_books_kernel, dim3(kBookParts, p.H), dim3(kBookThreads), 0, st, codebooks, books, unscale, p.d_k, dsub_log2);
-    if (int rc = check_launch("lookat_attend_pages_chunk (codebooks)"))
-        return rc;
+    if (!(cut.few && few_staged(cut.waves))) {
+        hipLaunchKernelGGL(chunk_books_kernel, dim3(kBookParts, p.H), dim3(kBookThreads), 0, st, codebooks, books, unscale, p.d_k, dsub_log2);
+        if (int rc = check_launch("lookat_attend_pages_chunk (codebooks)"))
+            return rc;
+    }
     const bool q32 = q_dtype == LOOKAT_F32, fp8 = pool->value_type == LOOKAT_VALUES_E4M3;
     const int rc = p.d_k == 128 ? launch_rows<128, false>(cut, p, a, q32, fp8, (unsigned)groups, st)
                    : dsub == 4  ? launch_rows<64, true>(cut, p, a, q32, fp8, (unsigned)groups, st)

@@ -255,9 +255,27 @@ def test_one_row_is_attention_of_one_token(lk):  # noqa: F811
     (40, 16, 4, 4, 60, 64, 4, 64),        # few rows of many heads that see little: two wavefronts
     (40, 16, 5, 6, 100, 128, 4, 128),
     (2, 3, 8, 16, 5000, 64, 8, 64),       # few rows in ranges: 128 of few heads
-    (1, 1, 4, 8, 9000, 128, 8, 128)])
+    (1, 1, 4, 8, 9000, 128, 8, 128),
+    (10, 10, 2, 128, 100, 128, 2, 64),    # 128 rows to a workgroup again
+    (6, 20, 2, 150, 100, 64, 8, 32),
+    (40, 16, 1, 50, 20, 64, 16, 16),      # two wavefronts, two tiles of rows
+    (2, 3, 1, 700, 0, 64, 8, 16),         # many rows of few heads
+    (1, 2, 2, 300, 1500, 128, 2, 64),
+    (2, 2, 1, 400, 77, 64, 16, 128)])
 def test_every_kernel(lk, B, H, g, N, before, d_k, m, page, dtype, kind):  # noqa: F811
-    """The kernels that large and small launches take, against torch in 64 bits.  The bound is that of `reference`, with the row's own sizes."""
+    """The kernels that large and small launches take, against torch in 64 bits."""
+    against_torch(lk, B, H, g, N, before, d_k, m, page, dtype, kind)
+
+
+@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page", [(8, 32, 1, 260, 400, 128, 8, 32), (10, 10, 2, 128, 300, 128, 4, 64), (6, 20, 2, 150, 200, 64, 8, 32),
+                                                       (40, 16, 2, 8, 200, 64, 8, 16), (3, 5, 1, 100, 900, 128, 16, 16)])
+def test_every_kernel_in_ranges(lk, B, H, g, N, before, d_k, m, page):  # noqa: F811
+    for splits, dtype in ((2, "float16"), (5, "float32")):
+        against_torch(lk, B, H, g, N, before, d_k, m, page, dtype, "float8", splits)
+
+
+def against_torch(lk, B, H, g, N, before, d_k, m, page, dtype, kind, splits=0):  # noqa: F811
+    """The bound is that of `reference`, with the row's own sizes."""
     gen = torch.Generator(device="cuda").manual_seed(B + N)
     rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
     lengths = [max(1, N + before - 3 * b) for b in range(B)]
@@ -272,7 +290,7 @@ def test_every_kernel(lk, B, H, g, N, before, d_k, m, page, dtype, kind):  # noq
     books = rnd(H, m, 256, d_k // m)
     q = rnd(B, N, H * g, d_k).to(getattr(torch, dtype)).transpose(1, 2)
     scale = 1 / math.sqrt(d_k)
-    got = lk.lookat_attend_pages_chunk(q, books, pool, table, i32(*lengths), scale, counts=i32(*counts))
+    got = lk.lookat_attend_pages_chunk(q, books, pool, table, i32(*lengths), scale, counts=i32(*counts), num_splits=splits)
     head, sub = torch.arange(H, device="cuda")[:, None, None], torch.arange(m, device="cuda")
     for b in range(B):
         n, k, ids = lengths[b], counts[b], table[b].long()
