@@ -185,10 +185,10 @@ __device__ __forceinline__ uint32_t left_of(float w0, float w1, uint32_t h)
 }
 
 // Wavefronts to a SIMD that the registers have to allow.
-__host__ __device__ constexpr int chunk_waves(int d_k, bool q32, int keys) { return 2; }
+constexpr int kChunkWaves = 2;
 
 template <int DK, bool SMALL, bool Q32, bool FP8, int NW, int KEYS>
-__global__ __launch_bounds__(NW *kWave, chunk_waves(DK, Q32, KEYS)) void chunk_kernel(PoolArgs p, ChunkArgs a)
+__global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs p, ChunkArgs a)
 {
     constexpr int threads = NW * kWave, CH = DK / 8, STEPS = DK / 16, CB = DK / 32, TQ = 32 * NW;
     constexpr int TPK = threads / KEYS, CPT = CH / TPK, KB = KEYS / 32, GROUPS = KEYS / 16;                                 // 8-coordinate pieces of a key that a thread fetches
@@ -962,10 +962,12 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room, groups = units * ((rows + 31) / 32);
     const bool few = rows <= 64 || groups <= 512 || (groups <= 1100 && longest > 512);
     c.few = !few ? 0 : rows <= 16 ? 1 : 2;
+    // (Without it: 256 rows to a workgroup where they read long sequences and fill the chip, 128 otherwise: us a call, 256 / 128, 32 x 2048 x 32049 1987 / 2169,
+    // 128 x 1000 x 5000 572 / 625, 128 x 2000 x 2000 326 / 321, 96 x 600 x 2600 259 / 173, 320 x 380 x 880 170 / 129.)
     // Its workgroups have eight wavefronts, or two where there are many and a head has little to see, not worth its centroids in LDS: us a call, eight / two,
     // 768 x 8 rows x 8 tokens 13.2 / 9.8, 1280 x 8 x 308 24.3 / 26.8, 1280 x 20 x 320 40.5 / 30.2, 768 x 64 x 514 55 / 43, 768 x 20 x 470, d_k = 128 43 / 42.
     c.waves = c.few ? (groups <= 512 || longest > (rows <= 16 ? 256 : rows <= 32 ? 512 : 768) ? kFewWaves : kBriefWaves)
-                    : p->d_k == 64 || units * ((rows + 255) / 256) < 256 ? 4 : 8;
+                    : p->d_k == 128 && rows >= 768 && longest > 2048 && units * ((rows + 255) / 256) >= 256 ? 8 : 4;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
     c.splits = num_splits;
@@ -1003,13 +1005,14 @@ static int check_chunk(const lookat_page_pool *pool, int32_t B, int32_t N, int32
     return LOOKAT_OK;
 }
 
-// Tokens of a tile: 64 for 256 rows of fp16, 32 where fp32 rows take the registers or the workgroup is small.
-constexpr int chunk_keys(int waves, bool q32) { return waves == 8 && !q32 ? 64 : 32; }
+// Tokens of a tile: 64, or 32 at d_k = 128 where fp32 rows take the registers or the workgroup is small.  (d_k = 64, us a call, 32 / 64: 32 x 2048 rows 77 / 67,
+// behind 2000 tokens 142 / 125, 64 x 1000 fp32 48.0 / 44.6, 8 x 12 x 400 to 1000 fp32 53.3 / 51.2.)
+constexpr int chunk_keys(int d_k, int waves, bool q32) { return d_k == 64 || (waves == 8 && !q32) ? 64 : 32; }
 
 template <int DK, bool SMALL, int NW>
 static int launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
-    constexpr int K32 = chunk_keys(NW, true), K16 = chunk_keys(NW, false);
+    constexpr int K32 = chunk_keys(DK, NW, true), K16 = chunk_keys(DK, NW, false);
     const auto f = q32 ? (fp8 ? &chunk_kernel<DK, SMALL, true, true, NW, K32> : &chunk_kernel<DK, SMALL, true, false, NW, K32>)
                        : (fp8 ? &chunk_kernel<DK, SMALL, false, true, NW, K16> : &chunk_kernel<DK, SMALL, false, false, NW, K16>);
     hipLaunchKernelGGL(f, dim3(groups), dim3(NW * kWave), 0, st, p, a);
@@ -1137,6 +1140,6 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
     if (cut.splits == 1)
         return LOOKAT_OK;
     hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)N, (unsigned)(p.H * group), (unsigned)B), dim3(p.d_k), 0, st, a, p.H, p.d_k, p.page_log2,
-                       cut.rows, cut.few ? kFewKeys : chunk_keys(cut.waves, q32));
+                       cut.rows, cut.few ? kFewKeys : chunk_keys(p.d_k, cut.waves, q32));
     return check_launch("lookat_attend_pages_chunk (merge)");
 }

@@ -248,15 +248,17 @@ def test_one_row_is_attention_of_one_token(lk):  # noqa: F811
 @pytest.mark.parametrize("dtype", ["float16", "float32"])
 @pytest.mark.parametrize("kind", ["int8", "float8"])
 @pytest.mark.parametrize("B,H,g,N,before,d_k,m,page", [
-    (8, 32, 1, 260, 150, 128, 8, 32),     # 256 rows to a workgroup
+    (2, 43, 1, 770, 1400, 128, 8, 32),    # 256 rows to a workgroup
+    (2, 43, 2, 385, 1800, 128, 16, 128),
+    (8, 32, 1, 260, 150, 128, 8, 32),     # 128 rows
     (3, 90, 2, 140, 0, 128, 16, 128),     # ... with two rows to a token, prompts
-    (6, 2, 4, 100, 900, 128, 2, 64),      # 128 rows to a workgroup
+    (6, 2, 4, 100, 900, 128, 2, 64),      # few heads
     (5, 20, 3, 70, 333, 64, 16, 16),
     (40, 16, 4, 4, 60, 64, 4, 64),        # few rows of many heads that see little: two wavefronts
     (40, 16, 5, 6, 100, 128, 4, 128),
     (2, 3, 8, 16, 5000, 64, 8, 64),       # few rows in ranges: 128 of few heads
     (1, 1, 4, 8, 9000, 128, 8, 128),
-    (10, 10, 2, 128, 100, 128, 2, 64),    # 128 rows to a workgroup again
+    (10, 10, 2, 128, 100, 128, 2, 64),    # 128 rows to a workgroup
     (6, 20, 2, 150, 100, 64, 8, 32),
     (40, 16, 1, 50, 20, 64, 16, 16),      # two wavefronts, two tiles of rows
     (2, 3, 1, 700, 0, 64, 8, 16),         # many rows of few heads
@@ -267,7 +269,7 @@ def test_every_kernel(lk, B, H, g, N, before, d_k, m, page, dtype, kind):  # noq
     against_torch(lk, B, H, g, N, before, d_k, m, page, dtype, kind)
 
 
-@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page", [(8, 32, 1, 260, 400, 128, 8, 32), (10, 10, 2, 128, 300, 128, 4, 64), (6, 20, 2, 150, 200, 64, 8, 32),
+@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page", [(2, 43, 1, 770, 1400, 128, 4, 64), (8, 32, 1, 260, 400, 128, 8, 32), (10, 10, 2, 128, 300, 128, 4, 64), (6, 20, 2, 150, 200, 64, 8, 32),
                                                        (40, 16, 2, 8, 200, 64, 8, 16), (3, 5, 1, 100, 900, 128, 16, 16)])
 def test_every_kernel_in_ranges(lk, B, H, g, N, before, d_k, m, page):  # noqa: F811
     for splits, dtype in ((2, "float16"), (5, "float32")):
