@@ -955,18 +955,20 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
 {
     ChunkCut c;
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
-    // The kernel for few rows, us a call with it / without.  Few workgroups of it: 8 (sequence, head) pairs x 48 rows x 200 tokens, d_k = 64 9.0 / 16.5, 40 x 256 x
-    // 1256 25 / 36, 16 x 1024 x 9024, d_k = 128 158 / 184, 1 x 2048 x 10048 38 / 59.  Up to 64 rows: 800 x 48 x 1048, d_k = 128 137 / 266, 200 x 64 x 4064 85 / 177.
-    // Some more, with something to see: 100 x 256 x 1156, d_k = 64 48 / 53, d_k = 128 76 / 90, but 200 x 128 x 228 31 / 20, 200 x 256 x 1256 88 / 64, 96 x 600 x
-    // 600 56 / 33.
+    // The kernel for few rows, us a call with it / without.  One tile of its rows, or few workgroups: 240 (sequence, head) pairs x 32 rows x 632 tokens, d_k = 128
+    // 17.5 / 44, 8 x 48 x 248, d_k = 64 9.0 / 16.5, 40 x 256 x 1256 25 / 36, 16 x 1024 x 9024, d_k = 128 158 / 184, 1 x 2048 x 10048 38 / 59.  Two tiles at d_k = 64:
+    // 400 x 64 x 664 37 / 45, but at d_k = 128 60 / 62 and, fp32 rows, 70 / 87, though 1264 tokens 88 / 100.  Some more where there is more to see: 200 x 128 x
+    // 1028 75 / 86, but 200 x 128 x 228 31 / 20, 400 x 96 x 996 101 / 81, 96 x 600 x 600 56 / 33.
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room, groups = units * ((rows + 31) / 32);
-    const bool few = rows <= 64 || groups <= 512 || (groups <= 1100 && longest > 512);
+    const bool few = rows <= 32 || groups <= 512 || (rows <= 64 && p->d_k == 64) || ((rows <= 64 || groups <= 1024) && longest > 1000);
     c.few = !few ? 0 : rows <= 16 ? 1 : 2;
     // (Without it: 256 rows to a workgroup where they read long sequences and fill the chip, 128 otherwise: us a call, 256 / 128, 32 x 2048 x 32049 1987 / 2169,
     // 128 x 1000 x 5000 572 / 625, 128 x 2000 x 2000 326 / 321, 96 x 600 x 2600 259 / 173, 320 x 380 x 880 170 / 129.)
     // Its workgroups have eight wavefronts, or two where there are many and a head has little to see, not worth its centroids in LDS: us a call, eight / two,
-    // 768 x 8 rows x 8 tokens 13.2 / 9.8, 1280 x 8 x 308 24.3 / 26.8, 1280 x 20 x 320 40.5 / 30.2, 768 x 64 x 514 55 / 43, 768 x 20 x 470, d_k = 128 43 / 42.
-    c.waves = c.few ? (groups <= 512 || longest > (rows <= 16 ? 256 : rows <= 32 ? 512 : 768) ? kFewWaves : kBriefWaves)
+    // 768 x 8 rows x 8 tokens 13.2 / 9.8, 768 x 12 x 128, d_k = 128 26.4 / 17.8, 1280 x 8 x 308 24.3 / 26.8, 375 x 1 x 32 10.1 / 11.6, 400 x 20 x 70, d_k = 128 24.9 / 22.2, 400 x 20 x 320 28.9 / 31.4, 1280 x 20 x 320 62.6 / 49.1,
+    // 1280 x 32 x 632 82 / 95, d_k = 64 400 x 64 x 1264 60.5 / 54.1.
+    const int64_t brief = groups <= (rows <= 16 ? 512 : 256) ? 0 : rows <= 16 ? 256 : groups <= 512 ? 128 : rows <= 32 || p->d_k == 128 ? 448 : 1536;
+    c.waves = c.few ? (longest > brief ? kFewWaves : kBriefWaves)
                     : p->d_k == 128 && rows >= 768 && longest > 2048 && units * ((rows + 255) / 256) >= 256 ? 8 : 4;
     c.rows = c.few ? 16 * c.few : 32 * c.waves;
     c.tiles = (int)((rows + c.rows - 1) / c.rows);
