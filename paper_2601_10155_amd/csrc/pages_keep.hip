@@ -718,12 +718,14 @@ static WeighCut weigh_cut(const lookat_page_pool *p, int32_t B, int32_t G, int32
     WeighCut c;
     // Small workgroups where there are more heads than large ones run at once, or where their short code holds a row (us a call of large / small ones:
     // 40 x 32 heads x 90 to 900 tokens, m = 16, 16.2 / 11.0, 64 x 32 x 30 to 300 in groups of 2 21.1 / 10.4, 64 x 12 x 500 to 5000 32.0 / 15.3, 16 x 12 x 900
-    // 4.7 / 3.8, but 16 x 32 x 2000 6.4 / 8.1), while their tables leave room for 16 wavefronts of them.
+    // 4.7 / 3.8, but 16 x 32 x 2000 6.4 / 8.1), while their tables leave room for 16 wavefronts of them.  Rows that a large one does not hold are cut either
+    // way: 24 x 32 x 8927 in groups of 8 122 / 93, 20 x 32 x 6300 to 9000 in groups of 4 60.7 / 40.5.
     const bool brief = units >= 96 && room <= weigh_few(G) * kWeighSmall;
-    if ((units > 512 || brief) && G * p->m <= 32 && room <= weigh_tokens(G, kWeighSmall)) {
+    const int64_t small = weigh_tokens(G, kWeighSmall);
+    if ((units > 512 || brief) && G * p->m <= 32 && (room <= small || (room > weigh_tokens(G, kWeighThreads) && room <= 1024 * small))) {
         c.threads = kWeighSmall;
-        c.chunk = (int)((room + kWeighSmall - 1) / kWeighSmall * kWeighSmall);
-        c.splits = 1;
+        c.chunk = (int)(room <= small ? (room + kWeighSmall - 1) / kWeighSmall * kWeighSmall : small);
+        c.splits = (int)((room + c.chunk - 1) / c.chunk);
         return c;
     }
     c.threads = kWeighThreads;
@@ -771,17 +773,22 @@ static int launch_weigh_phase(const PoolArgs &p, const WeighArgs &a, int64_t gro
     hipLaunchKernelGGL(f, dim3((unsigned)groups), dim3(THREADS), lds, st, p, a);
     return check_launch("lookat_pages_weigh");
 }
+template <int M, int G, int T, int THREADS>
+static int launch_weigh_threads(const PoolArgs &p, const WeighArgs &a, int64_t groups, hipStream_t st)
+{
+    if (a.splits == 1)
+        return launch_weigh_phase<M, G, kWeighAll, T, THREADS>(p, a, groups, st);
+    if (int rc = launch_weigh_phase<M, G, kWeighStats, T, THREADS>(p, a, groups, st))
+        return rc;
+    return launch_weigh_phase<M, G, kWeighAdd, T, THREADS>(p, a, groups, st);
+}
 template <int M, int G, int T>
 static int launch_weigh_phases(const PoolArgs &p, const WeighArgs &a, int threads, int64_t groups, hipStream_t st)
 {
     if constexpr (G * M <= 32)
         if (threads == kWeighSmall)
-            return launch_weigh_phase<M, G, kWeighAll, T, kWeighSmall>(p, a, groups, st);
-    if (a.splits == 1)
-        return launch_weigh_phase<M, G, kWeighAll, T, kWeighThreads>(p, a, groups, st);
-    if (int rc = launch_weigh_phase<M, G, kWeighStats, T, kWeighThreads>(p, a, groups, st))
-        return rc;
-    return launch_weigh_phase<M, G, kWeighAdd, T, kWeighThreads>(p, a, groups, st);
+            return launch_weigh_threads<M, G, T, kWeighSmall>(p, a, groups, st);
+    return launch_weigh_threads<M, G, T, kWeighThreads>(p, a, groups, st);
 }
 // Few scores a thread where that is enough: short code (us a call with it / with the long code: 12 heads x 1024 tokens 4.2 / 8.1, 16 x 8 x 1000 in groups of
 // 4 7.0 / 9.7).

@@ -99,7 +99,8 @@ def test_weigh_long_and_many(lk, B, H, L, g):  # noqa: F811
 
 
 @pytest.mark.parametrize("m,g,B,H,L", [(2, 1, 33, 3, 1000), (16, 2, 33, 3, 500), (8, 4, 33, 3, 250), (4, 8, 33, 3, 250), (4, 1, 35, 16, 8190),
-                                       (16, 2, 35, 16, 4090), (8, 4, 35, 16, 2040), (4, 8, 35, 16, 1020), (16, 1, 1, 600, 31)])
+                                       (16, 2, 35, 16, 4090), (8, 4, 35, 16, 2040), (4, 8, 35, 16, 1020), (16, 1, 1, 600, 31),
+                                       (2, 8, 35, 16, 4500), (4, 4, 35, 16, 8300)])
 def test_weigh_many_heads(lk, m, g, B, H, L):  # noqa: F811
     """Small workgroups, short code and long: lengths from none to the row's room, pages outside the pool, tables that are not finite."""
     rng = np.random.default_rng(L + m)
