@@ -7,14 +7,14 @@
 //   * S^T = K^ Q^T: a wavefront owns 32 rows (columns of S^T).  Centroids enter as two fp16 terms of 2^s w (22 bits; s one power of two per
 //     head, which brings the head's largest centroid entry to 2^14), fp16 queries exactly, fp32 queries as two terms of their own power of
 //     two (the product of the two small terms, 2^-22, is dropped).
-//   * a lane then holds 32 scores of ONE row: running reference and sum need no exchange but with the lane that holds the row's other keys.
+//   * a lane then holds 16 or 32 scores of ONE row: running reference and sum need no exchange but with the lane that holds the row's other keys.
 //     Reference and page exponents as in attention of one token: y = scale log2(e) s + e, w = 2^(y - R).
 //   * O^T = V^T P^T: keys are dealt to the rows of K^ (bits 2 and 3 of a row's number exchanged) such that the eight weights that a lane holds
 //     of an operand belong to eight consecutive tokens: the weights, as two fp16 terms, are the operand where they are, and the values' operand
 //     is eight consecutive stored bytes, as the page holds them.
-// The centroids are split once per call by a small kernel, into the workspace (or by every workgroup, see below).  A workgroup of NW wavefronts (32 NW rows of one key/value head,
-// query heads of a group side by side) fetches the centroids of 64 keys by code into LDS, two buffers of 64 keys in turn; their ids, codes and
-// centroids are requested three, two and one tiles ahead.
+// The centroids are split once per call by a small kernel, into the workspace (or by every workgroup, see below).  A workgroup of NW wavefronts (32 NW
+// rows of one key/value head, query heads of a group side by side) fetches the centroids of KEYS keys by code into LDS, two buffers of as many keys in
+// turn; their ids, codes and centroids are requested three, two and one tiles ahead.
 #include "pages_values.h"
 
 namespace lookat {
@@ -191,13 +191,14 @@ template <int DK, bool SMALL, bool Q32, bool FP8, int NW, int KEYS>
 __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs p, ChunkArgs a)
 {
     constexpr int threads = NW * kWave, CH = DK / 8, STEPS = DK / 16, CB = DK / 32, TQ = 32 * NW;
-    constexpr int TPK = threads / KEYS, CPT = CH / TPK, KB = KEYS / 32, GROUPS = KEYS / 16;                                 // 8-coordinate pieces of a key that a thread fetches
+    constexpr int TPK = threads / KEYS, CPT = CH / TPK;          // threads of a key, 8-coordinate pieces that each of them fetches
+    constexpr int KB = KEYS / 32, GROUPS = KEYS / 16;            // blocks of a product, groups of tokens that lie in one page
     constexpr int kPlane = KEYS * DK * 2, kBuffer = 2 * kPlane, kValues = KEYS * DK * 2;
     constexpr int kItems = KEYS / 8 * DK / 2, VPT = (kItems + threads - 1) / threads;    // two coordinates of eight tokens: 16 stored bytes
     static_assert(CH % TPK == 0, "whole pieces for every thread");
     __shared__ __align__(16) char keys_s[2 * kBuffer];           // [buffer][term][key][coordinate]
     __shared__ __align__(16) char values_s[2 * kValues];         // [buffer][octet][coordinate][token]
-    __shared__ int ids_s[4][GROUPS], exps_s[4][GROUPS];                    // of 16 tokens, by tile modulo 4
+    __shared__ int ids_s[4][GROUPS], exps_s[4][GROUPS];          // of 16 tokens, by tile modulo 4
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
     const Place at_work = place_of(a);
     if (!at_work.any)
