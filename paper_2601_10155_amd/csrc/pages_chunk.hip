@@ -1021,10 +1021,14 @@ static int launch_chunk(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp
     hipLaunchKernelGGL(f, dim3(groups), dim3(NW * kWave), 0, st, p, a);
     return check_launch("lookat_attend_pages_chunk");
 }
+// Whether two wavefronts take two blocks of rows.
+constexpr bool two_brief_blocks(int d_k, bool q32) { return d_k == 64 || !q32; }
+
 template <int DK, bool SMALL, int RB, int WAVES>
 static int launch_few(const PoolArgs &p, const ChunkArgs &a, bool q32, bool fp8, unsigned groups, hipStream_t st)
 {
-    const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, true, false, RB, WAVES>)
+    constexpr int R32 = RB == 2 && WAVES == kBriefWaves && !two_brief_blocks(DK, true) ? 1 : RB;
+    const auto f = q32 ? (fp8 ? &chunk_few_kernel<DK, SMALL, true, true, R32, WAVES> : &chunk_few_kernel<DK, SMALL, true, false, R32, WAVES>)
                        : (fp8 ? &chunk_few_kernel<DK, SMALL, false, true, RB, WAVES> : &chunk_few_kernel<DK, SMALL, false, false, RB, WAVES>);
     constexpr size_t results = few_lds_bytes(DK, WAVES), book = few_staged(WAVES) ? (size_t)kCentroids * DK * 4 : 0, lds = results > book ? results : book;
     if (lds > 60 * 1024) {
@@ -1087,12 +1091,21 @@ extern "C" int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B
         return fail(LOOKAT_ERR_ALIGN, "q, its strides, codebooks and out must be 16-byte aligned");
     if ((reinterpret_cast<uintptr_t>(lengths) | reinterpret_cast<uintptr_t>(counts)) & 3u)
         return fail(LOOKAT_ERR_ALIGN, "lengths and counts must be 4-byte aligned");
-    const ChunkCut cut = chunk_cut(pool, B, N, group, W, max_length, num_splits);
+    ChunkCut cut = chunk_cut(pool, B, N, group, W, max_length, num_splits);
     const size_t need = cut.books + cut.unscale + cut.part;
     if (!workspace || workspace_bytes < need)
         return fail(LOOKAT_ERR_WORKSPACE, "workspace of %zu bytes needed, got %zu", need, workspace ? workspace_bytes : (size_t)0);
     if (!aligned16(workspace))
         return fail(LOOKAT_ERR_ALIGN, "workspace must be 16-byte aligned");
+    // fp32 rows at d_k = 128 in two wavefronts: one block of 16 rows, of two the registers do not hold both terms beside the accumulators and
+    // operands (33 to 35 were spilled; us a call, two / one, 400 x 20 rows x 70 tokens 22.1 / 16.5, 1280 x 20 x 320 74 / 59, 1280 x 32 x 432
+    // 94 / 85, 768 x 24 x 124 31.1 / 33.1).  Partial rows take no more room: as many ranges, and ceil(rows / 16) * 16 <= ceil(rows / 32) * 32.
+    if (cut.few == 2 && cut.waves == kBriefWaves && !two_brief_blocks(pool->d_k, q_dtype == LOOKAT_F32)) {
+        cut.few = 1;
+        cut.rows = 16;
+        cut.tiles = (int)(((int64_t)N * group + cut.rows - 1) / cut.rows);
+        cut.work = (int64_t)B * pool->H * cut.tiles * cut.splits;
+    }
     const int64_t all_units = (int64_t)B * pool->H, per_unit = (int64_t)cut.tiles * cut.splits, whole = all_units / kXcds * per_unit;
     const int64_t left = all_units % kXcds * per_unit, per_die = (left + kXcds - 1) / kXcds, groups = (whole + per_die) * kXcds;
     if (!fits_launch(groups, cut.waves * kWave))
