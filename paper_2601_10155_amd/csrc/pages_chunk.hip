@@ -184,6 +184,32 @@ __device__ __forceinline__ uint32_t left_of(float w0, float w1, uint32_t h)
     return r;
 }
 
+// A stored NaN (e4m3 alone has one) belongs to the rows that see its token; for the others it would be multiplied by a weight of zero.  So in the
+// tiles whose tokens not all rows see zeros take the NaNs' places, and where there was one, what the rows that see it have is made NaN behind the
+// results' stores: without a NaN those tiles alone have a few instructions more.
+// Zeros in the places of NaNs (0x7f, 0xff); `any` is not zero if there was one.
+__device__ __forceinline__ void drop_nans(v4u &x, uint32_t &any)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t n = ((x[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+        x[k] &= ~((n << 1) - (n >> 7));
+        any |= n;
+    }
+}
+// Whether one of the tokens [first, last) has a NaN at coordinate d.
+template <int DK>
+__device__ __forceinline__ bool sees_nan(const uint8_t *head_values, uint32_t value_step, const int32_t *row, int pages, int page_log2, int first, int last, int d)
+{
+#pragma unroll 1
+    for (int l = first; l < last; ++l) {
+        const int id = row[l >> page_log2], t = l & ((1 << page_log2) - 1);
+        if ((uint32_t)id < (uint32_t)pages && (head_values[(uint64_t)(uint32_t)id * value_step + (uint32_t)((t & ~7) * DK + d * 8 + (t & 7))] & 0x7f) == 0x7f)
+            return true;
+    }
+    return false;
+}
+
 // Wavefronts to a SIMD that the registers have to allow.
 constexpr int kChunkWaves = 2;
 
@@ -199,6 +225,7 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
     __shared__ __align__(16) char keys_s[2 * kBuffer];           // [buffer][term][key][coordinate]
     __shared__ __align__(16) char values_s[2 * kValues];         // [buffer][octet][coordinate][token]
     __shared__ int ids_s[4][GROUPS], exps_s[4][GROUPS];          // of 16 tokens, by tile modulo 4
+    __shared__ int nan_s;                                        // whether drop_nans found one
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, half = lane >> 5, col = lane & 31;
     const Place at_work = place_of(a);
     if (!at_work.any)
@@ -319,13 +346,17 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
             const int item = tid + j * threads;
             if (kItems % threads == 0 || item < kItems) {
                 if constexpr (FP8) {
-                    // bytes without a token behind them may be NaN: zeros in their place
-                    if ((t + 1) * KEYS > range.end) {
+                    // bytes without a token behind them, which may be NaN, and NaNs that not all rows see: zeros in their place
+                    if ((t + 1) * KEYS > seen_by_all) {
                         const int m = range.end - t * KEYS - 8 * (item / (DK / 2));
                         const uint32_t lo = m >= 4 ? ~0u : m <= 0 ? 0u : (1u << (8 * m)) - 1;
                         const uint32_t hi = m >= 8 ? ~0u : m <= 4 ? 0u : (1u << (8 * (m - 4))) - 1;
                         stored[j].x &= lo, stored[j].y &= hi;
                         stored[j].z &= lo, stored[j].w &= hi;
+                        uint32_t any = 0;
+                        drop_nans(stored[j], any);
+                        if (any)
+                            nan_s = 1;
                     }
                     if (ids_s[t & 3][item / (DK / 2) >> 1] < 0)
                         stored[j] = (v4u){0, 0, 0, 0};
@@ -408,6 +439,8 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
     // Two tiles of keys and one of values are staged, the scores of the first are there before the loop.  (What can be requested together is: page
     // ids, then the codes of three tiles and the values, then the centroids of two.)
     put_page(range.t0, page_of(range.t0, id0), 0);
+    if (FP8 && tid == 0)
+        nan_s = 0;
     __syncthreads();
     load_values(range.t0);
     {
@@ -521,26 +554,36 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
     float u, w;
     lanes_xor32(z, u, w);
     z = u + w;
-    if (!mine)
-        return;
-    float f = 1.f;
-    float *to;
-    if (range.ranges == 1) {
-        f = z == 0.f ? 0.f : 1.f / z;     // (nothing to sum: zeros; a sum that is NaN stays one)
-        to = a.out + ((int64_t)(b * p.H * a.group + hq) * a.N + n) * DK;
-    } else {
-        to = a.part + (((int64_t)unit * a.tiles + tile) * a.splits + split) * TQ * (DK + kPartPad) + (wave * 32 + col) * (DK + kPartPad);
-        if (half == 0)
-            *reinterpret_cast<float2 *>(to + DK) = make_float2(ref, z);
-    }
-    // register i of acc[c] is coordinate 32 c + i % 4 + 8 (i / 4) + 4 half
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const v4f o = {acc[c][i] * f, acc[c][i + 1] * f, acc[c][i + 2] * f, acc[c][i + 3] * f};
-            *reinterpret_cast<v4f *>(to + 32 * c + 2 * i + 4 * half) = o;
+    if (mine) {
+        float f = 1.f;
+        float *to;
+        if (range.ranges == 1) {
+            f = z == 0.f ? 0.f : 1.f / z;     // (nothing to sum: zeros; a sum that is NaN stays one)
+            to = a.out + ((int64_t)(b * p.H * a.group + hq) * a.N + n) * DK;
+        } else {
+            to = a.part + (((int64_t)unit * a.tiles + tile) * a.splits + split) * TQ * (DK + kPartPad) + (wave * 32 + col) * (DK + kPartPad);
+            if (half == 0)
+                *reinterpret_cast<float2 *>(to + DK) = make_float2(ref, z);
         }
+        // register i of acc[c] is coordinate 32 c + i % 4 + 8 (i / 4) + 4 half
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const v4f o = {acc[c][i] * f, acc[c][i + 1] * f, acc[c][i + 2] * f, acc[c][i + 3] * f};
+                *reinterpret_cast<v4f *>(to + 32 * c + 2 * i + 4 * half) = o;
+            }
+        if constexpr (FP8)
+            if (nan_s) {
+                const int first = (seen_by_all / KEYS > range.t0 ? seen_by_all / KEYS : range.t0) * KEYS, last = seen < range.t1 * KEYS ? seen : range.t1 * KEYS;
+#pragma unroll 1
+                for (int i = 0; i < DK / 2; ++i) {
+                    const int d = 8 * (i / 4) + 4 * half + i % 4;
+                    if (sees_nan<DK>(head_values, value_step, row, p.pages, p.page_log2, first, last, d))
+                        to[d] = NAN;
+                }
+            }
+    }
 }
 
 // Few rows (drafted tokens, the ends of prompts), and few heads: 16 RB rows of a (sequence, head) to a workgroup, whose wavefronts take tiles of 32 tokens in
@@ -559,6 +602,7 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
     constexpr bool STAGED = few_staged(WAVES);
     constexpr int STEPS = DK / 32, CB = DK / 32, TQ = 16 * RB, ROW = DK + 4;
     __shared__ float tops_s[STAGED ? WAVES : 1];
+    __shared__ int nans_s[WAVES];         // whether drop_nans found one
     extern __shared__ __align__(16) char few_s[];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, quad = lane >> 4, col = lane & 15;
     const Place at = place_of(a);
@@ -728,6 +772,7 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
         for (int c = 0; c < CB; ++c)
             acc[j][c][0] = acc[j][c][1] = (v4f){0.f, 0.f, 0.f, 0.f};
     }
+    int nans = 0;                         // whether drop_nans found one in a tile of this wavefront
     if (t < range.t1) {
         load_codes(t, id_k0);
         if constexpr (!STAGED) {
@@ -807,6 +852,14 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
                     v[c].x &= lo, v[c].y &= hi;
                     v[c].z &= lo, v[c].w &= hi;
                 }
+                // and NaNs that not all rows see
+                if ((t + 1) * kFewKeys > seen_by_all) {
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int c = 0; c < CB; ++c)
+                        drop_nans(v[c], any);
+                    nans |= __builtin_amdgcn_ballot_w64(any != 0) != 0;
+                }
             }
         }
         const float unexp = power_of_two(-(int)e);
@@ -868,6 +921,7 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
     float2 *stats = reinterpret_cast<float2 *>(few_s + (size_t)WAVES * 16 * ROW * 4);
     if constexpr (STAGED)
         __syncthreads();                  // (the centroids were read)
+    int any = 0;
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
         float u, w;
@@ -875,7 +929,15 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
         lanes_xor32(u + w, u, w);
         if (quad == 0)
             stats[wave * 16 + col] = make_float2(ref[j], u + w);
+        if (FP8 && j == 0 && lane == 0)
+            nans_s[wave] = nans;
         __syncthreads();
+        if (FP8 && j == 0) {
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k)
+                any |= nans_s[k];
+            any = __builtin_amdgcn_readfirstlane(any);
+        }
         float top = kNoReference;
 #pragma unroll
         for (int k = 0; k < WAVES; ++k)
@@ -917,6 +979,23 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
         }
         if (j + 1 < RB)
             __syncthreads();
+    }
+    if constexpr (FP8) {
+        if (any) {
+            __syncthreads();              // (the results were stored)
+            const int first = (seen_by_all / kFewKeys > range.t0 ? seen_by_all / kFewKeys : range.t0) * kFewKeys, end = range.t1 * kFewKeys;
+#pragma unroll 1
+            for (int item = tid; item < TQ * DK; item += WAVES * kWave) {
+                const int r = r0 + item / DK, n = r / a.group, hq = h * a.group + r - n * a.group, d = item % DK;
+                if (n >= span.count)
+                    continue;
+                const int seen = seen_of(span, n);
+                float *to = range.ranges == 1 ? a.out + ((int64_t)(b * p.H * a.group + hq) * a.N + n) * DK
+                                              : a.part + ((((int64_t)at.unit * a.tiles + tile) * a.splits + split) * TQ + item / DK) * (DK + kPartPad);
+                if (sees_nan<DK>(head_values, value_step, row, p.pages, p.page_log2, first, seen < end ? seen : end, d))
+                    to[d] = NAN;
+            }
+        }
     }
 }
 

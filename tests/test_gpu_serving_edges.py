@@ -1,0 +1,83 @@
+"""Chunks, eviction and beam selection at the ends of what their documentation allows."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_pages import i32, lk  # noqa: F401
+from test_gpu_pages_chunk import U
+
+pytestmark = pytest.mark.gpu
+
+# sizes of chunks that take every kernel: B, H, g, N, before, d_k, m, page, num_splits
+CHUNKS = [
+    (2, 43, 1, 770, 1400, 128, 8, 32, 0),     # 256 rows to a workgroup
+    (8, 32, 1, 260, 150, 128, 8, 32, 0),      # 128 rows
+    (10, 10, 2, 128, 100, 128, 2, 64, 0),
+    (6, 20, 2, 150, 100, 64, 8, 32, 0),
+    (8, 32, 1, 260, 0, 64, 16, 16, 0),        # ... with centroids of four coordinates
+    (6, 2, 4, 100, 900, 128, 2, 64, 0),       # few rows or heads: eight wavefronts, two blocks of rows
+    (5, 20, 3, 7, 333, 64, 16, 16, 0),
+    (8, 3, 2, 8, 200, 64, 8, 64, 0),          # ... one
+    (40, 16, 4, 4, 60, 64, 4, 64, 0),         # two wavefronts, one block
+    (40, 16, 5, 6, 100, 128, 4, 128, 0),      # ... two
+    (40, 16, 1, 50, 20, 64, 16, 16, 0),
+    (6, 20, 2, 150, 200, 64, 8, 32, 3),       # in ranges
+    (8, 32, 1, 260, 400, 128, 8, 32, 2),
+    (2, 3, 8, 16, 1000, 64, 8, 64, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page,splits", CHUNKS)
+def test_a_stored_nan_reaches_the_rows_that_see_its_token(lk, B, H, g, N, before, d_k, m, page, splits, dtype):  # noqa: F811
+    """e4m3 has a NaN.  The coordinate that holds one is NaN in the rows from its token's position on, and no other output is touched: the
+    bound is that of test_gpu_pages_chunk's `against_torch`, with zeros in the NaNs' places."""
+    gen = torch.Generator(device="cuda").manual_seed(B + N + d_k)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    lengths = [max(1, N + before - 3 * b) for b in range(B)]
+    counts = [max(1, N - 2 * b) for b in range(B)]
+    W = -(-max(lengths) // page)
+    P = B * W
+    stored = (rnd(P, H, page // 8, d_k, 8) * 30).to(torch.float8_e4m3fn).view(torch.uint8)
+    table = torch.randperm(P, generator=gen, device="cuda").to(torch.int32).view(B, W)
+    for b in range(B):
+        n, k = lengths[b], counts[b]
+        # (the last token, the first of the chunk, some between, and one that all rows see)
+        for x, t in enumerate(sorted({max(0, n - x) for x in (1, k, 1 + k // 3, 1 + k // 2, k + 40)})):
+            stored[table[b, t // page].long(), (3 * b + x) % H, t % page // 8, (17 * b + 5 * x) % d_k, t % 8] = 0x7f if x % 2 else 0xff
+        if n < W * page:                              # (and bytes that no row sees)
+            stored[table[b, n // page].long(), :, n % page // 8, :, n % 8] = 0x7f
+    pool = lk.PagePool(torch.randint(0, 256, (P, H, page, m), generator=gen, device="cuda", dtype=torch.uint8), stored.view(torch.float8_e4m3fn),
+                       torch.randint(-8, -2, (P, H), generator=gen, device="cuda").to(torch.int8))
+    books = rnd(H, m, 256, d_k // m)
+    q = rnd(B, H * g, N, d_k).to(getattr(torch, dtype))
+    scale = 1 / math.sqrt(d_k)
+    got = lk.lookat_attend_pages_chunk(q, books, pool, table, i32(*lengths), scale, counts=i32(*counts), num_splits=splits)
+    head, sub = torch.arange(H, device="cuda")[:, None, None], torch.arange(m, device="cuda")
+    reached = 0
+    for b in range(B):
+        n, k, ids = lengths[b], counts[b], table[b].long()
+        code = pool.codes[ids].permute(1, 0, 2, 3).reshape(H, -1, m)[:, :n].long()
+        key = books.double()[head, sub, code].reshape(H, n, d_k)
+        val = pool.values[ids].double() * torch.exp2(pool.exponents[ids].double())[..., None, None, None]
+        val = val.permute(1, 0, 2, 4, 3).reshape(H, -1, d_k)[:, :n]
+        nan, val = val.isnan(), val.nan_to_num(0.0)
+        x = q[b, :, :k].double().reshape(H, g * k, d_k)
+        y = torch.matmul(x, key.transpose(1, 2).contiguous()).view(H, g, k, n) * scale
+        size = torch.matmul(x.abs(), key.abs().transpose(1, 2).contiguous()).amax(-1).view(H, g, k, 1) * scale * 1.4427
+        seen = torch.arange(n, device="cuda") <= n - k + torch.arange(k, device="cuda")[:, None]
+        p = torch.softmax(y.masked_fill(~seen, -math.inf), -1)
+        p = torch.where(seen.any(-1, keepdim=True), p, 0.0)
+        want = torch.matmul(p.view(H, g * k, n), val).view(H, g, k, d_k)
+        want = want.masked_fill((torch.matmul(seen.double(), nan.double()) > 0).view(H, 1, k, d_k), math.nan).view(H * g, k, d_k)
+        d = (3 * 2.0 ** -22 + (d_k + 3) * U) * size + 6 * U * (size + 64) \
+            + d_k * 2.0 ** -38 * x.abs().amax(-1).view(H, g, k, 1) * books.abs().amax().double() * scale * 1.4427
+        rel = 2 * (d * 0.6932 + 2.0 ** -21) + 4 * math.sqrt(n + 64) * U
+        floor = 1.01 * 2.0 ** (-3 - 32) * 448 * n
+        bound = (rel * torch.matmul(p.view(H, g * k, n), val.abs()).view(H, g, k, d_k)).reshape(H * g, k, d_k) + floor
+        mine = got[b, :, :k].double()
+        assert torch.equal(mine.isnan(), want.isnan()), (b, int((mine.isnan() != want.isnan()).sum()))
+        assert bool(((mine - want).abs() <= bound)[~want.isnan()].all()), b
+        assert not got[b, :, k:].any()
+        reached += int(want.isnan().sum())
+    assert reached
