@@ -404,11 +404,12 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
                 ql[s][e] = (_Float16)(w - (float)qh[s][e]);
             }
     }
-    // A negative scale turns the rows around, and a scale of zero becomes fp32's least, so that a score of -inf stays one.
-    if (a.scale_log2e < 0.f) {
+    // A negative scale turns the rows around, one of NaN makes their scores NaN (fmaxf would pass over it), and a scale of zero becomes fp32's
+    // least, so that a score of -inf stays one.
+    if (!(a.scale_log2e >= 0.f)) {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            qh[s] = -qh[s];
+            qh[s] = a.scale_log2e < 0.f ? -qh[s] : qh[s] * (_Float16)NAN;
             if constexpr (Q32)
                 ql[s] = -ql[s];
         }
@@ -750,11 +751,12 @@ __global__ __launch_bounds__(WAVES *kWave, 2) void chunk_few_kernel(PoolArgs p, 
                     ql[j][s][e] = (_Float16)(w - (float)qh[j][s][e]);
                 }
         }
-        // A negative scale turns the rows around, and a scale of zero becomes fp32's least, so that a score of -inf stays one.
-        if (a.scale_log2e < 0.f) {
+        // A negative scale turns the rows around, one of NaN makes their scores NaN (fmaxf would pass over it), and a scale of zero becomes fp32's
+        // least, so that a score of -inf stays one.
+        if (!(a.scale_log2e >= 0.f)) {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                qh[j][s] = -qh[j][s];
+                qh[j][s] = a.scale_log2e < 0.f ? -qh[j][s] : qh[j][s] * (_Float16)NAN;
                 if constexpr (Q32)
                     ql[j][s] = -ql[j][s];
             }

@@ -1,10 +1,11 @@
 """Chunks, eviction and beam selection at the ends of what their documentation allows."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_pages import i32, lk  # noqa: F401
+from test_gpu_pages import dev, i32, lk, on_gpu, random_cache  # noqa: F401
 from test_gpu_pages_chunk import U
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +82,26 @@ def test_a_stored_nan_reaches_the_rows_that_see_its_token(lk, B, H, g, N, before
         assert not got[b, :, k:].any()
         reached += int(want.isnan().sum())
     assert reached
+
+
+@pytest.mark.parametrize("kind", ["int8", "float8"])
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("B,H,g,N,before,d_k,m,page,splits", [CHUNKS[i] for i in (1, 3, 5, 7, 8, 11)])
+def test_a_scale_of_nan(lk, B, H, g, N, before, d_k, m, page, splits, dtype, kind):  # noqa: F811
+    """Every row that sees a token is NaN, as attention of one token is; a row that sees none gives zeros."""
+    rng = np.random.default_rng(N)
+    lengths = [N + before - b for b in range(B)]
+    lengths[0] = 3                                    # (its first rows stand before its first token)
+    W = -(-max(lengths) // page)
+    c = random_cache(rng, W, H, d_k, m, page, kind)
+    pool, table = on_gpu(lk, c), dev(np.tile(rng.permutation(W).astype(np.int32), (B, 1)))
+    books = dev(rng.standard_normal((H, m, 256, d_k // m)).astype(np.float32))
+    q = dev(rng.standard_normal((B, H * g, N, d_k)).astype(dtype))
+    got = lk.lookat_attend_pages_chunk(q, books, pool, table, i32(*lengths), math.nan, num_splits=splits)
+    sees = i32(*lengths)[:, None] - N + torch.arange(N, device="cuda") >= 0
+    assert torch.equal(got.isnan(), sees[:, None, :, None].expand(got.shape))
+    assert not got.nan_to_num(0.0).any()
+    if g in (1, 2, 4, 8):
+        lut = dev(rng.standard_normal((B, H * g, m, 256)).astype(np.float32))
+        one = lk.lookat_attend_pages(lut, pool, table, i32(*[0, *lengths[1:]]), math.nan)
+        assert bool(one[1:].isnan().all()) and not one[0].any()
