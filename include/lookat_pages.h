@@ -115,11 +115,12 @@ int lookat_attend_pages(const lookat_page_pool *pool, int32_t B, int32_t group,
  *     s[b,hq,n,l]   = sum_j q[b,hq,n,j] * k^(b, hq/group, l)_j
  *     out[b,hq,n,:] = sum_{l <= p} softmax_l(scale * s[b,hq,n,:]) * value(b, hq/group, l, :)
  * A row that sees no token gives zeros, and so does one whose tokens all have a score of -inf; other rows of out are left as they were.  A NaN
- * score or one of +inf makes its row NaN; other rows are not touched by it.  A scale of NaN makes every row NaN that sees a token, a stored NaN (E4M3) its
- * coordinate in the rows that see its token.  Centroids enter the product as two fp16 terms, scaled by one power
- * of two per key/value head: exactly to 2^-22 of themselves, or to 2^-40 of the head's largest finite centroid entry where that is more; fp16
- * queries exactly, fp32 queries to 2^-22 of themselves or 2^-40 of the row's largest entry; weights, sums and values as in lookat_attend_pages.  An
- * infinite centroid entry makes the scores of the tokens that have it NaN; what centroids hold that no token has does not matter.
+ * score or one of +inf makes its row NaN; other rows are not touched by it.  A scale of NaN makes every row NaN that sees a token, a stored NaN (E4M3)
+ * its coordinate in the rows that see its token.
+ * Centroids enter the product as two fp16 terms, scaled by one power of two per key/value head: exactly to 2^-22 of themselves, or to 2^-39 of the
+ * head's largest finite centroid entry where that is more (whether a token has that centroid or not: one of 1e30 leaves nothing of others of 1);
+ * fp16 queries exactly, fp32 queries to 2^-22 of themselves or 2^-39 of the row's largest entry; weights, sums and values as in
+ * lookat_attend_pages.  An infinite centroid entry makes the scores of the tokens that have it NaN; centroids that no token has may be NaN or infinite.
  *   q             [B, H*group, N, d_k] fp16 or fp32: element (b,hq,n,j) at q[b*q_stride_b + hq*q_stride_h + n*q_stride_n + j]; base 16-byte
  *                 aligned, strides multiples of 8 (fp16) or 4 (fp32) elements
  *   codebooks     [H, m, 256, d_k/m] fp32, 16-byte aligned
