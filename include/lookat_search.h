@@ -16,11 +16,13 @@ extern "C" {
  * The n best continuations of each of Q requests.  Rows q*beams .. q*beams + beams - 1 of logits are the beams of request q, scores their
  * log-probabilities so far; token v of row r makes
  *     scores[r] + logits[r,v] - log sum_u exp(logits[r,u])
- * Candidates of a request are ordered by that, falling, equal ones by (row, token), rising; the first n are written.  Rows are ordered as their
- * logits are whatever the rounding of the sum (candidates are compared in 64 bits, with the row's sum to fp32's precision; the score that is written is
- * rounded to fp32 once, below its range to its lowest number).  A logit of -inf is a token that cannot be chosen, a score of -inf a beam that has none (one that ended; all but the first
- * of a request that begins).  A row that has a NaN or +inf among its logits, or whose score is NaN or +inf, gives no candidate either.  Where a
- * request has fewer than n candidates the rest is -inf, -1, -1.
+ * Candidates of a request are ordered by that, falling, equal ones by (row, token), rising; the first n are written.  A row's candidates are ordered
+ * as its logits are whatever the rounding of the sum.  Candidates are compared in 64 bits; the log of a row's sum is good to 2^-18 (to 5.4e-7 in
+ * what was measured: rows with most of their weight in equal logits far below the maximum), so that two beams' candidates whose scores lie closer
+ * than 2^-17 may change places.  The score that is written is rounded to fp32 once, below its range to its lowest number.
+ * A logit of -inf is a token that cannot be chosen, a score of -inf a beam that has none (one that ended; all but the first of a request that
+ * begins).  A row that has a NaN or +inf among its logits, or whose score is NaN or +inf, gives no candidate either.  Where a request has fewer than n
+ * candidates the rest is -inf, -1, -1.
  *   logits        fp16 or fp32, element (r,v) at logits[r*logit_stride + v], logit_stride >= V; any alignment of its type
  *   scores        [Q*beams] fp32
  *   scores_out    [Q,n] fp32;  tokens [Q,n] int32;  parents [Q,n] int32: first_parent + r, what lookat_pages_fork takes as sources if the beams'

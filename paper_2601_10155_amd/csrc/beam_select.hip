@@ -4,7 +4,11 @@
 // the sum of exp(x - m).  A lower bound on the n-th best is the n-th largest of the lanes' maxima (found bit by bit with ballots); few logits reach
 // it, and one lane takes each and counts those ahead of it.  Where more than 64 reach it (large n) the n-th best itself is found bit by bit
 // among them, first its value, then among equal ones its place; where more than kListed do (many equal logits), among all.  Listed logits near m
-// enter the sum in 64 bits, so that the terms that dominate a row's sum carry no fp32 rounding; the others' roundings average out.
+// enter the sum in 64 bits, so that the terms that dominate a peaked row's sum carry no fp32 rounding.  The others are off by |d| u for the
+// difference d = x - m, 1.25 |d| u for its product with log2(e) and 2 u for the exponential, u = 2^-24, and their sum over a lane, by pairs, by 16 u at
+// most.  In a row of many equal logits all of that may go one way: 50 u = 2^-18.4 at d = -14, and with up to 2^24 logits no d gives more; 5.4e-7 was
+// the most in 250 thousand such rows.  (The sum one term after the other: 9.3e-7, and 64 x 8 x 131072 56.5 us a call, so 57.0; the product's rounding carried
+// along: 64.8.)
 // In the second launch a workgroup takes a request.  A lower bound on the n-th best score, found as above from a few entries of every sorted list,
 // leaves few candidates, whose places are counted.  Where more than kMostFound reach the bound (many equal scores) each wavefront takes the n best of its
 // share of the lists one by one, and those are merged by counting.
@@ -67,6 +71,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
 {
     constexpr int PER = 16 / (int)sizeof(FT), LOADS = E / PER;     // a load's logits
     static_assert(kWave * E <= 1 << kPlaceBits, "a logit's number fits its bits");
+    constexpr int kPairLevels = E == 16 ? 4 : 5;
+    static_assert(E == 1 << kPairLevels, "whole pairs");
     __shared__ uint64_t lists[kSelectWaves][kListed];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t item = (int64_t)blockIdx.x * kSelectWaves + wave;
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
     float rest = 0.f;
     auto sweep = [&](auto all, float at_least, int most) {
         found = 0;
-        rest = 0.f;
+        float pairs[kPairLevels + 1];     // sums of 2^level terms
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             const bool reaches = x[j] >= at_least;
@@ -140,8 +146,14 @@ __global__ __launch_bounds__(kSelectThreads) void select_rows_kernel(SelectArgs 
                 found += __builtin_popcountll(mask);
             }
             const float e = fast_exp2((x[j] - base) * kLog2eF);
-            rest += reaches ? 0.f : e;
+            float sum = reaches ? 0.f : e;
+            int level = 0;
+#pragma unroll
+            for (; j >> level & 1; ++level)
+                sum += pairs[level];
+            pairs[level] = sum;
         }
+        rest = pairs[kPairLevels];
     };
     sweep(std::true_type(), border, 0);
     float ties = 0.f;                     // logits at the border that are not listed

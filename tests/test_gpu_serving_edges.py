@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from bars import record
 from test_gpu_pages import dev, i32, lk, on_gpu, random_cache  # noqa: F401
 from test_gpu_pages_chunk import U
 
@@ -105,3 +106,24 @@ def test_a_scale_of_nan(lk, B, H, g, N, before, d_k, m, page, splits, dtype, kin
         lut = dev(rng.standard_normal((B, H * g, m, 256)).astype(np.float32))
         one = lk.lookat_attend_pages(lut, pool, table, i32(*[0, *lengths[1:]]), math.nan)
         assert bool(one[1:].isnan().all()) and not one[0].any()
+
+
+SUM = 2.0 ** -18       # of a row's sum of exponentials (include/lookat_search.h); a score is off by as much, and by its own rounding
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("V", [20000, 131072])
+def test_peaks_above_many_equal_logits(lk, V, dtype):  # noqa: F811
+    """Every term's rounding goes the same way.  Terms e^d beside peaks of 1: with u = 2^-24 a term is off by |d| u for the difference, |d| (u + u / 4) for its product
+    with log2(e), 2 u for the exponential, and the sum of a lane's terms by 16 u; for d > -14 that is 50 u < 2^-18."""
+    top = 0.0
+    for base in np.arange(-9, 12, 0.37):
+        d = -torch.linspace(0.05, 14, 160, device="cuda", dtype=torch.float64)
+        x = (base + d[:, None]).expand(160, V).to(getattr(torch, dtype)).contiguous()
+        x[:, ::2048] = float(base)
+        want = x[:, 0].double() - torch.logsumexp(x.double(), -1)
+        s = lk.lookat_beam_select(x, torch.zeros(160, device="cuda"), 1, 1)[0][:, 0].double()
+        off = (s - want).abs() - 2.0 ** -24 * want.abs()
+        top = max(top, float(off.max()))
+    record(f"log-sum of a peaked row, {V} {dtype}", top)
+    assert top <= SUM
