@@ -6,8 +6,9 @@ import pytest
 import torch
 
 from bars import record
-from test_gpu_pages import dev, i32, lk, on_gpu, random_cache  # noqa: F401
+from test_gpu_pages import assert_pool, dev, i32, lk, on_gpu, random_cache  # noqa: F401
 from test_gpu_pages_chunk import U
+from test_gpu_pages_keep import evict_reference, spread_weights
 
 pytestmark = pytest.mark.gpu
 
@@ -26,7 +27,12 @@ CHUNKS = [
     (40, 16, 1, 50, 20, 64, 16, 16, 0),
     (6, 20, 2, 150, 200, 64, 8, 32, 3),       # in ranges
     (8, 32, 1, 260, 400, 128, 8, 32, 2),
-    (2, 3, 8, 16, 1000, 64, 8, 64, 4)]
+    (2, 3, 8, 16, 1000, 64, 8, 64, 4),
+    (8, 3, 2, 8, 200, 128, 8, 64, 0),         # one block of rows at d_k = 128, eight wavefronts and two
+    (40, 16, 4, 4, 60, 128, 16, 64, 0),
+    (40, 16, 1, 50, 20, 64, 8, 32, 0),        # two wavefronts, two blocks, centroids of eight coordinates
+    (8, 3, 2, 8, 200, 64, 16, 64, 0),         # one block, centroids of four, eight wavefronts and two
+    (40, 16, 4, 4, 60, 64, 16, 64, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["float16", "float32"])
@@ -127,3 +133,90 @@ def test_peaks_above_many_equal_logits(lk, V, dtype):  # noqa: F811
         top = max(top, float(off.max()))
     record(f"log-sum of a peaked row, {V} {dtype}", top)
     assert top <= SUM
+
+
+@pytest.mark.parametrize("room,n", [(5000, 4900), (8192, 8192), (8193, 8193), (20000, 20000), (32768, 32768), (32768, 700), (32769, 30000)])
+@pytest.mark.parametrize("page,kind", [(16, "int8"), (128, "float8")])
+def test_the_choice_of_long_evictions(lk, room, n, page, kind):  # noqa: F811
+    """Weights of 8 and of 32 tokens a thread in registers, and read again: many equal weights on both sides of the border, NaN, lengths far below a row's room."""
+    rng = np.random.default_rng(room + n)
+    H, B = 3, 2
+    W = -(-room // page)
+    lengths, keep = [n, n // 3], [n // 4 + 1, n // 10]
+    W_out = -(-max(keep) // page)
+    held = [-(-x // page) for x in lengths]
+    P = sum(held) + B * W_out
+    c = random_cache(rng, P, H, 64, 4, page, kind, -5, -2)
+    ids = rng.permutation(P).astype(np.int32)
+    table = np.full((B, W), -1, np.int32)
+    table[0, :held[0]], table[1, :held[1]] = ids[:held[0]], ids[held[0]: sum(held)]
+    table_out = ids[sum(held):].reshape(B, W_out)
+    weights = spread_weights(rng, B, H, W * page)
+    weights[:, 1] = rng.integers(0, 4, weights[:, 1].shape) / 7      # (the border lies among equal ones)
+    weights[0, 2] = 0.25                                             # (all equal)
+    weights[1, 2, ::5] = np.nan
+    start = np.full((B, H, W_out * page), -2.0, np.float32)
+    pool, out = on_gpu(lk, c), dev(start)
+    ws = torch.empty(lk.pages_evict_workspace_bytes(pool, B, W_out), dtype=torch.uint8, device="cuda")
+    lk.lookat_pages_evict(pool, dev(table), i32(*lengths), dev(weights), i32(*keep), dev(table_out), first=4, recent=64, weights_out=out, workspace=ws)
+    after, places, want = evict_reference(c, table, lengths, weights, keep, 4, 64, table_out, start)
+    got = ws.view(torch.int32).view(B, H, W_out * page).cpu().numpy()
+    for (b, h), at in places.items():
+        assert got[b, h, :len(at)].tolist() == at, (b, h)
+    assert np.array_equal(out.cpu().numpy(), want, equal_nan=True)
+    assert_pool(pool, after)
+
+
+def select_reference(x, scores, beams, n):
+    """In 64 bits by a stable sort: scores, parents, tokens, and the least distance between neighbours of different beams that are not equal."""
+    R, V = x.shape
+    s = (x.double() - torch.logsumexp(x.double(), -1, keepdim=True) + scores.double()[:, None]).view(R // beams, beams * V)
+    s, at = torch.where(s.isnan(), -math.inf, s).sort(dim=-1, descending=True, stable=True)
+    s, at = s[:, :n + 1], at[:, :n + 1]
+    row = torch.arange(R // beams, device=x.device)[:, None] * beams + at // V
+    gap = (s[:, :-1] - s[:, 1:])[(row[:, :-1] != row[:, 1:]) & (s[:, :-1] != s[:, 1:]) & s[:, 1:].isfinite()]
+    none = s[:, :n] == -math.inf
+    return s[:, :n], row[:, :n].masked_fill(none, -1), (at % V)[:, :n].masked_fill(none, -1), float(gap.min()) if gap.numel() else math.inf
+
+
+def check_select(lk, x, scores, beams, n):  # noqa: F811
+    want = select_reference(x, scores, beams, n)
+    assert want[3] > 2 * SUM, "the inputs have a near tie"
+    s, parents, tokens = lk.lookat_beam_select(x, scores, beams, n)
+    assert torch.equal(parents.long(), want[1]) and torch.equal(tokens.long(), want[2])
+    ok = want[0].isfinite()
+    assert torch.equal(s.isneginf(), ~ok)
+    assert bool(((s.double() - want[0]).abs() <= SUM + 2.0 ** -24 * want[0].abs())[ok].all())
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("Q,beams,V,n", [(1, 5, 300000, 9), (1, 3, 400001, 64), (2, 17, 70000, 30), (1, 600, 1025, 12), (300, 2, 30001, 5)])
+def test_selection_by_32_logits_a_lane(lk, Q, beams, V, n, dtype):  # noqa: F811
+    """Large launches and many lists.  Beams far apart, so that half-precision logits make no near ties between them."""
+    gen = torch.Generator(device="cuda").manual_seed(V + n)
+    x = torch.randn((Q * beams, V), generator=gen, device="cuda")
+    x = (2 * x + 4 * (x - 2).clamp(min=0)).to(getattr(torch, dtype))
+    if beams > 2:
+        x[1] = -math.inf
+        x[2, : V - 3] = -math.inf
+    # (scores with a near tie between beams are passed over)
+    for seed in range(40):
+        scores = -torch.rand(Q * beams, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda") * 30
+        if select_reference(x, scores, beams, n)[3] > 2 * SUM:
+            break
+    check_select(lk, x, scores, beams, n)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+@pytest.mark.parametrize("n", [1, 40, 64])
+@pytest.mark.parametrize("beams,V", [(1, 40000), (5, 300000)])       # (16 and 32 logits a lane)
+def test_equal_logits(lk, beams, V, n, dtype):  # noqa: F811
+    """More equal logits than a list holds, the n-th of them in either half of its part or between its halves, at the ends of parts and of the row."""
+    at = torch.arange(V, device="cuda")
+    rows = [torch.zeros(V, device="cuda"), (at % 2).float(), (at % 2048 >= 1004).float(), (at % 2048 >= 1084).float() * 2, (at % 2048 >= 2000).float(),
+            (at >= V - 700).float(), torch.where(at % 2 == 0, 0.0, -0.0), torch.where(at == V - 1, 1.0, 0.0), torch.where(at < 30, -math.inf, 3.0)]
+    for row in rows:
+        x = row.to(getattr(torch, dtype)).expand(beams, V).contiguous()
+        scores = torch.zeros(beams, device="cuda")
+        check_select(lk, x, scores, beams, n)
+        check_select(lk, x, scores - 5 * torch.arange(beams, device="cuda"), beams, n)
