@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PoolArgs p, Ev
             octet_has[token / 8] = has;
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
     uint8_t *values = p.values;
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PoolArgs p, Ev
             copy_code(p.codes + (to + (token & (PAGE - 1))) * p.m, p.codes + (from + (pos[g] & (PAGE - 1))) * p.m, p.m, 0);
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
 #pragma unroll 1
