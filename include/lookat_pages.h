@@ -152,6 +152,8 @@ int lookat_attend_pages_chunk(const lookat_page_pool *pool, int32_t B, int32_t N
  * weights held.  A token in a page outside the pool, and a query head whose tokens all have a score of -inf, add nothing; a NaN score or one
  * of +inf makes the weights of its key/value head NaN (that sequence's).  Weights behind a sequence's last token are left as they were.  Every weight
  * has one writer and its sum one order: results are reproducible bit for bit.
+ * One query per query head and call: what the rows of a prompt pay is not summed by lookat_attend_pages_chunk, so after a prompt weights are what
+ * the caller put there, until later queries add theirs (or the prompt's do, a call with their tables for each row that is to count).
  *   lut           [B, H*group, m, 256] fp32, 16-byte aligned;  group 1, 2, 4 or 8
  *   weights       element (b,h,l) at weights[(b*H+h)*weight_stride_bh + l], l < columns <= weight_stride_bh
  *   max_length    the longest length the host knows of, or 0 for W * page: it sizes the launch alone
@@ -176,7 +178,9 @@ int lookat_pages_weigh(const lookat_page_pool *pool, int32_t B, int32_t group,
  * at positions 0..k-1, in their order, as if lookat_pages_write wrote the values that they stand for into an empty sequence: a page's exponent is
  * the least that its tokens allow, so a token is rounded only where its exponent grows, by half a step of the new one at most.  What these
  * pages have behind the last token stays as it was; table, lengths and the books are not changed.  So a user reserves k tokens for an empty slot, calls
- * this with its row, and frees the old slot: pages shared with other sequences are read, not written.
+ * this with its row, and frees the old slot: pages shared with other sequences are read, not written.  Both slots hold pages in between: a pool
+ * that is brought down when it is full keeps ceil(k / page) pages back for each sequence of a call.  Where all weights are equal (zeros after a
+ * prompt) the lowest positions are kept beside the last `recent`.
  * No page of table_out may be named twice or be one that is read.  A kept token in a page outside the pool leaves its place as it was, and so do
  * those whose place is in one.
  *   weights       as in lookat_pages_weigh, read;  keep [B] int32;  first, recent >= 0

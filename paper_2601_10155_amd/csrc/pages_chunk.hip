@@ -14,7 +14,7 @@
 //     is eight consecutive stored bytes, as the page holds them.
 // The centroids are split once per call by a small kernel, into the workspace (or by every workgroup, see below).  A workgroup of NW wavefronts (32 NW
 // rows of one key/value head, query heads of a group side by side) fetches the centroids of KEYS keys by code into LDS, two buffers of as many keys in
-// turn; their ids, codes and centroids are requested three, two and one tiles ahead.
+// turn; their ids, codes, centroids and values are requested four, three, two and one tiles ahead.
 #include "pages_values.h"
 
 namespace lookat {
@@ -141,8 +141,8 @@ __device__ __forceinline__ KeyRange key_range(const ChunkSpan &s, int last_row, 
 
 // Which work a workgroup has.  Units (sequence, head) are dealt to the dies in turn, all workgroups of a unit on one die (they read the same keys,
 // values and centroids); the units that eight dies do not divide are dealt by workgroups.  The last rows come first: they see most.  A die's
-// workgroups go round its 32 compute units, and every second round turns back, so that no compute unit gets the longest of each (prompts of 400 to
-// 1000 rows, all workgroups in flight at once: unit by unit 60.7 us, so 57.9).
+// workgroups go round its 32 compute units, and every second round turns back, so that no compute unit gets the longest of each (us a call, without the turn /
+// so: prompts of 96 heads x 400 to 1000 fp32 rows 48.0 / 47.0, 64 x 1000 fp16 rows 41.6 / 40.6, but 96 x 400 to 1000 fp16 40.8 / 41.3).
 struct Place {
     int unit, tile, split;
     bool any;
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(NW *kWave, kChunkWaves) void chunk_kernel(PoolArgs 
 // the two blocks of 16 such that a lane's eight scores belong to one octet.
 // A workgroup of eight wavefronts splits its head's codebook itself, into LDS (64 or 128 KB), and looks its operands up there; one of two takes them from the
 // books in memory.  Looked up in memory by eight wavefronts a tile's operands were 4 KB to 16 KB of scattered 64-byte pieces: us a call, so / from LDS, 16 x 12
-// x 8 rows behind 1000 tokens 18.0 / 11.1, 32 x 2 behind 20000, d_k = 128 62.8 / 30.3, 1280 x 2 behind 200 to 2000, d_k = 128 144 / 81.
+// x 8 rows behind 1000 tokens 15.9 / 9.7, 32 x 2 behind 20000, d_k = 128 56.0 / 27.8, 1280 x 2 behind 200 to 2000, d_k = 128 118 / 76.
 constexpr int kFewWaves = 8, kBriefWaves = 2, kFewKeys = 32;
 __host__ __device__ constexpr bool few_staged(int waves) { return waves == kFewWaves; }
 __host__ __device__ constexpr size_t few_lds_bytes(int d_k, int waves) { return (size_t)waves * 16 * (d_k + 4) * 4 + waves * 16 * 8; }
@@ -1038,17 +1038,18 @@ static ChunkCut chunk_cut(const lookat_page_pool *p, int32_t B, int32_t N, int32
     ChunkCut c;
     const int64_t units = (int64_t)B * p->H, rows = (int64_t)N * group;
     // The kernel for few rows, us a call with it / without.  One tile of its rows, or few workgroups: 240 (sequence, head) pairs x 32 rows x 632 tokens, d_k = 128
-    // 17.5 / 44, 8 x 48 x 248, d_k = 64 9.0 / 16.5, 40 x 256 x 1256 25 / 36, 16 x 1024 x 9024, d_k = 128 158 / 184, 1 x 2048 x 10048 38 / 59.  Two tiles at d_k = 64:
-    // 400 x 64 x 664 37 / 45, but at d_k = 128 60 / 62 and, fp32 rows, 70 / 87, though 1264 tokens 88 / 100.  Some more where there is more to see: 200 x 128 x
-    // 1028 75 / 86, but 200 x 128 x 228 31 / 20, 400 x 96 x 996 101 / 81, 96 x 600 x 600 56 / 33.
+    // 17.8 / 46, 8 x 48 x 248, d_k = 64 8.9 / 15.7, 40 x 256 x 1256 26 / 33, 16 x 1024 x 9024, d_k = 128 155 / 181, 1 x 2048 x 10048 25 / 41.  Two tiles at d_k = 64:
+    // 400 x 64 x 664 29 / 37, but at d_k = 128 61 / 57 and, fp32 rows, 79 / 67, though 1264 tokens 81 / 93.  Some more where there is more to see: 200 x 128 x
+    // 1028, d_k = 128 73 / 86, but 200 x 128 x 228 31 / 30, 400 x 96 x 996 91 / 80, 96 x 600 x 600 98 / 47.
     const int64_t room = (int64_t)W * p->page, longest = max_length > 0 && max_length < room ? max_length : room, groups = units * ((rows + 31) / 32);
     const bool few = rows <= 32 || groups <= 512 || (rows <= 64 && p->d_k == 64) || ((rows <= 64 || groups <= 1024) && longest > 1000);
     c.few = !few ? 0 : rows <= 16 ? 1 : 2;
-    // (Without it: 256 rows to a workgroup where they read long sequences and fill the chip, 128 otherwise: us a call, 256 / 128, 32 x 2048 x 32049 1987 / 2169,
-    // 128 x 1000 x 5000 572 / 625, 128 x 2000 x 2000 326 / 321, 96 x 600 x 2600 259 / 173, 320 x 380 x 880 170 / 129.)
+    // (Without it: 256 rows to a workgroup where they read long sequences and fill the chip, 128 otherwise: us a call at d_k = 128, 256 / 128, 32 x 2048 x 32049
+    // 1917 / 2209, 128 x 1000 x 5000 575 / 634, 128 x 2000 x 2000 315 / 322, 96 x 600 x 2600 268 / 176, 320 x 380 x 880 167 / 125.)
     // Its workgroups have eight wavefronts, or two where there are many and a head has little to see, not worth its centroids in LDS: us a call, eight / two,
-    // 768 x 8 rows x 8 tokens 13.2 / 9.8, 768 x 12 x 128, d_k = 128 26.4 / 17.8, 1280 x 8 x 308 24.3 / 26.8, 375 x 1 x 32 10.1 / 11.6, 400 x 20 x 70, d_k = 128 24.9 / 22.2, 400 x 20 x 320 28.9 / 31.4, 1280 x 20 x 320 62.6 / 49.1,
-    // 1280 x 32 x 632 82 / 95, d_k = 64 400 x 64 x 1264 60.5 / 54.1.
+    // d_k = 64 768 x 8 rows x 8 tokens 13.1 / 9.4, 1280 x 8 x 308 23.3 / 23.5, 375 x 1 x 32 8.8 / 9.6, 400 x 20 x 320 16.8 / 16.6, 400 x 64 x 1264 51.3 / 47.2; d_k = 128
+    // 768 x 12 x 128 26.1 / 20.9, 400 x 20 x 70 21.7 / 17.0 (fp32 rows 26.4 / 18.6), 400 x 20 x 320 25.1 / 27.0 (32.5 / 33.2), 1280 x 20 x 320 61.7 / 47.4
+    // (79 / 71), 1280 x 32 x 632 77 / 76 (100 / 123).
     const int64_t brief = groups <= (rows <= 16 ? 512 : 256) ? 0 : rows <= 16 ? 256 : groups <= 512 ? 128 : rows <= 32 || p->d_k == 128 ? 448 : 1536;
     c.waves = c.few ? (longest > brief ? kFewWaves : kBriefWaves)
                     : p->d_k == 128 && rows >= 768 && longest > 2048 && units * ((rows + 255) / 256) >= 256 ? 8 : 4;
@@ -1089,8 +1090,8 @@ static int check_chunk(const lookat_page_pool *pool, int32_t B, int32_t N, int32
     return LOOKAT_OK;
 }
 
-// Tokens of a tile: 64, or 32 at d_k = 128 where fp32 rows take the registers or the workgroup is small.  (d_k = 64, us a call, 32 / 64: 32 x 2048 rows 77 / 67,
-// behind 2000 tokens 142 / 125, 64 x 1000 fp32 48.0 / 44.6, 8 x 12 x 400 to 1000 fp32 53.3 / 51.2.)
+// Tokens of a tile: 64, or 32 at d_k = 128 where fp32 rows take the registers or the workgroup is small.  (d_k = 64, us a call, 32 / 64: 32 x 2048 rows 78 / 68,
+// behind 2000 tokens 152 / 140, 64 x 1000 fp32 47.7 / 44.1, 96 heads x 400 to 1000 fp32 47.6 / 47.0.)
 constexpr int chunk_keys(int d_k, int waves, bool q32) { return d_k == 64 || (waves == 8 && !q32) ? 64 : 32; }
 
 template <int DK, bool SMALL, int NW>
