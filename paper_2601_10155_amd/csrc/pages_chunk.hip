@@ -1023,7 +1023,7 @@ __global__ void chunk_merge_kernel(ChunkArgs a, int H, int d_k, int page_log2, i
         z = fmaf(f, x[d_k + 1], z * fix);
         top = to;
     }
-    a.out[((int64_t)(b * H * a.group + hq) * a.N + n) * d_k + d] = z == 0.f ? 0.f : o / z;
+    a.out[((int64_t)(b * H * a.group + hq) * a.N + n) * d_k + d] = z == 0.f ? o * 0.f : o / z;     // (nothing to sum: zeros, but a stored NaN stays one)
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------

@@ -114,6 +114,29 @@ def test_a_scale_of_nan(lk, B, H, g, N, before, d_k, m, page, splits, dtype, kin
         assert bool(one[1:].isnan().all()) and not one[0].any()
 
 
+@pytest.mark.parametrize("N,H,splits", [(4, 2, 1), (4, 2, 3), (200, 60, 1), (200, 60, 2)])
+@pytest.mark.parametrize("d_k,m", [(64, 8), (128, 16)])
+def test_a_stored_nan_among_scores_of_minus_infinity(lk, N, H, splits, d_k, m):  # noqa: F811
+    """A row whose scores are all -inf gives zeros, but NaN at the coordinates at which it sees one, whether its tokens are cut into ranges or not."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    n, page = N + 100, 32
+    W = -(-n // page)
+    stored = (torch.randn((W, H, page // 8, d_k, 8), generator=gen, device="cuda") * 30).to(torch.float8_e4m3fn).view(torch.uint8)
+    at = n - 1 - N // 2
+    stored[at // page, :, at % page // 8, 3, at % 8] = 0x7f
+    stored[1, 0, 0, 7, 5] = 0xff                      # (one that all rows see)
+    pool = lk.PagePool(torch.randint(0, 256, (W, H, page, m), generator=gen, device="cuda", dtype=torch.uint8), stored.view(torch.float8_e4m3fn),
+                       torch.zeros((W, H), dtype=torch.int8, device="cuda"))
+    books = torch.rand((H, m, 256, d_k // m), generator=gen, device="cuda") + 0.5
+    q = -torch.rand((1, H, N, d_k), generator=gen, device="cuda") - 0.5
+    got = lk.lookat_attend_pages_chunk(q, books, pool, torch.arange(W, dtype=torch.int32, device="cuda")[None], i32(n), 3e38, num_splits=splits)
+    want = torch.zeros_like(got)
+    want[0, :, at - (n - N):, 3] = math.nan
+    want[0, 0, :, 7] = math.nan
+    assert torch.equal(got.isnan(), want.isnan())
+    assert not got.nan_to_num(0.0).any()
+
+
 SUM = 2.0 ** -18       # of a row's sum of exponentials (include/lookat_search.h); a score is off by as much, and by its own rounding
 
 
