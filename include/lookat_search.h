@@ -25,8 +25,9 @@ extern "C" {
  * candidates the rest is -inf, -1, -1.
  *   logits        fp16 or fp32, element (r,v) at logits[r*logit_stride + v], logit_stride >= V; any alignment of its type
  *   scores        [Q*beams] fp32
- *   scores_out    [Q,n] fp32;  tokens [Q,n] int32;  parents [Q,n] int32: first_parent + r, what lookat_pages_fork takes as sources if the beams'
- *                 sequences are the slots from first_parent on (a -1 is passed over there)
+ *   scores_out    [Q,n] fp32, which may be scores where n = beams;  tokens [Q,n] int32
+ *   parents       [Q,n] int32: first_parent + r, what lookat_pages_fork takes as sources if the beams' sequences are the slots from first_parent on
+ *                 (a -1 is passed over there)
  *   workspace     lookat_beam_select_workspace_bytes(Q, beams, V, n) bytes, 16-byte aligned; calls in flight at once must not share one
  * Supported: 1 <= n <= 64, 1 <= beams <= 1024, Q*beams <= 65535, V <= 2^24; otherwise LOOKAT_ERR_UNSUPPORTED or LOOKAT_ERR_SHAPE.
  */

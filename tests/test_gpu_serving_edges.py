@@ -243,3 +243,26 @@ def test_equal_logits(lk, beams, V, n, dtype):  # noqa: F811
         scores = torch.zeros(beams, device="cuda")
         check_select(lk, x, scores, beams, n)
         check_select(lk, x, scores - 5 * torch.arange(beams, device="cuda"), beams, n)
+
+
+def test_scores_in_place(lk):  # noqa: F811
+    """A search step whose scores take the place of the last ones (as many beams as before), eager and replayed."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    Q, beams, V = 40, 5, 3001
+    x = torch.randn((Q * beams, V), generator=gen, device="cuda")
+    start = -torch.rand(Q * beams, generator=gen, device="cuda")
+    want = lk.lookat_beam_select(x, start, beams, beams)
+    scores = start.clone()
+    parents, tokens = torch.empty((Q, beams), dtype=torch.int32, device="cuda"), torch.empty((Q, beams), dtype=torch.int32, device="cuda")
+    ws = torch.empty(lk.beam_select_workspace_bytes(Q, beams, V, beams), dtype=torch.uint8, device="cuda")
+    step = lambda: lk.lookat_beam_select(x, scores, beams, beams, scores_out=scores.view(Q, beams), parents=parents, tokens=tokens, workspace=ws)  # noqa: E731
+    step()
+    assert torch.equal(scores.view(Q, beams), want[0]) and torch.equal(parents, want[1]) and torch.equal(tokens, want[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        want = lk.lookat_beam_select(x, scores.clone(), beams, beams)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(scores.view(Q, beams), want[0]) and torch.equal(parents, want[1]) and torch.equal(tokens, want[2])
