@@ -32,7 +32,8 @@ CHUNKS = [
     (40, 16, 4, 4, 60, 128, 16, 64, 0),
     (40, 16, 1, 50, 20, 64, 8, 32, 0),        # two wavefronts, two blocks, centroids of eight coordinates
     (8, 3, 2, 8, 200, 64, 16, 64, 0),         # one block, centroids of four, eight wavefronts and two
-    (40, 16, 4, 4, 60, 64, 16, 64, 0)]
+    (40, 16, 4, 4, 60, 64, 16, 64, 0),
+    (40, 16, 5, 6, 100, 128, 4, 128, 3)]      # two wavefronts in ranges, the last of them short
 
 
 @pytest.mark.parametrize("dtype", ["float16", "float32"])
